@@ -7,6 +7,9 @@ output and workspace tensors).  Every step of the computation runs in the HIP
 kernels of ``libelas.so``; there is no fallback: if the library is not built,
 or a tensor is not on the GPU, the call raises.
 
+The operators around the FFN in a training step (norms, embedding, gradient
+clipping; ``include/elas_train.h``) are in ``train`` and exported here too.
+
 bf16 tensors use ``torch.bfloat16``; the compressed 2:4 metadata uses
 ``torch.uint8``; weight gradients are ``torch.float32``.
 """
@@ -58,6 +61,7 @@ _lib = None
 _p = ctypes.c_void_p
 _i64 = ctypes.c_int64
 _u32 = ctypes.c_uint32
+_f32 = ctypes.c_float
 _sz = ctypes.c_size_t
 
 _SIGNATURES = {
@@ -424,3 +428,9 @@ def elas_timing_collect() -> dict:
         _check(L.elas_timing_entry(i, buf, 128, ctypes.byref(launches), ctypes.byref(ms)))
         out[buf.value.decode()] = (launches.value, ms.value)
     return out
+
+
+from . import train  # noqa: E402  (needs the names above)
+from .train import *  # noqa: E402,F401,F403
+
+__all__ += train.__all__

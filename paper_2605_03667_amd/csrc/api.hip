@@ -11,8 +11,10 @@
 #include "internal.h"
 
 namespace {
-
 thread_local std::string g_last_error;
+}
+
+namespace elas {
 
 int fail(int code, const char* fmt, ...) {
   char buf[512];
@@ -24,32 +26,34 @@ int fail(int code, const char* fmt, ...) {
   return code;
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+void begin_call() {
+  g_last_error.clear();
+  debug_sync_reset();
+}
 
-// NULL / alignment check of one device pointer.
 int check_ptr(const void* p, const char* name) {
   if (p == nullptr) return fail(ELAS_ERR_NULL, "%s is NULL", name);
-  if (!aligned16(p)) return fail(ELAS_ERR_ALIGN, "%s is not 16-byte aligned", name);
+  if (((uintptr_t)p & 15u) != 0) return fail(ELAS_ERR_ALIGN, "%s is not 16-byte aligned", name);
   return ELAS_OK;
 }
 
-#define ELAS_CHECK(expr)            \
-  do {                              \
-    int rc_ = (expr);               \
-    if (rc_ != ELAS_OK) return rc_; \
-  } while (0)
-
-// Status of a launch sequence: its own error, else (ELAS_DEBUG_SYNC) the
-// first failure seen when synchronising after one of its kernels.
 int device_status(hipError_t e, const char* what) {
   if (e != hipSuccess) return fail(ELAS_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
   const char* tag = nullptr;
-  const hipError_t d = elas::debug_sync_error(&tag);
+  const hipError_t d = debug_sync_error(&tag);
   if (d != hipSuccess)
     return fail(ELAS_ERR_DEVICE, "%s: kernel %s failed (ELAS_DEBUG_SYNC): %s", what, tag ? tag : "?",
                 hipGetErrorString(d));
   return ELAS_OK;
 }
+
+}  // namespace elas
+
+namespace {
+
+using elas::check_ptr;
+using elas::device_status;
+using elas::fail;
 
 // Sizes are bounded so every element offset fits comfortably in int64 and in
 // the 32-bit grid dimensions used by the launchers.
@@ -182,8 +186,7 @@ int64_t elas_meta_ld(int64_t N) { return N > 0 ? elas::meta_ld(N) : 0; }
 
 int elas_sparsify_24(const uint16_t* h, int64_t M, int64_t N, uint32_t flags, uint16_t* vals,
                      uint8_t* meta, void* stream) {
-  g_last_error.clear();
-  elas::debug_sync_reset();
+  elas::begin_call();
   if (flags & ~ELAS_SPARSIFY_RAW) return fail(ELAS_ERR_FLAGS, "unknown flags 0x%x", flags);
   if (M < 0 || M > kMaxDim) return fail(ELAS_ERR_SHAPE, "M=%lld out of range", (long long)M);
   if (N <= 0 || N % 8 || N > kMaxDim)
@@ -208,8 +211,7 @@ size_t elas_spmm_24_workspace_bytes(int64_t M, int64_t K, int64_t N, int b_layou
 int elas_spmm_24(const uint16_t* a_vals, const uint8_t* a_meta, int64_t M, int64_t K, const uint16_t* b,
                  int64_t N, int b_layout, uint16_t* c, void* workspace, size_t workspace_bytes,
                  void* stream) {
-  g_last_error.clear();
-  elas::debug_sync_reset();
+  elas::begin_call();
   if (b_layout != ELAS_B_KN && b_layout != ELAS_B_NK)
     return fail(ELAS_ERR_FLAGS, "b_layout must be ELAS_B_KN or ELAS_B_NK");
   if (M < 0 || M > kMaxDim) return fail(ELAS_ERR_SHAPE, "M=%lld out of range", (long long)M);
@@ -240,8 +242,7 @@ int elas_lowrank_ffn_fwd(const uint16_t* x, const uint16_t* U_up, const uint16_t
                          const uint16_t* V_down, int64_t T, int64_t d, int64_t d_ff, int64_t r, uint32_t flags,
                          uint16_t* y, uint16_t* P, uint16_t* s_vals, uint8_t* s_meta, uint16_t* Z,
                          void* workspace, size_t workspace_bytes, void* stream) {
-  g_last_error.clear();
-  elas::debug_sync_reset();
+  elas::begin_call();
   elas::FfnArgs a{};
   bool noop = false;
   ELAS_CHECK(prepare_fwd(x, U_up, V_up, U_down, V_down, T, d, d_ff, r, flags, y, P, s_vals, s_meta, Z, a, noop));
@@ -260,8 +261,7 @@ int elas_lowrank_ffn_fwd_noalloc(const uint16_t* x, const uint16_t* U_up, const 
                                  const uint16_t* U_down, const uint16_t* V_down, int64_t T, int64_t d, int64_t d_ff,
                                  int64_t r, uint32_t flags, uint16_t* y, uint16_t* P, uint16_t* s_vals,
                                  uint8_t* s_meta, uint16_t* Z, void* stream) {
-  g_last_error.clear();
-  elas::debug_sync_reset();
+  elas::begin_call();
   elas::FfnArgs a{};
   bool noop = false;
   ELAS_CHECK(prepare_fwd(x, U_up, V_up, U_down, V_down, T, d, d_ff, r, flags, y, P, s_vals, s_meta, Z, a, noop));
@@ -286,8 +286,7 @@ int elas_lowrank_ffn_bwd(const uint16_t* dy, const uint16_t* x, const uint16_t* 
                          int64_t r, uint32_t flags, const uint16_t* P, const uint16_t* s_vals,
                          const uint8_t* s_meta, const uint16_t* Z, uint16_t* dx, float* dU_up, float* dV_up,
                          float* dU_down, float* dV_down, void* workspace, size_t workspace_bytes, void* stream) {
-  g_last_error.clear();
-  elas::debug_sync_reset();
+  elas::begin_call();
   if (flags & ~(ELAS_MODE_DENSE | ELAS_BWD_STE))
     return fail(ELAS_ERR_FLAGS, "backward flags: only ELAS_MODE_DENSE or ELAS_BWD_STE are allowed");
   const bool dense = (flags & ELAS_MODE_DENSE) != 0, ste = (flags & ELAS_BWD_STE) != 0;
@@ -328,8 +327,7 @@ int elas_lowrank_ffn_bwd(const uint16_t* dy, const uint16_t* x, const uint16_t* 
 
 int elas_fullrank_ffn_fwd(const uint16_t* x, const uint16_t* W_up, const uint16_t* W_down, int64_t T, int64_t d,
                           int64_t d_ff, uint16_t* y, uint16_t* S, void* stream) {
-  g_last_error.clear();
-  elas::debug_sync_reset();
+  elas::begin_call();
   ELAS_CHECK(check_ffn_dims(T, d, d_ff, 8));
   if (T == 0) return ELAS_OK;
   ELAS_CHECK(check_ptr(x, "x"));

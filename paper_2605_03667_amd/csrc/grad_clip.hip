@@ -1,0 +1,221 @@
+// Global norm of the gradients over many tensors, and their clipping (the formulas
+// are in include/elas_train.h).
+//
+// Two launches for up to kTensors tensors: the squares, as one 64-bit partial sum
+// per workgroup, and the scaling, in which every workgroup adds up the partial sums
+// for itself (16 KB from L2) instead of waiting for a launch that does it once.
+// Tensors are cut into pieces of kPiece values; the pieces of all tensors of a
+// launch are numbered through and dealt out to the workgroups in turn, so that one
+// long tensor and a hundred short ones load the card alike.  Bound by HBM: one read for
+// the norm, one read and one write for the scaling.  The scaling takes the pieces in
+// the opposite order, so that it begins with what the caches still hold.
+#include <math.h>
+
+#include <algorithm>
+
+#include "../../include/elas_train.h"
+#include "internal.h"
+#include "rows.h"
+
+namespace elas {
+
+namespace {
+
+constexpr int kTensors = 128;     // per launch: the table below is a kernel argument (< 4 KB)
+constexpr int kPiece = 8192;      // values
+constexpr int kGroups = 2048;     // most workgroups, and partial sums, per launch
+
+struct GradTable {
+  const void* in[kTensors];
+  void* out[kTensors];
+  int64_t n[kTensors];
+  uint32_t first[kTensors + 1];   // number of each tensor's first piece; [count] = pieces in all
+  uint32_t bf16[kTensors / 32];   // bit k: tensor k is bf16
+  int count;
+};
+
+// (tensors need their element's alignment only: 16-byte accesses at any such address)
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+
+// Values of one thread in a full piece: 32, as 16-byte parts of which part k of all
+// threads is contiguous.
+__device__ __forceinline__ void load_part(const float* p, float (&v)[4]) {
+  const f32x4 q = *(const f32x4_any*)p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = q[i];
+}
+__device__ __forceinline__ void load_part(const uint16_t* p, float (&v)[8]) {
+  const u32x4 q = *(const u32x4_any*)p;
+  unpack8(make_uint4(q[0], q[1], q[2], q[3]), v);
+}
+__device__ __forceinline__ void store_part(float* p, const float (&v)[4]) {
+  *(f32x4_any*)p = f32x4{v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ void store_part(uint16_t* p, const float (&v)[8]) {
+  *(u32x4_any*)p = u32x4{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3]), bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7])};
+}
+__device__ __forceinline__ float value_of(float e) { return e; }
+__device__ __forceinline__ float value_of(uint16_t e) { return __builtin_bit_cast(float, (uint32_t)e << 16); }
+__device__ __forceinline__ void set_value(float* p, float v) { *p = v; }
+__device__ __forceinline__ void set_value(uint16_t* p, float v) { *p = (uint16_t)bf16x2_rne(v, 0.f); }
+
+// Squares are taken in 64 bits: exact for every float, and no sum of them overflows.
+template <class E>
+__device__ __forceinline__ void square_piece(const E* g, int64_t n, double (&s)[2]) {
+  constexpr int N = 16 / sizeof(E), PARTS = 32 / N;
+  float v[PARTS][N];
+  if (n >= kPiece) {
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) load_part(g + (k * 256 + threadIdx.x) * N, v[k]);
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i & 1] = fma((double)v[k][i], (double)v[k][i], s[i & 1]);
+    return;
+  }
+  for (int64_t i = threadIdx.x; i < n; i += 256) {
+    const double x = value_of(g[i]);
+    s[0] = fma(x, x, s[0]);
+  }
+}
+
+// Piece c's tensor, walking from tensor k (either way), and whether it is bf16.
+__device__ __forceinline__ int tensor_of(const uint32_t* first, uint32_t c, int k) {
+  while (c >= first[k + 1]) ++k;
+  while (c < first[k]) --k;
+  return k;
+}
+
+__global__ __launch_bounds__(256) void grad_square_kernel(const GradTable g, double* part) {
+  __shared__ double red[4];
+  __shared__ uint32_t first[kTensors + 1];
+  for (int k = threadIdx.x; k <= g.count; k += 256) first[k] = g.first[k];
+  __syncthreads();
+  const uint32_t pieces = first[g.count];
+  double s[2] = {0.0, 0.0};
+  int k = 0;
+  for (uint32_t c = blockIdx.x; c < pieces; c += gridDim.x) {
+    k = __builtin_amdgcn_readfirstlane(tensor_of(first, c, k));
+    const int64_t at = (int64_t)(c - first[k]) * kPiece, n = g.n[k] - at;
+    if (g.bf16[k >> 5] >> (k & 31) & 1u)
+      square_piece((const uint16_t*)g.in[k] + at, n, s);
+    else
+      square_piece((const float*)g.in[k] + at, n, s);
+  }
+  const double sum = block_sum<4>(s[0] + s[1], red);
+  if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+// Norm from the partial sums, in the same order in every workgroup.
+__device__ __forceinline__ double norm_of(const double* part, int64_t parts, double* red) {
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < parts; i += 256) s += part[i];
+  return sqrt(block_sum<4>(s, red));
+}
+
+__global__ __launch_bounds__(256) void grad_norm_kernel(const double* part, int64_t parts, float* norm) {
+  __shared__ double red[4];
+  const double v = norm_of(part, parts, red);
+  if (threadIdx.x == 0) norm[0] = (float)v;
+}
+
+template <class E>
+__device__ __forceinline__ void scale_piece(const E* g, E* out, int64_t n, float f) {
+  constexpr int N = 16 / sizeof(E), PARTS = 32 / N;
+  if (n >= kPiece) {
+    float v[PARTS][N];
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) load_part(g + (k * 256 + threadIdx.x) * N, v[k]);
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[k][i] *= f;
+      store_part(out + (k * 256 + threadIdx.x) * N, v[k]);
+    }
+    return;
+  }
+  for (int64_t i = threadIdx.x; i < n; i += 256) set_value(out + i, value_of(g[i]) * f);
+}
+
+// stats NULL: another launch writes them.
+__global__ __launch_bounds__(256) void grad_scale_kernel(const GradTable g, const double* part, int64_t parts, float max_norm, float* stats) {
+  __shared__ double red[4];
+  __shared__ uint32_t first[kTensors + 1];
+  for (int k = threadIdx.x; k <= g.count; k += 256) first[k] = g.first[k];
+  const double norm = norm_of(part, parts, red);   // (its barriers are passed before `first` is read)
+  const bool finite = norm < (double)INFINITY, clips = finite && norm > (double)max_norm;
+  const float factor = clips ? (float)((double)max_norm / norm) : 1.f;
+  if (stats && blockIdx.x == 0 && threadIdx.x == 0) {
+    stats[0] = (float)norm;
+    stats[1] = finite ? factor : 0.f;
+  }
+  const uint32_t pieces = first[g.count];
+  int k = g.count - 1;
+  for (uint32_t i = blockIdx.x; i < pieces; i += gridDim.x) {
+    const uint32_t c = pieces - 1 - i;
+    k = __builtin_amdgcn_readfirstlane(tensor_of(first, c, k));
+    if (!clips && g.in[k] == g.out[k]) continue;
+    const int64_t at = (int64_t)(c - first[k]) * kPiece, n = g.n[k] - at;
+    if (g.bf16[k >> 5] >> (k & 31) & 1u)
+      scale_piece((const uint16_t*)g.in[k] + at, (uint16_t*)g.out[k] + at, n, factor);
+    else
+      scale_piece((const float*)g.in[k] + at, (float*)g.out[k] + at, n, factor);
+  }
+}
+
+// The table of the tensors k0 .. of one launch (empty ones take no piece).
+void fill(GradTable& g, const void* const* in, void* const* out, const int64_t* numel, const int32_t* dtype, int64_t k0, int64_t n) {
+  g.count = (int)std::min<int64_t>(kTensors, n - k0);
+  uint32_t pieces = 0;
+  for (int k = 0; k < kTensors / 32; ++k) g.bf16[k] = 0;
+  for (int k = 0; k < g.count; ++k) {
+    g.in[k] = in[k0 + k];
+    g.out[k] = out ? out[k0 + k] : nullptr;
+    g.n[k] = numel[k0 + k];
+    g.first[k] = pieces;
+    pieces += (uint32_t)((g.n[k] + kPiece - 1) / kPiece);
+    if (dtype[k0 + k] == ELAS_GRAD_BF16) g.bf16[k >> 5] |= 1u << (k & 31);
+  }
+  g.first[g.count] = pieces;
+}
+
+int64_t launches(int64_t n) { return (n + kTensors - 1) / kTensors; }
+
+}  // namespace
+
+size_t grad_workspace_bytes(int64_t n) { return (size_t)launches(n) * kGroups * sizeof(double); }
+
+hipError_t run_grad_norm(const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype, int64_t n, bool clip,
+                         float max_norm, float* stats, void* ws, hipStream_t stream) {
+  double* part = (double*)ws;
+  int64_t parts = 0;
+  GradTable g;
+  for (int64_t k = 0; k < n; k += kTensors) {
+    fill(g, grads, out, numel, dtype, k, n);
+    const unsigned groups = std::min<uint32_t>(g.first[g.count], kGroups);
+    if (groups == 0) continue;
+    TimedLaunch tl("grad_square", stream);
+    hipLaunchKernelGGL(grad_square_kernel, dim3(groups), dim3(256), 0, stream, g, part + parts);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    parts += groups;
+  }
+  if (!clip) {
+    TimedLaunch tl("grad_norm", stream);
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, stream, part, parts, stats);
+    return hipGetLastError();
+  }
+  // (one launch at least, which writes the statistics where there are no values)
+  for (int64_t l = std::max<int64_t>(launches(n), 1) - 1; l >= 0; --l) {
+    fill(g, grads, out, numel, dtype, l * kTensors, n);
+    TimedLaunch tl("grad_scale", stream);
+    hipLaunchKernelGGL(grad_scale_kernel, dim3(std::max(1u, std::min<uint32_t>(g.first[g.count], kGroups))), dim3(256), 0, stream, g, part,
+                       parts, max_norm, l == 0 ? stats : nullptr);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace elas
