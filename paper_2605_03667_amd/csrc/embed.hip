@@ -1,5 +1,14 @@
 // Token embedding with scaling, and its gradient by sorted tokens (the formulas
 // are in include/elas_train.h).
+//
+// The lookup is a copy bound by HBM and by latency: a wave takes 4 pieces of 512
+// features at a time, of one token or of several, so that 4 rows are on their way at
+// once.
+//
+// The gradient sorts the tokens by id first (stably, so that every row's sum has one
+// order) and then walks the sorted tokens and the table's rows together.  The sort
+// works on 4 to 8 bytes a token and is bound by latency and launches; the sum reads dx
+// and writes the table once and is bound by HBM.
 #include <algorithm>
 
 #include "internal.h"
@@ -11,180 +20,525 @@ namespace {
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-__device__ __forceinline__ int64_t id_at(const void* ids, bool i64, int64_t t) {
-  return i64 ? ((const int64_t*)ids)[t] : (int64_t)((const int32_t*)ids)[t];
+__device__ __forceinline__ int64_t id_at(const EmbedArgs& a, int64_t t) {
+  return a.ids_i64 ? ((const int64_t*)a.ids)[t] : (int64_t)((const int32_t*)a.ids)[t];
+}
+// Sort key of a token: its id, V where that is outside the table.
+__device__ __forceinline__ uint32_t key_at(const EmbedArgs& a, int64_t t) {
+  const int64_t id = id_at(a, t);
+  return id >= 0 && id < a.V ? (uint32_t)id : (uint32_t)a.V;
 }
 
+// ---- lookup -----------------------------------------------------------------------
+
+// Parts of 512 features of consecutive tokens, numbered through; a wave takes 4 of
+// them, `parts` to a token.
 template <class R>
-__global__ __launch_bounds__(256) void embed_fwd_kernel(const EmbedArgs a) {
-  const int64_t pieces = a.d / 8, total = a.T * pieces;
-  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
-    const int64_t t = q / pieces, c = (q - t * pieces) * 8;
-    const int64_t id = id_at(a.ids, a.ids_i64, t);
-    float v[8] = {};
-    if (id >= 0 && id < a.V) {
-      load8(a.table + id * a.d + c, v);
+__global__ __launch_bounds__(256) void embed_fwd_kernel(const EmbedArgs a, uint32_t parts) {
+  const uint32_t lane = threadIdx.x & 63;
+  const int64_t waves = (int64_t)gridDim.x * 4, total = a.T * parts;
+  for (int64_t q0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 4; q0 < total; q0 += waves * 4) {
+    int64_t t = q0 / parts;   // (the one division of a wave's turn)
+    uint32_t part = (uint32_t)(q0 - t * parts);
+    Piece<uint16_t> row[4];
+    int64_t at[4];
+    bool ok[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t c = part * 512 + lane * 8;
+      ok[k] = t < a.T && c < (uint32_t)a.d;
+      const uint32_t key = t < a.T ? key_at(a, t) : (uint32_t)a.V;
+      row[k].load(a.table + (int64_t)key * a.d + c, ok[k] && key < (uint32_t)a.V);
+      at[k] = t * a.d + c;
+      if (++part == parts) part = 0, ++t;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float v[8];
+      row[k].get(v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= a.scale;
+      if (ok[k]) store8((R*)a.x + at[k], v);
     }
-    store8((R*)a.x + t * a.d + c, v);
   }
 }
 
-// ---- the gradient ----------------------------------------------------------------
-// Tokens are sorted by id with a stable radix sort of 8 bits a pass (ids outside
-// the table become V and sort behind all others); workgroup c holds the tokens
-// c * kChunk ...  Then one workgroup adds up the tokens of each row of the table.
-constexpr int kChunk = 2048;
+// ---- the sort -----------------------------------------------------------------------
+// Least significant digit first, at most 9 bits a pass.  A workgroup of 16 waves takes
+// 1024 E tokens, wave w the E rounds of 64 from w 64 E on, so that (wave, round, lane)
+// is the order of the tokens.  One LDS counter for each wave and digit: of the lanes of
+// a round that hold the same digit the lowest adds their number to the counter, and
+// what it held before plus the number of lower such lanes is the token's place among
+// the wave's tokens of that digit.  LDS operations of a wave are done in order, so the
+// rounds need no wait between them.
+constexpr int kDigits = 512;
 
-__global__ __launch_bounds__(256) void embed_keys_kernel(const EmbedArgs a, uint32_t* key, uint32_t* pos) {
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t >= a.T) return;
-  const int64_t id = id_at(a.ids, a.ids_i64, t);
-  key[t] = id >= 0 && id < a.V ? (uint32_t)id : (uint32_t)a.V;
-  pos[t] = (uint32_t)t;
+// Places among the wave's own tokens of the same digit.
+template <int E>
+__device__ __forceinline__ void wave_ranks(const uint32_t (&digit)[E], const bool (&ok)[E], int bits, uint32_t* count, uint32_t (&rank)[E]) {
+  const uint32_t lane = threadIdx.x & 63;
+  uint32_t before[E], lower[E];
+  int leader[E];
+#pragma unroll
+  for (int r = 0; r < E; ++r) {
+    uint64_t same = __ballot(ok[r]);
+    for (int b = 0; b < bits; ++b) {
+      const bool set = (digit[r] >> b) & 1u;
+      const uint64_t m = __ballot(set);
+      same &= set ? m : ~m;
+    }
+    lower[r] = __popcll(same & ((1ull << lane) - 1));
+    leader[r] = __ffsll((unsigned long long)same) - 1;
+    before[r] = 0;
+    if (ok[r] && lower[r] == 0) before[r] = atomicAdd(&count[digit[r]], (uint32_t)__popcll(same));
+  }
+#pragma unroll
+  for (int r = 0; r < E; ++r) rank[r] = __shfl(before[r], ok[r] ? leader[r] : 0) + lower[r];
 }
 
-__global__ __launch_bounds__(256) void embed_hist_kernel(const uint32_t* key, int64_t T, int shift, uint32_t* hist) {
-  __shared__ uint32_t n[256];
-  n[threadIdx.x] = 0;
-  __syncthreads();
-  for (int64_t i = threadIdx.x; i < kChunk; i += 256) {
-    const int64_t t = (int64_t)blockIdx.x * kChunk + i;
-    if (t < T) atomicAdd(&n[(key[t] >> shift) & 255u], 1u);
+// Exclusive prefix sums over `bins` <= 512 values, one per thread 0 .. bins - 1.
+__device__ __forceinline__ uint32_t bin_scan(uint32_t v, int bins, uint32_t* tmp) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t s = v;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const uint32_t o = __shfl_up(s, m);
+    if (lane >= m) s += o;
   }
-  __syncthreads();
-  hist[(int64_t)blockIdx.x * 256 + threadIdx.x] = n[threadIdx.x];
-}
-
-// hist[c][digit] becomes the place of chunk c's first key with that digit.
-__global__ __launch_bounds__(256) void embed_scan_kernel(uint32_t* hist, int64_t chunks) {
-  __shared__ uint32_t total[256];
-  uint32_t n = 0;
-  for (int64_t c = 0; c < chunks; ++c) {
-    const uint32_t h = hist[c * 256 + threadIdx.x];
-    hist[c * 256 + threadIdx.x] = n;
-    n += h;
-  }
-  total[threadIdx.x] = n;
+  if (lane == 63 && wave * 64 < bins) tmp[wave] = s;
   __syncthreads();
   uint32_t before = 0;
-  for (int k = 0; k < (int)threadIdx.x; ++k) before += total[k];
-  for (int64_t c = 0; c < chunks; ++c) hist[c * 256 + threadIdx.x] += before;
+  for (int w = 0; w < wave && w * 64 < bins; ++w) before += tmp[w];
+  return before + s - v;
 }
 
-// One wave per chunk, 64 keys at a time in order: a key's place among the equal
-// digits of its 64 is the number of lower lanes that hold the same digit.
-__global__ __launch_bounds__(64) void embed_scatter_kernel(const uint32_t* key, const uint32_t* pos, int64_t T, int shift,
-                                                           const uint32_t* hist, uint32_t* key_out, uint32_t* pos_out) {
-  __shared__ uint32_t base[256];
-  const int lane = threadIdx.x;
-  for (int k = lane; k < 256; k += 64) base[k] = hist[(int64_t)blockIdx.x * 256 + k];
-  __syncthreads();
-  for (int64_t i = 0; i < kChunk; i += 64) {
-    const int64_t t = (int64_t)blockIdx.x * kChunk + i + lane;
-    const bool ok = t < T;
-    const uint32_t k = ok ? key[t] : 0u, digit = (k >> shift) & 255u;
-    uint64_t same = __ballot(ok);
+// count[w][digit] becomes the number of equal digits in the waves before w; the return
+// value is the workgroup's number of tokens with digit threadIdx.x (< bins).
+__device__ __forceinline__ uint32_t wave_prefixes(uint32_t* count, int bins) {
+  uint32_t n = 0;
+  if ((int)threadIdx.x < bins) {
 #pragma unroll
-    for (int bit = 0; bit < 8; ++bit) {
-      const uint64_t m = __ballot((digit >> bit) & 1u);
-      same &= (digit >> bit) & 1u ? m : ~m;
+    for (int w = 0; w < 16; ++w) {
+      const uint32_t c = count[w * kDigits + threadIdx.x];
+      count[w * kDigits + threadIdx.x] = n;
+      n += c;
     }
-    const uint32_t rank = __popcll(same & ((1ull << lane) - 1));
-    const uint32_t at = base[digit] + rank;
+  }
+  return n;
+}
+
+// Up to 1024 E tokens by one workgroup, all passes in shared memory.  Entries are
+// key << tbits | token.
+template <int E>
+__global__ __launch_bounds__(1024) void embed_sort_kernel(const EmbedArgs a, int passes, int bits, int tbits, uint32_t* key_out, uint32_t* pos_out) {
+  __shared__ uint32_t count[16 * kDigits], base[kDigits], tmp[8], entries[1024 * E];
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int T = (int)a.T, bins = 1 << bits;
+  uint32_t e[E], digit[E], rank[E];
+  bool ok[E];
+#pragma unroll
+  for (int r = 0; r < E; ++r) {
+    const int t = (int)((wave * E + r) * 64 + lane);
+    ok[r] = t < T;
+    e[r] = ok[r] ? key_at(a, t) << tbits | (uint32_t)t : 0u;
+  }
+  for (int p = 0; p < passes; ++p) {
+    for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) count[i] = 0;
     __syncthreads();
-    if (ok && rank == 0) base[digit] += __popcll(same);
+#pragma unroll
+    for (int r = 0; r < E; ++r) digit[r] = (e[r] >> (tbits + p * bits)) & (uint32_t)(bins - 1);
+    wave_ranks<E>(digit, ok, bits, count + wave * kDigits, rank);
     __syncthreads();
-    if (ok) {
-      key_out[at] = k;
-      pos_out[at] = pos[t];
+    const uint32_t n = wave_prefixes(count, bins);
+    const uint32_t first = bin_scan(n, bins, tmp);
+    if ((int)threadIdx.x < bins) base[threadIdx.x] = first;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < E; ++r)
+      if (ok[r]) entries[base[digit[r]] + count[wave * kDigits + digit[r]] + rank[r]] = e[r];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < E; ++r) e[r] = entries[(wave * E + r) * 64 + lane];   // (entries past T: not used)
+  }
+#pragma unroll
+  for (int r = 0; r < E; ++r) {
+    const int i = (int)((wave * E + r) * 64 + lane);
+    if (i < T) {
+      key_out[i] = e[r] >> tbits;
+      pos_out[i] = e[r] & ((1u << tbits) - 1);
     }
   }
 }
 
-__device__ __forceinline__ int64_t lower_bound(const uint32_t* key, int64_t T, uint32_t v) {
+// The keys and tokens a pass starts from: the ids in their order, or what the pass
+// before left.
+struct SortInput {
+  const uint32_t *key, *pos;   // NULL: the ids
+};
+__device__ __forceinline__ uint32_t input_key(const EmbedArgs& a, const SortInput& in, int64_t t) { return in.key ? in.key[t] : key_at(a, t); }
+
+// hist[workgroup][digit]
+template <int E>
+__global__ __launch_bounds__(1024) void embed_hist_kernel(const EmbedArgs a, SortInput in, int shift, int bits, uint32_t* hist) {
+  __shared__ uint32_t count[kDigits];
+  const int bins = 1 << bits;
+  if ((int)threadIdx.x < bins) count[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < E; ++r) {
+    const int64_t t = (int64_t)blockIdx.x * (1024 * E) + r * 1024 + threadIdx.x;
+    if (t < a.T) atomicAdd(&count[(input_key(a, in, t) >> shift) & (uint32_t)(bins - 1)], 1u);
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < bins) hist[(int64_t)blockIdx.x * bins + threadIdx.x] = count[threadIdx.x];
+}
+
+template <int E>
+__global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, SortInput in, int shift, int bits, const uint32_t* hist,
+                                                             uint32_t* key_out, uint32_t* pos_out) {
+  __shared__ uint32_t count[16 * kDigits], base[kDigits], tmp[8];
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int bins = 1 << bits;
+  for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) count[i] = 0;
+  uint32_t k[E], pos[E], digit[E], rank[E];
+  bool ok[E];
+#pragma unroll
+  for (int r = 0; r < E; ++r) {
+    const int64_t t = (int64_t)blockIdx.x * (1024 * E) + (wave * E + r) * 64 + lane;
+    ok[r] = t < a.T;
+    k[r] = ok[r] ? input_key(a, in, t) : 0u;
+    pos[r] = ok[r] && in.pos ? in.pos[t] : (uint32_t)t;
+    digit[r] = (k[r] >> shift) & (uint32_t)(bins - 1);
+  }
+  // the digit's tokens in all workgroups and in those before this one
+  uint32_t all = 0, before = 0;
+  if ((int)threadIdx.x < bins) {
+#pragma unroll 8
+    for (uint32_t g = 0; g < gridDim.x; ++g) {
+      const uint32_t n = hist[(int64_t)g * bins + threadIdx.x];
+      all += n;
+      before += g < blockIdx.x ? n : 0u;
+    }
+  }
+  const uint32_t first = bin_scan(all, bins, tmp);   // (its barrier: the counters are cleared)
+  if ((int)threadIdx.x < bins) base[threadIdx.x] = first + before;
+  wave_ranks<E>(digit, ok, bits, count + wave * kDigits, rank);
+  __syncthreads();
+  wave_prefixes(count, bins);
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < E; ++r)
+    if (ok[r]) {
+      const uint32_t at = base[digit[r]] + count[wave * kDigits + digit[r]] + rank[r];
+      key_out[at] = k[r];
+      pos_out[at] = pos[r];
+    }
+}
+
+// ---- the sums -------------------------------------------------------------------------
+// Overwriting, the sorted tokens and the table's rows form one sequence: token p lies at
+// p + kRowWeight key[p], row v, whose end writes it, after its tokens.  It is cut into
+// `chunks` of equal length, so that many tokens of one row, many rows of one token and
+// long stretches of rows without tokens load the waves alike (a row's 4 bytes per
+// feature written weigh as two tokens' 2 bytes read).  Where a cut falls into a row
+// of up to 32 tokens, it is moved behind them.  Rows cut all the same
+// are joined by embed_join_kernel: each chunk's sum over the row it leaves open goes to
+// `carry`, and the chunk that ends the row writes its own part.
+// Adding, only the tokens form the sequence.
+constexpr int kRowWeight = 2;
+
+struct SumArgs {
+  const uint32_t *key, *pos;   // sorted
+  int64_t chunk;               // length of a chunk
+  int chunks, slices;          // slices of 512 features
+  float* carry;                // [chunks][d]
+  uint32_t* carry_row;         // [chunks]; ~0: none
+};
+
+// First p in [0, T) with p + weight key[p] >= at, else T.
+__device__ __forceinline__ int64_t first_at(const uint32_t* key, int64_t T, int weight, int64_t at) {
+  const int lane = threadIdx.x & 63;
   int64_t lo = 0, hi = T;
   while (lo < hi) {
-    const int64_t m = (lo + hi) / 2;
-    if (key[m] < v) lo = m + 1; else hi = m;
+    const int64_t step = (hi - lo + 63) / 64;
+    const int64_t p = min(lo + (lane + 1) * step, hi) - 1;   // the last of the lane's share
+    const uint64_t m = __ballot(p + (int64_t)weight * key[p] >= at);
+    if (m == 0) return hi;
+    const int k = __ffsll((unsigned long long)m) - 1;
+    lo += k * step;
+    hi = min(lo + step, hi) - 1;
   }
   return lo;
 }
 
-template <class R>
-__global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const uint32_t* key, const uint32_t* pos) {
-  for (int64_t v = blockIdx.x; v < a.V; v += gridDim.x) {
-    const int64_t p0 = lower_bound(key, a.T, (uint32_t)v), p1 = lower_bound(key, a.T, (uint32_t)v + 1);
-    if (a.add && p0 == p1) continue;
-    for (int64_t c = threadIdx.x * 8; c < a.d; c += 2048) {
-      float s[8] = {}, x[8];
-      for (int64_t p = p0; p < p1; ++p) {
-        load8((const R*)a.dx + (int64_t)pos[p] * a.d + c, x);
-        for (int i = 0; i < 8; ++i) s[i] += x[i];
+struct Cut {
+  int64_t p;    // first token
+  uint32_t v;   // first row whose end lies behind the cut
+};
+__device__ __forceinline__ Cut cut_at(const EmbedArgs& a, const uint32_t* key, int64_t at) {
+  const int lane = threadIdx.x & 63;
+  const int weight = a.add ? 0 : kRowWeight;
+  const uint32_t V = (uint32_t)a.V;
+  Cut c;
+  c.p = a.add ? min(at, a.T) : first_at(key, a.T, weight, at);
+  // the keys of the 32 tokens before and the 32 from the cut on (outside: none of a token's)
+  const int64_t q = c.p - 32 + lane;
+  const uint32_t none = V + 1, k = q >= 0 && q < a.T ? key[q] : none;
+  const uint32_t left = __builtin_amdgcn_readlane(k, 31), right = __builtin_amdgcn_readlane(k, 32);
+  if (left == right && right < V) {
+    // in the middle of a row.  Of one of 32 tokens or fewer both ends are seen from every
+    // cut, so that all its cuts are moved; of a longer one none is.
+    const uint64_t other = __ballot(k != right);
+    const uint32_t below = (uint32_t)other, above = (uint32_t)(other >> 32);
+    c.v = right;
+    if (below != 0 && above != 0) {
+      const int rest = __ffs(above) - 1;
+      if (__clz(below) + rest <= 32) {
+        c.p += rest;
+        c.v = right + 1;
       }
-      float* out = a.dtable + v * a.d + c;
-      if (a.add) load8(out, x);
-      for (int i = 0; i < 8; ++i) s[i] = a.scale * s[i] + (a.add ? x[i] : 0.f);
-      store8(out, s);
     }
+    return c;
+  }
+  // between rows: behind the row on the left, and as far into the rows without tokens as the cut lies
+  const uint32_t lo = left < V ? left + 1 : left == none ? 0u : V, hi = right < V ? right : V;
+  const int64_t in = weight ? (at - c.p + weight - 1) / weight : 0;
+  c.v = (uint32_t)max((int64_t)lo, min((int64_t)hi, in));
+  return c;
+}
+
+template <class R, bool ADD>
+__global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const SumArgs s) {
+  constexpr int U = ADD ? 4 : 8;   // tokens on their way at once
+  const int lane = threadIdx.x & 63;
+  const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t chunk = task / s.slices;
+  if (chunk >= s.chunks) return;   // (no barriers below)
+  const int slice = (int)(task - chunk * s.slices);
+  const uint32_t c = (uint32_t)slice * 512 + lane * 8;
+  const bool there = c < (uint32_t)a.d;
+  const Cut c0 = cut_at(a, s.key, chunk * s.chunk), c1 = cut_at(a, s.key, (chunk + 1) * s.chunk);
+  const uint32_t V = (uint32_t)a.V;
+  float acc[8] = {};
+  uint32_t row = c0.v;   // the row being added up
+  bool open = false;     // whether it has tokens here
+  auto store = [&](uint32_t v, const Piece<float>& old) __attribute__((always_inline)) {
+    float o[8];
+    if (ADD) old.get(o);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = ADD ? fmaf(a.scale, acc[i], o[i]) : a.scale * acc[i], acc[i] = 0.f;
+    if (there) store8(a.dtable + (int64_t)v * a.d + c, o);
+  };
+  const Piece<float> nothing = {};
+  int64_t p = c0.p;
+  for (; p < c1.p; p += 64) {
+    const int n = (int)min((int64_t)64, c1.p - p);
+    const uint32_t k = lane < n ? s.key[p + lane] : V, pos = lane < n ? s.pos[p + lane] : 0u;
+    const uint32_t after = ADD && lane < n && p + lane + 1 < a.T ? s.key[p + lane + 1] : V + 1;
+    for (int j = 0; j < n; j += U) {
+      Piece<R> x[U];
+      Piece<float> old[ADD ? U : 1];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t ku = __builtin_amdgcn_readlane(k, j + u);   // (past n: V)
+        const int64_t t = __builtin_amdgcn_readlane(pos, j + u);
+        if (ku >= V) continue;
+        x[u].load(((const R*)a.dx + t * a.d) + c, there);
+        if (ADD && __builtin_amdgcn_readlane(after, j + u) != ku) old[ADD ? u : 0].load((a.dtable + (int64_t)ku * a.d) + c, there);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t ku = __builtin_amdgcn_readlane(k, j + u);
+        if (ku >= V) continue;
+        if (!ADD)
+          for (; row < ku; ++row, open = false) store(row, nothing);
+        float v[8];
+        x[u].get(v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] += v[i];
+        row = ku;
+        open = true;
+        if (ADD && __builtin_amdgcn_readlane(after, j + u) != ku) {
+          store(ku, old[ADD ? u : 0]);
+          open = false;
+        }
+      }
+    }
+  }
+  if (!ADD)
+    for (; row < c1.v; ++row, open = false) store(row, nothing);
+  if (open && there) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] *= a.scale;
+    store8(s.carry + chunk * a.d + c, acc);
+  }
+  if (slice == 0 && lane == 0) s.carry_row[chunk] = open ? row : ~0u;
+}
+
+// Adds the sums of the chunks that left a row open, in their order, to the row.  A
+// workgroup looks after the run of such chunks that begins at its own; its 4 quarters
+// take a share of a long run each.
+__global__ __launch_bounds__(1024) void embed_join_kernel(const EmbedArgs a, const SumArgs s) {
+  __shared__ float4 red[3][256];
+  const int c0 = blockIdx.x;
+  const uint32_t row = s.carry_row[c0];
+  if (row == ~0u || (c0 > 0 && s.carry_row[c0 - 1] == row)) return;
+  int n = 1;
+  while (c0 + n < s.chunks && s.carry_row[c0 + n] == row) ++n;
+  const int quarter = threadIdx.x >> 8, i = threadIdx.x & 255;
+  const int b = c0 + n * quarter / 4, e = c0 + n * (quarter + 1) / 4;
+  for (int64_t at = 0; at < a.d; at += 1024) {
+    const int64_t c = at + i * 4;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < a.d) {
+#pragma unroll 8
+      for (int k = b; k < e; ++k) {
+        const float4 y = *(const float4*)(s.carry + (int64_t)k * a.d + c);
+        x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+      }
+    }
+    __syncthreads();
+    if (quarter > 0) red[quarter - 1][i] = x;
+    __syncthreads();
+    if (quarter > 0 || c >= a.d) continue;
+    float4* out = (float4*)(a.dtable + (int64_t)row * a.d + c);
+    const float4 o = *out;
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      const float4 y = red[q][i];
+      x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+    }
+    *out = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
   }
 }
 
-struct BwdPlan {
+// ---- host -----------------------------------------------------------------------------
+
+int bit_length(int64_t v) {
+  int n = 0;
+  for (; v > 0; v >>= 1) ++n;
+  return n;
+}
+
+// Sort and cuts of one call, and its regions of the workspace.
+struct Plan {
+  int passes, bits, tbits;
+  bool one_group;      // sorted by one workgroup
+  int per_thread;      // tokens of a thread in a pass
+  int groups;
+  SumArgs sum;
   uint32_t *key[2], *pos[2], *hist;
   size_t bytes;
 };
-BwdPlan plan(void* ws, int64_t T) {
-  const size_t n = (size_t)cdiv(T, 64) * 64;
-  uint32_t* p = (uint32_t*)ws;
-  BwdPlan b;
-  for (int i = 0; i < 2; ++i) {
-    b.key[i] = p + (2 * i) * n;
-    b.pos[i] = p + (2 * i + 1) * n;
+Plan plan(void* ws, int64_t T, int64_t V, int64_t d, bool add) {
+  Plan p{};
+  const int key_bits = bit_length(V);   // keys 0 .. V
+  p.passes = (key_bits + 8) / 9;
+  p.bits = (key_bits + p.passes - 1) / p.passes;
+  p.tbits = std::max(1, bit_length(T - 1));
+  p.one_group = T <= 16384 && key_bits + p.tbits <= 32;
+  p.per_thread = p.one_group ? (T <= 1024 ? 1 : T <= 4096 ? 4 : 16) : (T <= (1 << 18) ? 4 : 16);
+  p.groups = (int)cdiv(T, 1024 * p.per_thread);
+  p.sum.slices = (int)cdiv(d, 512);
+  // about 8 waves to a SIMD, and not under a few tokens or rows to a chunk
+  const int64_t length = add ? T : T + kRowWeight * V;
+  p.sum.chunk = std::max<int64_t>(add ? 4 : 16, cdiv(length * p.sum.slices, 8192));
+  p.sum.chunks = (int)cdiv(length, p.sum.chunk);
+  size_t used = 0;
+  auto take = [&](size_t n) {
+    uint32_t* r = ws ? (uint32_t*)((char*)ws + used) : nullptr;
+    used += (n * sizeof(uint32_t) + 255) / 256 * 256;
+    return r;
+  };
+  for (int i = 0; i < (p.one_group || p.passes == 1 ? 1 : 2); ++i) {
+    p.key[i] = take((size_t)T);
+    p.pos[i] = take((size_t)T);
   }
-  b.hist = p + 4 * n;
-  b.bytes = (4 * n + (size_t)cdiv(T, kChunk) * 256) * sizeof(uint32_t);
-  return b;
+  if (!p.one_group) p.hist = take((size_t)p.groups << p.bits);
+  p.sum.carry_row = take((size_t)p.sum.chunks);
+  p.sum.carry = (float*)take((size_t)(p.sum.chunks * d));
+  p.bytes = used;
+  return p;
+}
+
+template <int E>
+hipError_t sort_passes(const EmbedArgs& a, const Plan& p, int& at, hipStream_t stream) {
+  for (int k = 0; k < p.passes; ++k) {
+    const int to = p.passes == 1 ? 0 : k & 1;
+    const SortInput in = k == 0 ? SortInput{nullptr, nullptr} : SortInput{p.key[1 - to], p.pos[1 - to]};
+    {
+      TimedLaunch tl("embed_bwd_sort", stream);
+      hipLaunchKernelGGL(embed_hist_kernel<E>, dim3((unsigned)p.groups), dim3(1024), 0, stream, a, in, k * p.bits, p.bits, p.hist);
+    }
+    TimedLaunch tl("embed_bwd_sort", stream);
+    hipLaunchKernelGGL(embed_scatter_kernel<E>, dim3((unsigned)p.groups), dim3(1024), 0, stream, a, in, k * p.bits, p.bits,
+                       (const uint32_t*)p.hist, p.key[to], p.pos[to]);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    at = to;
+  }
+  return hipSuccess;
+}
+
+template <int E>
+void sort_one_group(const EmbedArgs& a, const Plan& p, hipStream_t stream) {
+  TimedLaunch tl("embed_bwd_sort", stream);
+  hipLaunchKernelGGL(embed_sort_kernel<E>, dim3(1), dim3(1024), 0, stream, a, p.passes, p.bits, p.tbits, p.key[0], p.pos[0]);
+}
+
+template <class R>
+void launch_sum(const EmbedArgs& a, const SumArgs& s, hipStream_t stream) {
+  const dim3 grid((unsigned)cdiv((int64_t)s.chunks * s.slices, 4));
+  if (a.add)
+    hipLaunchKernelGGL((embed_sum_kernel<R, true>), grid, dim3(256), 0, stream, a, s);
+  else
+    hipLaunchKernelGGL((embed_sum_kernel<R, false>), grid, dim3(256), 0, stream, a, s);
 }
 
 }  // namespace
 
-size_t embed_bwd_workspace_bytes(int64_t T, int64_t V, int64_t d, bool add) { return plan(nullptr, T).bytes; }
+size_t embed_bwd_workspace_bytes(int64_t T, int64_t V, int64_t d, bool add) { return plan(nullptr, T, V, d, add).bytes; }
 
 hipError_t run_embed_fwd(const EmbedArgs& a, hipStream_t stream) {
   TimedLaunch tl("embed_fwd", stream);
-  const unsigned grid = (unsigned)std::min<int64_t>(cdiv(a.T * (a.d / 8), 256), 1 << 20);
+  const uint32_t parts = (uint32_t)cdiv(a.d, 512);
+  const unsigned grid = (unsigned)std::min<int64_t>(cdiv(a.T * parts, 16), 1 << 20);
   if (a.res_f32)
-    hipLaunchKernelGGL(embed_fwd_kernel<float>, dim3(grid), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(embed_fwd_kernel<float>, dim3(grid), dim3(256), 0, stream, a, parts);
   else
-    hipLaunchKernelGGL(embed_fwd_kernel<uint16_t>, dim3(grid), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(embed_fwd_kernel<uint16_t>, dim3(grid), dim3(256), 0, stream, a, parts);
   return hipGetLastError();
 }
 
 hipError_t run_embed_bwd(const EmbedArgs& a, hipStream_t stream) {
-  const BwdPlan b = plan(a.ws, a.T);
-  const unsigned chunks = (unsigned)cdiv(a.T, kChunk);
+  Plan p = plan(a.ws, a.T, a.V, a.d, a.add);
   int at = 0;
   if (a.T > 0) {
-    TimedLaunch tl("embed_bwd_sort", stream);
-    hipLaunchKernelGGL(embed_keys_kernel, dim3((unsigned)cdiv(a.T, 256)), dim3(256), 0, stream, a, b.key[0], b.pos[0]);
-    for (int shift = 0; shift < 32 && (a.V >> shift) > 0; shift += 8) {
-      hipLaunchKernelGGL(embed_hist_kernel, dim3(chunks), dim3(256), 0, stream, b.key[at], a.T, shift, b.hist);
-      hipLaunchKernelGGL(embed_scan_kernel, dim3(1), dim3(256), 0, stream, b.hist, (int64_t)chunks);
-      hipLaunchKernelGGL(embed_scatter_kernel, dim3(chunks), dim3(64), 0, stream, b.key[at], b.pos[at], a.T, shift, b.hist,
-                         b.key[1 - at], b.pos[1 - at]);
-      at = 1 - at;
-    }
+    hipError_t e = hipSuccess;
+    if (!p.one_group)
+      e = p.per_thread == 4 ? sort_passes<4>(a, p, at, stream) : sort_passes<16>(a, p, at, stream);
+    else if (p.per_thread == 1)
+      sort_one_group<1>(a, p, stream);
+    else if (p.per_thread == 4)
+      sort_one_group<4>(a, p, stream);
+    else
+      sort_one_group<16>(a, p, stream);
+    if (e == hipSuccess) e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  p.sum.key = p.key[at];
+  p.sum.pos = p.pos[at];
+  {
+    TimedLaunch tl("embed_bwd_sum", stream);
+    if (a.res_f32)
+      launch_sum<float>(a, p.sum, stream);
+    else
+      launch_sum<uint16_t>(a, p.sum, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  TimedLaunch tl("embed_bwd_sum", stream);
-  const unsigned grid = (unsigned)std::min<int64_t>(a.V, 1 << 20);
-  if (a.res_f32)
-    hipLaunchKernelGGL(embed_sum_kernel<float>, dim3(grid), dim3(256), 0, stream, a, b.key[at], b.pos[at]);
-  else
-    hipLaunchKernelGGL(embed_sum_kernel<uint16_t>, dim3(grid), dim3(256), 0, stream, a, b.key[at], b.pos[at]);
+  TimedLaunch tl("embed_bwd_join", stream);
+  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)p.sum.chunks), dim3(1024), 0, stream, a, p.sum);
   return hipGetLastError();
 }
 

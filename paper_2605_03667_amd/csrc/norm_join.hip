@@ -9,192 +9,583 @@ namespace elas {
 
 namespace {
 
-// One workgroup per row; the row is read again where a sum over it is needed first.
-template <class R>
-__global__ __launch_bounds__(256) void join_fwd_kernel(const NormJoinArgs a) {
-  __shared__ float red[4];
-  const int64_t d = a.d;
-  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-  const R* h = (const R*)a.h + t * d;
-  const uint16_t* b = a.b ? a.b + t * d : nullptr;
-  const uint16_t* gate = a.gate ? a.gate + (a.gate_token ? t * d : 0) : nullptr;
-  float rho = 1.f;
-  if (a.w_post) {
-    float s = 0.f;
-    for (int64_t c = threadIdx.x * 8; c < d; c += 2048) {
-      float v[8];
-      load8(b + c, v);
-      for (int i = 0; i < 8; ++i) s += v[i] * v[i];
-    }
-    rho = 1.f / sqrtf(block_sum<4>(s, red) / d + a.eps);
-  }
-  auto joined = [&](int64_t c, float (&v)[8]) {
-    load8(h + c, v);
-    if (!b) return;
-    float u[8], w[8];
-    load8(b + c, u);
-    if (a.w_post) {
-      load8(a.w_post + c, w);
-      for (int i = 0; i < 8; ++i) u[i] = u[i] * rho * w[i];
-    }
-    if (gate) {
-      load8(gate + c, w);
-      for (int i = 0; i < 8; ++i) u[i] *= w[i];
-    }
-    for (int i = 0; i < 8; ++i) v[i] = a.res_scale * v[i] + a.block_scale * u[i];
-  };
-  float s = 0.f;
-  if (a.w_pre)
-    for (int64_t c = threadIdx.x * 8; c < d; c += 2048) {
-      float v[8];
-      joined(c, v);
-      for (int i = 0; i < 8; ++i) s += v[i] * v[i];
-    }
-  const float sig = 1.f / sqrtf(block_sum<4>(s, red) / d + a.eps);
-  for (int64_t c = threadIdx.x * 8; c < d; c += 2048) {
-    float v[8], w[8];
-    joined(c, v);
-    if (a.w_pre) load8(a.w_pre + c, w);
-    if (b) store8((R*)a.h_out + t * d + c, v);
-    if (a.w_pre) {
-      for (int i = 0; i < 8; ++i) v[i] = v[i] * sig * w[i];
-      store8(a.n + t * d + c, v);
+// ---- rows of up to 2048 W NV features, W = 1, 2 or 4 waves to a row ----------------
+// The row stays in registers, lane l of the row's W waves holding the pieces of 8
+// features l, l + 64 W, ..  (NV of them).
+
+// Where a thread's row and pieces lie.
+template <int W, int NV>
+struct RowLanes {
+  static constexpr int WAVES = W < 4 ? 4 : W;   // of a workgroup
+  static constexpr int ROWS = WAVES / W;        // rows it works on at a time
+  int slot;
+  uint32_t c[NV];   // (unsigned: an offset beside a uniform address)
+  bool there[NV];
+  __device__ __forceinline__ explicit RowLanes(int d) {
+    slot = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W));   // (the same in all of a wave)
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      c[v] = ((v * W * 64) + threadIdx.x % (64 * W)) * 8;
+      there[v] = c[v] < (uint32_t)d;
     }
   }
+};
+
+// Sums of N values over a row's W waves.  `red` is free again after the next call
+// with another `red`.
+template <int W, int WAVES, int N>
+__device__ __forceinline__ void row_sums(float (&s)[N], float (&red)[WAVES][N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
+  if constexpr (W > 1) {
+    const int wave = threadIdx.x >> 6, w0 = wave / W * W;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) red[wave][i] = s[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      s[i] = red[w0][i];
+#pragma unroll
+      for (int w = 1; w < W; ++w) s[i] += red[w0 + w][i];
+    }
   }
 }
 
-// Workgroup g takes the rows g, g + grid, ..; its sums over them of the gains' and
-// the shared gate's gradients go to row g of `part`, [grid][3][d].
-template <class R>
-__global__ __launch_bounds__(256) void join_bwd_kernel(const NormJoinArgs a, float* part) {
-  __shared__ float red[4];
-  const int64_t d = a.d;
-  float* sums = part + (int64_t)blockIdx.x * 3 * d;
-  for (int64_t c = threadIdx.x; c < 3 * d; c += 256) sums[c] = 0.f;
-  __syncthreads();
-  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-    const R* h = (const R*)a.h + t * d;
-    const uint16_t* b = a.b ? a.b + t * d : nullptr;
-    const uint16_t* gate = a.gate ? a.gate + (a.gate_token ? t * d : 0) : nullptr;
-    float hh = 0.f, qh = 0.f, bb = 0.f;
-    for (int64_t c = threadIdx.x * 8; c < d; c += 2048) {
-      float v[8], q[8], w[8];
-      if (a.w_pre) {
-        load8(h + c, v);
-        load8(a.dn + t * d + c, q);
-        load8(a.w_pre + c, w);
-        for (int i = 0; i < 8; ++i) hh += v[i] * v[i], qh += q[i] * w[i] * v[i];
-      }
+template <class R, int W, int NV>
+__global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_fwd_kernel(const NormJoinArgs a) {
+  using Lanes = RowLanes<W, NV>;
+  __shared__ float red[2][Lanes::WAVES][1];
+  const Lanes l((int)a.d);
+  const float inv_d = 1.f / (float)a.d;
+  for (int64_t t0 = (int64_t)blockIdx.x * Lanes::ROWS; t0 < a.T; t0 += (int64_t)gridDim.x * Lanes::ROWS) {
+    const int64_t t = t0 + l.slot, at = t * a.d;
+    if (W == 1 && t >= a.T) break;
+    const bool live = t < a.T;
+    Piece<R> h[NV];
+    Piece<uint16_t> b[NV], gate[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const bool ok = live && l.there[v];
+      h[v].load(((const R*)a.h + at) + l.c[v], ok);
+      if (a.b) b[v].load((a.b + at) + l.c[v], ok);
+      if (a.gate) gate[v].load(a.gate + (a.gate_token ? at : 0) + l.c[v], ok);
+    }
+    float x[NV][8];
+    if (a.b) {
+      float rho = 1.f;
       if (a.w_post) {
-        load8(b + c, v);
-        for (int i = 0; i < 8; ++i) bb += v[i] * v[i];
+        float s[1] = {0.f};
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          float u[8];
+          b[v].get(u);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[0] = fmaf(u[i], u[i], s[0]);
+        }
+        row_sums<W>(s, red[0]);
+        rho = 1.f / sqrtf(s[0] * inv_d + a.eps);
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        float u[8], k[8];
+        b[v].get(u);
+        if (a.w_post) {
+          Piece<uint16_t> w;
+          w.load(a.w_post + l.c[v], l.there[v]);
+          w.get(k);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) u[i] = u[i] * rho * k[i];
+        }
+        if (a.gate) {
+          gate[v].get(k);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) u[i] *= k[i];
+        }
+        h[v].get(x[v]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[v][i] = fmaf(a.res_scale, x[v][i], a.block_scale * u[i]);
+        if (live && l.there[v]) store8(((R*)a.h_out + at) + l.c[v], x[v]);
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) h[v].get(x[v]);
+    }
+    if (a.w_pre) {
+      float s[1] = {0.f};
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[0] = fmaf(x[v][i], x[v][i], s[0]);
+      row_sums<W>(s, red[1]);
+      const float sig = 1.f / sqrtf(s[0] * inv_d + a.eps);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        float k[8];
+        Piece<uint16_t> w;
+        w.load(a.w_pre + l.c[v], l.there[v]);
+        w.get(k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k[i] *= x[v][i] * sig;
+        if (live && l.there[v]) store8((a.n + at) + l.c[v], k);
       }
     }
-    hh = block_sum<4>(hh, red);
-    qh = block_sum<4>(qh, red);
-    bb = block_sum<4>(bb, red);
-    const float sig = 1.f / sqrtf(hh / d + a.eps), rho = a.w_post ? 1.f / sqrtf(bb / d + a.eps) : 1.f;
-    const float ch = qh * sig * sig * sig / d;
-    auto grad = [&](int64_t c, float (&g)[8]) {   // G
-      for (int i = 0; i < 8; ++i) g[i] = 0.f;
-      if (a.dh_out) load8((const R*)a.dh_out + t * d + c, g);
+    // (a lone second or first sum would leave `red` in use)
+    if (W > 1 && !(a.w_pre && a.w_post)) __syncthreads();
+  }
+}
+
+// The sums over the tokens: acc[0] of dn xh, acc[1] of G bh (times the token's
+// gate where there is one for each), added up in the workgroup at the end and
+// written to row blockIdx.x of `part`, [grid][2][d].
+template <class R, int W, int NV>
+__global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_bwd_kernel(const NormJoinArgs a, float* part) {
+  using Lanes = RowLanes<W, NV>;
+  __shared__ float red3[Lanes::WAVES][3], red1[Lanes::WAVES][1];
+  const Lanes l((int)a.d);
+  const float inv_d = 1.f / (float)a.d;
+  float acc[2][NV][8] = {};
+  Piece<uint16_t> w_pre[NV], w_post[NV], shared[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    if (a.w_pre) w_pre[v].load(a.w_pre + l.c[v], l.there[v]);
+    if (a.w_post) w_post[v].load(a.w_post + l.c[v], l.there[v]);
+    if (a.gate && !a.gate_token) shared[v].load(a.gate + l.c[v], l.there[v]);
+  }
+  for (int64_t t0 = (int64_t)blockIdx.x * Lanes::ROWS; t0 < a.T; t0 += (int64_t)gridDim.x * Lanes::ROWS) {
+    const int64_t t = t0 + l.slot, at = t * a.d;
+    Piece<R> h[NV], dho[NV];
+    Piece<uint16_t> dn[NV], b[NV], gate[NV];
+    bool ok[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      ok[v] = t < a.T && l.there[v];
       if (a.w_pre) {
-        float v[8], q[8], w[8];
-        load8(h + c, v);
-        load8(a.dn + t * d + c, q);
-        load8(a.w_pre + c, w);
-        for (int i = 0; i < 8; ++i) g[i] += sig * (q[i] * w[i]) - v[i] * ch;
+        h[v].load(((const R*)a.h + at) + l.c[v], ok[v]);
+        dn[v].load((a.dn + at) + l.c[v], ok[v]);
       }
-    };
-    float pb = 0.f;
-    if (a.w_post)
-      for (int64_t c = threadIdx.x * 8; c < d; c += 2048) {
-        float g[8], v[8], w[8];
-        grad(c, g);
-        load8(a.w_post + c, w);
-        load8(b + c, v);
-        for (int i = 0; i < 8; ++i) pb += g[i] * a.block_scale * w[i] * v[i] * (gate ? __builtin_bit_cast(float, (uint32_t)gate[c + i] << 16) : 1.f);
-      }
-    pb = block_sum<4>(pb, red);
-    const float cb = pb * rho * rho * rho / d;
-    for (int64_t c = threadIdx.x * 8; c < d; c += 2048) {
-      float g[8], v[8], q[8], w[8], o[8];
-      grad(c, g);
+      if (a.b) b[v].load((a.b + at) + l.c[v], ok[v]);
+      if (a.dh_out) dho[v].load(((const R*)a.dh_out + at) + l.c[v], ok[v]);
+      if (a.gate_token) gate[v].load((a.gate + at) + l.c[v], ok[v]);
+    }
+    float s[3] = {0.f, 0.f, 0.f};   // |h'|^2, q h', |b|^2
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      w_pre[v].keep_packed(), w_post[v].keep_packed(), shared[v].keep_packed();
+      float x[8], q[8], k[8];
       if (a.w_pre) {
-        load8(h + c, v);
-        load8(a.dn + t * d + c, q);
-        for (int i = 0; i < 8; ++i) sums[2 * d + c + i] += q[i] * v[i] * sig;
-      }
-      if (b) load8(b + c, v);
-      if (a.dh) {
-        for (int i = 0; i < 8; ++i) o[i] = (b ? a.res_scale : 1.f) * g[i];
-        store8((R*)a.dh + t * d + c, o);
-      }
-      if (!b) continue;
-      for (int i = 0; i < 8; ++i) g[i] *= a.block_scale;
-      if (a.w_post) load8(a.w_post + c, w);
-      if (gate) {
-        float k[8];
-        load8(gate + c, k);
-        for (int i = 0; i < 8; ++i) o[i] = g[i] * (a.w_post ? v[i] * rho * w[i] : v[i]);
-        if (a.gate_token)
-          store8((uint16_t*)a.dgate + t * d + c, o);
-        else
-          for (int i = 0; i < 8; ++i) sums[c + i] += o[i];
-        for (int i = 0; i < 8; ++i) g[i] *= k[i];
-      }
-      if (a.w_post) {
+        h[v].get(x), dn[v].get(q), w_pre[v].get(k);
+#pragma unroll
         for (int i = 0; i < 8; ++i) {
-          sums[d + c + i] += g[i] * v[i] * rho;
-          g[i] = rho * (g[i] * w[i]) - v[i] * cb;
+          s[0] = fmaf(x[i], x[i], s[0]);
+          s[1] = fmaf(q[i] * k[i], x[i], s[1]);
         }
       }
-      store8(a.db + t * d + c, g);
+      if (a.w_post) {
+        b[v].get(x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[2] = fmaf(x[i], x[i], s[2]);
+      }
+    }
+    if (a.w_pre || a.w_post) row_sums<W>(s, red3);
+    const float sig = 1.f / sqrtf(s[0] * inv_d + a.eps), rho = a.w_post ? 1.f / sqrtf(s[2] * inv_d + a.eps) : 1.f;
+    const float ch = s[1] * sig * inv_d;   // mean of q xh
+    float g[NV][8], pb[1] = {0.f};
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      h[v].keep_packed(), dn[v].keep_packed(), b[v].keep_packed();
+      w_pre[v].keep_packed();
+      float x[8], q[8], k[8];
+      if (a.dh_out)
+        dho[v].get(g[v]);
+      else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[v][i] = 0.f;
+      if (a.w_pre) {
+        h[v].get(x), dn[v].get(q), w_pre[v].get(k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float xh = x[i] * sig;
+          acc[0][v][i] = fmaf(q[i], xh, acc[0][v][i]);
+          g[v][i] = fmaf(sig, fmaf(-ch, xh, q[i] * k[i]), g[v][i]);
+        }
+      }
+      if (a.dh && ok[v]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = a.res_scale * g[v][i];
+        store8(((R*)a.dh + at) + l.c[v], q);
+      }
+      if (!a.b) continue;
+      b[v].get(x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= rho;
+      if (a.w_post) w_post[v].get(k);
+      if (a.gate_token) {
+        if (ok[v]) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) q[i] = a.block_scale * g[v][i] * (a.w_post ? x[i] * k[i] : x[i]);
+          store8(((uint16_t*)a.dgate + at) + l.c[v], q);
+        }
+        gate[v].get(q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[v][i] *= q[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[1][v][i] = fmaf(g[v][i], x[i], acc[1][v][i]);
+      if (a.gate && !a.gate_token) {
+        shared[v].get(q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[v][i] *= q[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[v][i] *= a.block_scale;
+      if (a.w_post) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          g[v][i] *= k[i];
+          pb[0] = fmaf(g[v][i], x[i], pb[0]);
+        }
+      }
+    }
+    if (a.b) {
+      if (a.w_post) {
+        row_sums<W>(pb, red1);
+        const float cb = pb[0] * inv_d;   // mean of p bh
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          float x[8];
+          b[v].keep_packed();
+          b[v].get(x);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) g[v][i] = rho * fmaf(-cb, x[i] * rho, g[v][i]);
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        if (ok[v]) store8((a.db + at) + l.c[v], g[v]);
+    }
+    // (without a second sum red3 would still be in use)
+    if (W > 1 && !a.w_post) __syncthreads();
+  }
+  if (!part) return;
+  // rows of a workgroup are added in order, in shared memory
+  const bool need[2] = {a.dw_pre != nullptr, a.dw_post || (a.dgate && !a.gate_token)};
+  extern __shared__ __attribute__((aligned(16))) float sum[];   // [2][d]
+#pragma unroll
+  for (int r = 0; r < Lanes::ROWS; ++r) {
+    if (l.slot == r) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+          if (need[k] && l.there[v]) {
+            float* o = (r + 1 == Lanes::ROWS ? part + (int64_t)blockIdx.x * 2 * a.d : sum) + k * a.d + l.c[v];
+            if (r > 0) {
+              float x[8];
+              load8(sum + k * a.d + l.c[v], x);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) acc[k][v][i] = x[i] + acc[k][v][i];
+            }
+            store8(o, acc[k][v]);
+          }
+    }
+    if (r + 1 < Lanes::ROWS) __syncthreads();
+  }
+}
+
+// The gradients from the sums `part` [rows][2][d] (with A the second one):
+// dw_pre = sum dn xh, dgate = block_scale w_post A, dw_post = block_scale gate A.
+// A workgroup takes 32 columns: 8 threads of 4 columns times 32 shares of the rows.
+// Columns begin at c0 (d where the first sum is not needed).
+__global__ __launch_bounds__(256) void join_reduce_kernel(const NormJoinArgs a, const float* part, int rows, int64_t c0, int64_t c1) {
+  __shared__ float4 red[32][8];
+  const int64_t d = a.d, c = c0 + (int64_t)blockIdx.x * 32 + threadIdx.x % 8 * 4;
+  const int share = threadIdx.x / 8, r1 = (int)((int64_t)rows * (share + 1) / 32);
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (c < c1) {
+#pragma unroll 8
+    for (int r = (int)((int64_t)rows * share / 32); r < r1; ++r) {
+      const float4 x = *(const float4*)(part + r * 2 * d + c);
+      s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+    }
+  }
+  red[share][threadIdx.x % 8] = s;
+  __syncthreads();
+  const int64_t col = c0 + (int64_t)blockIdx.x * 32 + threadIdx.x;
+  if (threadIdx.x >= 32 || col >= c1) return;
+  float v = 0.f;
+#pragma unroll
+  for (int k = 0; k < 32; ++k) v += ((const float*)red[k])[threadIdx.x];
+  if (col < d) {
+    a.dw_pre[col] = v;
+    return;
+  }
+  auto factor = [&](const uint16_t* p) { return p ? as_float((uint32_t)p[col - d] << 16) : 1.f; };
+  v *= a.block_scale;
+  if (a.dgate && !a.gate_token) ((float*)a.dgate)[col - d] = v * factor(a.w_post);
+  if (a.dw_post) a.dw_post[col - d] = v * (a.gate_token ? 1.f : factor(a.gate));
+}
+
+// ---- wider rows -------------------------------------------------------------------
+// One workgroup per row; the row is read again where a sum over it is needed first.
+
+// 8 features of the operands at column c of row t (absent: zeros, or ones for factors).
+template <class R>
+struct WideRow {
+  const NormJoinArgs& a;
+  int64_t at;
+  __device__ __forceinline__ void factor(const uint16_t* p, int64_t i, float (&v)[8]) const {
+    if (p) return load8(p + i, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = 1.f;
+  }
+  // the forward's u before the gate, or h' where there is no block
+  __device__ __forceinline__ void joined(int64_t c, float rho, float (&x)[8]) const {
+    load8((const R*)a.h + at + c, x);
+    if (!a.b) return;
+    float u[8], w[8], k[8];
+    load8(a.b + at + c, u);
+    factor(a.w_post, c, w);
+    factor(a.gate, (a.gate_token ? at : 0) + c, k);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = fmaf(a.res_scale, x[i], a.block_scale * (u[i] * rho * w[i] * k[i]));
+  }
+  // the backward's G, and xh and dn where there is a norm
+  __device__ __forceinline__ void grad(int64_t c, float sig, float ch, float (&g)[8], float (&xh)[8], float (&q)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = 0.f;
+    if (a.dh_out) load8((const R*)a.dh_out + at + c, g);
+    if (!a.w_pre) return;
+    float w[8];
+    load8((const R*)a.h + at + c, xh);
+    load8(a.dn + at + c, q);
+    load8(a.w_pre + c, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      xh[i] *= sig;
+      g[i] = fmaf(sig, fmaf(-ch, xh[i], q[i] * w[i]), g[i]);
+    }
+  }
+};
+
+template <class R>
+__global__ __launch_bounds__(256) void join_fwd_wide_kernel(const NormJoinArgs a) {
+  __shared__ float red[4];
+  const float inv_d = 1.f / (float)a.d;
+  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const WideRow<R> row{a, t * a.d};
+    float rho = 1.f, sig = 1.f, x[8];
+    if (a.w_post) {
+      float s = 0.f;
+      for (int64_t c = threadIdx.x * 8; c < a.d; c += 2048) {
+        load8(a.b + row.at + c, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
+      }
+      rho = 1.f / sqrtf(block_sum<4>(s, red) * inv_d + a.eps);
+    }
+    if (a.w_pre) {
+      float s = 0.f;
+      for (int64_t c = threadIdx.x * 8; c < a.d; c += 2048) {
+        row.joined(c, rho, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
+      }
+      sig = 1.f / sqrtf(block_sum<4>(s, red) * inv_d + a.eps);
+    }
+    for (int64_t c = threadIdx.x * 8; c < a.d; c += 2048) {
+      row.joined(c, rho, x);   // (before the stores, which may go to the same place)
+      if (a.b) store8((R*)a.h_out + row.at + c, x);
+      if (!a.w_pre) continue;
+      float w[8];
+      load8(a.w_pre + c, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] *= x[i] * sig;
+      store8(a.n + row.at + c, w);
     }
   }
 }
 
-__global__ __launch_bounds__(256) void join_reduce_kernel(const float* part, int64_t rows, int64_t d, float* dgate, float* dw_post,
-                                                          float* dw_pre) {
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= 3 * d) return;
-  float s = 0.f;
-  for (int64_t r = 0; r < rows; ++r) s += part[r * 3 * d + c];
-  float* out = c < d ? dgate : c < 2 * d ? dw_post : dw_pre;
-  if (out) out[c % d] = s;
+// The sums over a workgroup's tokens are kept in its row of `part` (a thread's
+// columns are its own).
+template <class R>
+__global__ __launch_bounds__(256) void join_bwd_wide_kernel(const NormJoinArgs a, float* part) {
+  __shared__ float red[4];
+  const int64_t d = a.d;
+  const float inv_d = 1.f / (float)d;
+  float* sums = part ? part + (int64_t)blockIdx.x * 2 * d : nullptr;
+  bool first = true;
+  auto add_sums = [&](float* to, const float (&x)[8], const float (&y)[8]) {
+    float s[8] = {};
+    if (!first) load8(to, s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = fmaf(x[i], y[i], s[i]);
+    store8(to, s);
+  };
+  if (sums && blockIdx.x >= a.T)
+    for (int64_t c = threadIdx.x; c < 2 * d; c += 256) sums[c] = 0.f;
+  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x, first = false) {
+    const WideRow<R> row{a, t * d};
+    float hh = 0.f, qh = 0.f, bb = 0.f, x[8], q[8], w[8], g[8];
+    for (int64_t c = threadIdx.x * 8; c < d; c += 2048) {
+      if (a.w_pre) {
+        load8((const R*)a.h + row.at + c, x);
+        load8(a.dn + row.at + c, q);
+        load8(a.w_pre + c, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) hh = fmaf(x[i], x[i], hh), qh = fmaf(q[i] * w[i], x[i], qh);
+      }
+      if (a.w_post) {
+        load8(a.b + row.at + c, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bb = fmaf(x[i], x[i], bb);
+      }
+    }
+    const float sig = 1.f / sqrtf(block_sum<4>(hh, red) * inv_d + a.eps);
+    const float ch = block_sum<4>(qh, red) * sig * inv_d;
+    const float b2 = block_sum<4>(bb, red);
+    const float rho = a.w_post ? 1.f / sqrtf(b2 * inv_d + a.eps) : 1.f;
+    float cb = 0.f;
+    if (a.w_post) {
+      float pb = 0.f;
+      for (int64_t c = threadIdx.x * 8; c < d; c += 2048) {
+        float k[8];
+        row.grad(c, sig, ch, g, x, q);
+        load8(a.b + row.at + c, x);
+        load8(a.w_post + c, w);
+        row.factor(a.gate, (a.gate_token ? row.at : 0) + c, k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pb = fmaf(a.block_scale * g[i] * k[i] * w[i], x[i] * rho, pb);
+      }
+      cb = block_sum<4>(pb, red) * inv_d;
+    }
+    for (int64_t c = threadIdx.x * 8; c < d; c += 2048) {
+      float k[8], o[8];
+      row.grad(c, sig, ch, g, x, q);
+      if (a.w_pre) add_sums(sums + c, q, x);
+      if (a.b) load8(a.b + row.at + c, x);
+      if (a.dh) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = a.res_scale * g[i];
+        store8((R*)a.dh + row.at + c, o);
+      }
+      if (!a.b) continue;
+      row.factor(a.w_post, c, w);
+      row.factor(a.gate, (a.gate_token ? row.at : 0) + c, k);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= rho;   // bh
+      if (a.gate_token) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = a.block_scale * g[i] * x[i] * w[i], g[i] *= k[i];
+        store8((uint16_t*)a.dgate + row.at + c, o);
+      }
+      if (sums) add_sums(sums + d + c, g, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float p = a.block_scale * g[i] * (a.gate_token ? 1.f : k[i]) * w[i];
+        g[i] = a.w_post ? rho * fmaf(-cb, x[i], p) : p;
+      }
+      store8(a.db + row.at + c, g);
+    }
+  }
 }
 
-int64_t bwd_groups(int64_t T) { return std::max<int64_t>(1, std::min<int64_t>(T, 1024)); }
+// How rows of d features are worked on: `waves` to a row (0: the kernels for wider
+// rows), `pieces` of 8 features to a lane.
+struct RowShape {
+  int waves, pieces;
+};
+RowShape row_shape(int64_t d) {
+  if (d <= 512) return {1, 1};
+  if (d <= 1024) return {2, 1};
+  if (d <= 2048) return {4, 1};
+  if (d <= 4096) return {8, 1};
+  if (d <= 8192) return {8, 2};
+  return {0, 0};
+}
+int64_t row_groups(int64_t T, int64_t d) {   // workgroups, at one row (or set of rows) each
+  const int w = row_shape(d).waves, rows = w == 1 ? 4 : w == 2 ? 2 : 1;
+  return (T + rows - 1) / rows;
+}
+// Forward: a workgroup per row or set of rows (1B, 65536 tokens, float32 stream: 269 us,
+// with 2048 workgroups that go on to further rows 312).  Backward: each workgroup leaves
+// a row of partial sums, so as many as the card holds at once at most: 4 to a CU, or 2
+// where a float32 stream has twice the bytes in flight for each (1B, 65536 tokens, bf16:
+// 331 us with 512, 315 with 1024, 325 with 2048; 32768 tokens, float32: 267, 287, 294).
+int64_t fwd_grid(int64_t T, int64_t d) { return std::min<int64_t>(row_groups(T, d), 1 << 20); }
+int64_t bwd_grid(int64_t T, int64_t d, bool res_f32) {
+  return std::max<int64_t>(1, std::min<int64_t>(row_groups(T, d), res_f32 ? 512 : 1024));
+}
+
+template <class R>
+void launch_fwd(const NormJoinArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)fwd_grid(a.T, a.d));
+  const RowShape s = row_shape(a.d);
+  if (s.waves == 1)
+    hipLaunchKernelGGL((join_fwd_kernel<R, 1, 1>), grid, dim3(256), 0, stream, a);
+  else if (s.waves == 2)
+    hipLaunchKernelGGL((join_fwd_kernel<R, 2, 1>), grid, dim3(256), 0, stream, a);
+  else if (s.waves == 4)
+    hipLaunchKernelGGL((join_fwd_kernel<R, 4, 1>), grid, dim3(256), 0, stream, a);
+  else if (s.waves == 8 && s.pieces == 1)
+    hipLaunchKernelGGL((join_fwd_kernel<R, 8, 1>), grid, dim3(512), 0, stream, a);
+  else if (s.waves == 8)
+    hipLaunchKernelGGL((join_fwd_kernel<R, 8, 2>), grid, dim3(512), 0, stream, a);
+  else
+    hipLaunchKernelGGL((join_fwd_wide_kernel<R>), grid, dim3(256), 0, stream, a);
+}
+
+template <class R>
+void launch_bwd(const NormJoinArgs& a, float* part, hipStream_t stream) {
+  const dim3 grid((unsigned)bwd_grid(a.T, a.d, a.res_f32));
+  const RowShape s = row_shape(a.d);
+  const size_t lds = part ? (size_t)(2 * a.d) * sizeof(float) : 0;   // (where a workgroup takes several rows)
+  if (s.waves == 1)
+    hipLaunchKernelGGL((join_bwd_kernel<R, 1, 1>), grid, dim3(256), lds, stream, a, part);
+  else if (s.waves == 2)
+    hipLaunchKernelGGL((join_bwd_kernel<R, 2, 1>), grid, dim3(256), lds, stream, a, part);
+  else if (s.waves == 4)
+    hipLaunchKernelGGL((join_bwd_kernel<R, 4, 1>), grid, dim3(256), 0, stream, a, part);
+  else if (s.waves == 8 && s.pieces == 1)
+    hipLaunchKernelGGL((join_bwd_kernel<R, 8, 1>), grid, dim3(512), 0, stream, a, part);
+  else if (s.waves == 8)
+    hipLaunchKernelGGL((join_bwd_kernel<R, 8, 2>), grid, dim3(512), 0, stream, a, part);
+  else
+    hipLaunchKernelGGL((join_bwd_wide_kernel<R>), grid, dim3(256), 0, stream, a, part);
+}
 
 }  // namespace
 
-size_t norm_join_bwd_workspace_bytes(int64_t T, int64_t d) { return (size_t)(bwd_groups(T) * 3 * d) * sizeof(float); }
+size_t norm_join_bwd_workspace_bytes(int64_t T, int64_t d, bool res_f32) {
+  return (size_t)(bwd_grid(T, d, res_f32) * 2 * d) * sizeof(float);
+}
 
 hipError_t run_norm_join_fwd(const NormJoinArgs& a, hipStream_t stream) {
   TimedLaunch tl("norm_join_fwd", stream);
   if (a.res_f32)
-    hipLaunchKernelGGL(join_fwd_kernel<float>, dim3((unsigned)std::min<int64_t>(a.T, 1 << 20)), dim3(256), 0, stream, a);
+    launch_fwd<float>(a, stream);
   else
-    hipLaunchKernelGGL(join_fwd_kernel<uint16_t>, dim3((unsigned)std::min<int64_t>(a.T, 1 << 20)), dim3(256), 0, stream, a);
+    launch_fwd<uint16_t>(a, stream);
   return hipGetLastError();
 }
 
 hipError_t run_norm_join_bwd(const NormJoinArgs& a, hipStream_t stream) {
-  float* part = (float*)a.ws;
-  const unsigned groups = (unsigned)bwd_groups(a.T);
+  const bool first = a.dw_pre, second = a.dw_post || (a.dgate && !a.gate_token);
+  float* part = first || second ? (float*)a.ws : nullptr;
   {
     TimedLaunch tl("norm_join_bwd", stream);
     if (a.res_f32)
-      hipLaunchKernelGGL(join_bwd_kernel<float>, dim3(groups), dim3(256), 0, stream, a, part);
+      launch_bwd<float>(a, part, stream);
     else
-      hipLaunchKernelGGL(join_bwd_kernel<uint16_t>, dim3(groups), dim3(256), 0, stream, a, part);
+      launch_bwd<uint16_t>(a, part, stream);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || !part) return e;
   }
   TimedLaunch tl("norm_join_bwd_sums", stream);
-  hipLaunchKernelGGL(join_reduce_kernel, dim3((unsigned)((3 * a.d + 255) / 256)), dim3(256), 0, stream, part, (int64_t)groups, a.d,
-                     a.gate_token ? nullptr : (float*)a.dgate, a.dw_post, a.dw_pre);
+  const int64_t c0 = first ? 0 : a.d, c1 = second ? 2 * a.d : a.d;
+  hipLaunchKernelGGL(join_reduce_kernel, dim3((unsigned)((c1 - c0 + 31) / 32)), dim3(256), 0, stream, a, (const float*)part,
+                     (int)bwd_grid(a.T, a.d, a.res_f32), c0, c1);
   return hipGetLastError();
 }
 

@@ -12,7 +12,7 @@ import ctypes
 
 import torch
 
-from . import _check, _f32, _i64, _p, _SIGNATURES, _stream, _sz, _u32, _workspace, lib
+from . import _check, _f32, _i64, _p, _SIGNATURES, _sz, _u32, _workspace, lib
 
 __all__ = [
     "ELAS_RES_F32", "ELAS_GATE_TOKEN", "ELAS_IDS_I64", "ELAS_EMBED_ADD", "ELAS_GRAD_F32", "ELAS_GRAD_BF16",
@@ -43,6 +43,11 @@ _SIGNATURES.update({
 })
 
 _BF16, _F32 = torch.bfloat16, torch.float32
+
+
+# torch's current stream of a device, without the object that torch.cuda.current_stream makes
+# (0.1 us instead of 1.9, of calls of 6)
+_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _arg(t: torch.Tensor, shape, dtype: torch.dtype, device: int, name: str) -> int:
@@ -119,7 +124,7 @@ def elas_norm_join_fwd(h, b=None, gate=None, w_post=None, w_pre=None, res_scale:
     ho_p = None if b is None else _arg(_required(out.get("h"), "out['h']"), (T, d), h.dtype, dev, "out['h']")
     n_p = None if w_pre is None else _arg(_required(out.get("n"), "out['n']"), (T, d), _BF16, dev, "out['n']")
     _check(lib().elas_norm_join_fwd(h_p, b_p, gate_p, post_p, pre_p, T, d, res_scale, block_scale, eps, flags | gate_flag,
-                                    ho_p, n_p, _stream(h.device)))
+                                    ho_p, n_p, _stream(dev)))
     return out
 
 
@@ -167,7 +172,7 @@ def elas_norm_join_bwd(dh, dn, h, b=None, gate=None, w_post=None, w_pre=None, re
            grad("dw_post", w_post, row, _F32), grad("dw_pre", w_pre, row, _F32))
     workspace, ws_p, ws_n = _scratch(workspace, elas_norm_join_bwd_workspace_bytes(T, d, flags | gate_flag), device)
     _check(lib().elas_norm_join_bwd(dh_p, dn_p, h_p, b_p, gate_p, post_p, pre_p, T, d, res_scale, block_scale, eps,
-                                    flags | gate_flag, *out, ws_p, ws_n, _stream(device)))
+                                    flags | gate_flag, *out, ws_p, ws_n, _stream(dev)))
     return grads
 
 
@@ -194,7 +199,7 @@ def elas_embed_fwd(ids, table, scale: float = 1.0, dtype: torch.dtype = torch.bf
     flags |= _res_flag(dtype, "dtype")
     table_p = _arg(table, (V, d), _BF16, dev, "table")
     out_p = _arg(out, (*ids.shape, d), dtype, dev, "out")
-    _check(lib().elas_embed_fwd(ids_p, table_p, ids.numel(), V, d, scale, flags, out_p, _stream(table.device)))
+    _check(lib().elas_embed_fwd(ids_p, table_p, ids.numel(), V, d, scale, flags, out_p, _stream(dev)))
     return out
 
 
@@ -221,7 +226,7 @@ def elas_embed_bwd(ids, dx, V: int, scale: float = 1.0, dtable: torch.Tensor | N
     dtable_p = _arg(dtable, (V, d), _F32, dev, "dtable")
     T = ids.numel()
     workspace, ws_p, ws_n = _scratch(workspace, elas_embed_bwd_workspace_bytes(T, V, d, flags), dx.device)
-    _check(lib().elas_embed_bwd(ids_p, dx_p, T, V, d, scale, flags, dtable_p, ws_p, ws_n, _stream(dx.device)))
+    _check(lib().elas_embed_bwd(ids_p, dx_p, T, V, d, scale, flags, dtable_p, ws_p, ws_n, _stream(dev)))
     return dtable
 
 
@@ -279,7 +284,7 @@ def elas_grad_norm(grads, norm: torch.Tensor | None = None, workspace: torch.Ten
         norm = torch.empty(1, dtype=_F32, device=dev)
     norm_p = _arg(norm, (1,), _F32, dev.index, "norm")
     workspace, ws_p, ws_n = _scratch(workspace, elas_grad_workspace_bytes(len(grads)), dev)
-    _check(lib().elas_grad_norm(pointers, numel, dtype, len(grads), norm_p, ws_p, ws_n, _stream(dev)))
+    _check(lib().elas_grad_norm(pointers, numel, dtype, len(grads), norm_p, ws_p, ws_n, _stream(dev.index)))
     return norm
 
 
@@ -302,5 +307,5 @@ def elas_grad_clip(grads, max_norm: float, out=None, stats: torch.Tensor | None 
         stats = torch.empty(2, dtype=_F32, device=dev)
     stats_p = _arg(stats, (2,), _F32, dev.index, "stats")
     workspace, ws_p, ws_n = _scratch(workspace, elas_grad_workspace_bytes(len(grads)), dev)
-    _check(lib().elas_grad_clip(pointers, out_p, numel, dtype, len(grads), max_norm, stats_p, ws_p, ws_n, _stream(dev)))
+    _check(lib().elas_grad_clip(pointers, out_p, numel, dtype, len(grads), max_norm, stats_p, ws_p, ws_n, _stream(dev.index)))
     return stats
