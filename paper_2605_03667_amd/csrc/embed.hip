@@ -33,22 +33,25 @@ __device__ __forceinline__ uint32_t key_at(const EmbedArgs& a, int64_t t) {
 
 // Parts of 512 features of consecutive tokens, numbered through; a wave takes 4 of
 // them, `parts` to a token.
-template <class R>
+template <class R, bool STREAM>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(const EmbedArgs a, uint32_t parts) {
+  constexpr bool SPLIT = sizeof(R) == 4;
   const uint32_t lane = threadIdx.x & 63;
   const int64_t waves = (int64_t)gridDim.x * 4, total = a.T * parts;
-  for (int64_t q0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 4; q0 < total; q0 += waves * 4) {
+  for (int64_t q0 = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 4; q0 < total; q0 += waves * 4) {
     int64_t t = q0 / parts;   // (the one division of a wave's turn)
     uint32_t part = (uint32_t)(q0 - t * parts);
-    Piece<uint16_t> row[4];
+    Piece<uint16_t, SPLIT> row[4];
     int64_t at[4];
-    bool ok[4];
+    bool there[4], there2[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const uint32_t c = part * 512 + lane * 8;
-      ok[k] = t < a.T && c < (uint32_t)a.d;
+      const uint32_t c = part * 512 + lane * (SPLIT ? 4 : 8);
+      there[k] = t < a.T && c < (uint32_t)a.d;
+      there2[k] = SPLIT ? t < a.T && c + 256 < (uint32_t)a.d : there[k];
       const uint32_t key = t < a.T ? key_at(a, t) : (uint32_t)a.V;
-      row[k].load(a.table + (int64_t)key * a.d + c, ok[k] && key < (uint32_t)a.V);
+      const bool inside = key < (uint32_t)a.V;
+      row[k].load(a.table + (int64_t)key * a.d + c, there[k] && inside, there2[k] && inside);
       at[k] = t * a.d + c;
       if (++part == parts) part = 0, ++t;
     }
@@ -58,7 +61,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const EmbedArgs a, uint3
       row[k].get(v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= a.scale;
-      if (ok[k]) store8((R*)a.x + at[k], v);
+      Piece<R, SPLIT>::template store<STREAM>((R*)a.x + at[k], v, there[k], there2[k]);
     }
   }
 }
@@ -170,10 +173,10 @@ __global__ __launch_bounds__(1024) void embed_sort_kernel(const EmbedArgs a, int
   }
 }
 
-// The keys and tokens a pass starts from: the ids in their order, or what the pass
-// before left.
+// The keys and tokens a pass starts from: the ids in their order (NULL), or what the
+// pass before left.
 struct SortInput {
-  const uint32_t *key, *pos;   // NULL: the ids
+  const uint32_t *key, *pos;
 };
 __device__ __forceinline__ uint32_t input_key(const EmbedArgs& a, const SortInput& in, int64_t t) { return in.key ? in.key[t] : key_at(a, t); }
 
@@ -193,13 +196,14 @@ __global__ __launch_bounds__(1024) void embed_hist_kernel(const EmbedArgs a, Sor
   if ((int)threadIdx.x < bins) hist[(int64_t)blockIdx.x * bins + threadIdx.x] = count[threadIdx.x];
 }
 
+// (Counting the next pass's digits here, with atomics, instead of in a launch of their own
+// was measured: 48 us instead of 10 + 5 at 65536 tokens, most of which share few digits.)
 template <int E>
 __global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, SortInput in, int shift, int bits, const uint32_t* hist,
                                                              uint32_t* key_out, uint32_t* pos_out) {
   __shared__ uint32_t count[16 * kDigits], base[kDigits], tmp[8];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int bins = 1 << bits;
-  for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) count[i] = 0;
   uint32_t k[E], pos[E], digit[E], rank[E];
   bool ok[E];
 #pragma unroll
@@ -208,12 +212,12 @@ __global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, 
     ok[r] = t < a.T;
     k[r] = ok[r] ? input_key(a, in, t) : 0u;
     pos[r] = ok[r] && in.pos ? in.pos[t] : (uint32_t)t;
-    digit[r] = (k[r] >> shift) & (uint32_t)(bins - 1);
   }
+  for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) count[i] = 0;
   // the digit's tokens in all workgroups and in those before this one
   uint32_t all = 0, before = 0;
   if ((int)threadIdx.x < bins) {
-#pragma unroll 8
+#pragma unroll 16
     for (uint32_t g = 0; g < gridDim.x; ++g) {
       const uint32_t n = hist[(int64_t)g * bins + threadIdx.x];
       all += n;
@@ -222,17 +226,19 @@ __global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, 
   }
   const uint32_t first = bin_scan(all, bins, tmp);   // (its barrier: the counters are cleared)
   if ((int)threadIdx.x < bins) base[threadIdx.x] = first + before;
+#pragma unroll
+  for (int r = 0; r < E; ++r) digit[r] = (k[r] >> shift) & (uint32_t)(bins - 1);
   wave_ranks<E>(digit, ok, bits, count + wave * kDigits, rank);
   __syncthreads();
   wave_prefixes(count, bins);
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < E; ++r)
-    if (ok[r]) {
-      const uint32_t at = base[digit[r]] + count[wave * kDigits + digit[r]] + rank[r];
-      key_out[at] = k[r];
-      pos_out[at] = pos[r];
-    }
+  for (int r = 0; r < E; ++r) {
+    if (!ok[r]) continue;
+    const uint32_t at = base[digit[r]] + count[wave * kDigits + digit[r]] + rank[r];
+    key_out[at] = k[r];
+    pos_out[at] = pos[r];
+  }
 }
 
 // ---- the sums -------------------------------------------------------------------------
@@ -307,44 +313,58 @@ __device__ __forceinline__ Cut cut_at(const EmbedArgs& a, const uint32_t* key, i
   return c;
 }
 
+// A value that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)v >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
 template <class R, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const SumArgs s) {
-  constexpr int U = ADD ? 4 : 8;   // tokens on their way at once
-  const int lane = threadIdx.x & 63;
-  const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t chunk = task / s.slices;
+  constexpr int U = ADD ? 4 : sizeof(R) == 2 ? 16 : 8;   // tokens on their way at once
+  __shared__ Cut cuts[5];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // the workgroup's 4 tasks lie in at most 4 chunks: their cuts, one to a wave
+  const int64_t task0 = (int64_t)blockIdx.x * 4, chunk0 = task0 / s.slices, last = (task0 + 3) / s.slices + 1;
+  for (int i = wave; chunk0 + i <= last; i += 4) {
+    const Cut c = cut_at(a, s.key, (chunk0 + i) * s.chunk);
+    if (lane == 0) cuts[i] = c;
+  }
+  __syncthreads();
+  const int64_t task = task0 + wave, chunk = task / s.slices;
   if (chunk >= s.chunks) return;   // (no barriers below)
   const int slice = (int)(task - chunk * s.slices);
-  const uint32_t c = (uint32_t)slice * 512 + lane * 8;
-  const bool there = c < (uint32_t)a.d;
-  const Cut c0 = cut_at(a, s.key, chunk * s.chunk), c1 = cut_at(a, s.key, (chunk + 1) * s.chunk);
+  const uint32_t c = (uint32_t)slice * 512 + lane * 4;
+  const bool there = c < (uint32_t)a.d, there2 = c + 256 < (uint32_t)a.d;
+  const int i0 = (int)(chunk - chunk0);
+  const Cut c0 = {uniform(cuts[i0].p), (uint32_t)uniform(cuts[i0].v)}, c1 = {uniform(cuts[i0 + 1].p), (uint32_t)uniform(cuts[i0 + 1].v)};
   const uint32_t V = (uint32_t)a.V;
   float acc[8] = {};
   uint32_t row = c0.v;   // the row being added up
   bool open = false;     // whether it has tokens here
-  auto store = [&](uint32_t v, const Piece<float>& old) __attribute__((always_inline)) {
+  auto store = [&](uint32_t v, const Piece<float, true>& old) __attribute__((always_inline)) {
     float o[8];
     if (ADD) old.get(o);
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = ADD ? fmaf(a.scale, acc[i], o[i]) : a.scale * acc[i], acc[i] = 0.f;
-    if (there) store8(a.dtable + (int64_t)v * a.d + c, o);
+    Piece<float, true>::store<!ADD>((a.dtable + (int64_t)v * a.d) + c, o, there, there2);
   };
-  const Piece<float> nothing = {};
+  const Piece<float, true> nothing = {};
   int64_t p = c0.p;
   for (; p < c1.p; p += 64) {
     const int n = (int)min((int64_t)64, c1.p - p);
     const uint32_t k = lane < n ? s.key[p + lane] : V, pos = lane < n ? s.pos[p + lane] : 0u;
     const uint32_t after = ADD && lane < n && p + lane + 1 < a.T ? s.key[p + lane + 1] : V + 1;
     for (int j = 0; j < n; j += U) {
-      Piece<R> x[U];
-      Piece<float> old[ADD ? U : 1];
+      Piece<R, true> x[U];
+      Piece<float, true> old[ADD ? U : 1];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const uint32_t ku = __builtin_amdgcn_readlane(k, j + u);   // (past n: V)
         const int64_t t = __builtin_amdgcn_readlane(pos, j + u);
         if (ku >= V) continue;
-        x[u].load(((const R*)a.dx + t * a.d) + c, there);
-        if (ADD && __builtin_amdgcn_readlane(after, j + u) != ku) old[ADD ? u : 0].load((a.dtable + (int64_t)ku * a.d) + c, there);
+        x[u].load(((const R*)a.dx + t * a.d) + c, there, there2);
+        if (ADD && __builtin_amdgcn_readlane(after, j + u) != ku) old[ADD ? u : 0].load((a.dtable + (int64_t)ku * a.d) + c, there, there2);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -367,49 +387,56 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const
   }
   if (!ADD)
     for (; row < c1.v; ++row, open = false) store(row, nothing);
-  if (open && there) {
+  if (open) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] *= a.scale;
-    store8(s.carry + chunk * a.d + c, acc);
+    Piece<float, true>::store<false>((s.carry + chunk * a.d) + c, acc, there, there2);
   }
   if (slice == 0 && lane == 0) s.carry_row[chunk] = open ? row : ~0u;
 }
 
 // Adds the sums of the chunks that left a row open, in their order, to the row.  A
-// workgroup looks after the run of such chunks that begins at its own; its 4 quarters
-// take a share of a long run each.
+// workgroup looks after the run of such chunks that begins at its own, for 1024
+// columns; its 4 quarters take a share of the run each.
 __global__ __launch_bounds__(1024) void embed_join_kernel(const EmbedArgs a, const SumArgs s) {
   __shared__ float4 red[3][256];
-  const int c0 = blockIdx.x;
-  const uint32_t row = s.carry_row[c0];
-  if (row == ~0u || (c0 > 0 && s.carry_row[c0 - 1] == row)) return;
-  int n = 1;
-  while (c0 + n < s.chunks && s.carry_row[c0 + n] == row) ++n;
+  const int lane = threadIdx.x & 63, c0 = blockIdx.x;
+  // rows of the chunk before, of this one and of the next 62
+  const int q0 = c0 - 1 + lane;
+  const uint32_t near = q0 >= 0 && q0 < s.chunks ? s.carry_row[q0] : ~0u;
+  const uint32_t row = __builtin_amdgcn_readlane(near, 1);
+  if (row == ~0u || __builtin_amdgcn_readlane(near, 0) == row) return;
+  uint64_t other = __ballot(near != row) & ~1ull;
+  int n = 0;   // chunks of the run
+  for (int q = c0 - 1; other == 0;) {
+    q += 64;
+    n = q - c0;
+    other = __ballot(!(q + lane < s.chunks && s.carry_row[q + lane] == row));
+  }
+  n = n > 0 ? n + __ffsll((unsigned long long)other) - 1 : __ffsll((unsigned long long)other) - 2;
   const int quarter = threadIdx.x >> 8, i = threadIdx.x & 255;
-  const int b = c0 + n * quarter / 4, e = c0 + n * (quarter + 1) / 4;
-  for (int64_t at = 0; at < a.d; at += 1024) {
-    const int64_t c = at + i * 4;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (c < a.d) {
+  const int b = c0 + (int)((int64_t)n * quarter / 4), e = c0 + (int)((int64_t)n * (quarter + 1) / 4);
+  const int64_t c = (int64_t)blockIdx.y * 1024 + i * 4;
+  const bool there = c < a.d;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (there) {
 #pragma unroll 8
-      for (int k = b; k < e; ++k) {
-        const float4 y = *(const float4*)(s.carry + (int64_t)k * a.d + c);
-        x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
-      }
-    }
-    __syncthreads();
-    if (quarter > 0) red[quarter - 1][i] = x;
-    __syncthreads();
-    if (quarter > 0 || c >= a.d) continue;
-    float4* out = (float4*)(a.dtable + (int64_t)row * a.d + c);
-    const float4 o = *out;
-#pragma unroll
-    for (int q = 0; q < 3; ++q) {
-      const float4 y = red[q][i];
+    for (int k = b; k < e; ++k) {
+      const float4 y = *(const float4*)(s.carry + (int64_t)k * a.d + c);
       x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
     }
-    *out = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
   }
+  if (quarter > 0) red[quarter - 1][i] = x;
+  __syncthreads();
+  if (quarter > 0 || !there) return;
+  float4* out = (float4*)(a.dtable + (int64_t)row * a.d + c);
+  const float4 o = *out;
+#pragma unroll
+  for (int q = 0; q < 3; ++q) {
+    const float4 y = red[q][i];
+    x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+  }
+  *out = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
 }
 
 // ---- host -----------------------------------------------------------------------------
@@ -436,8 +463,8 @@ Plan plan(void* ws, int64_t T, int64_t V, int64_t d, bool add) {
   p.passes = (key_bits + 8) / 9;
   p.bits = (key_bits + p.passes - 1) / p.passes;
   p.tbits = std::max(1, bit_length(T - 1));
-  p.one_group = T <= 16384 && key_bits + p.tbits <= 32;
-  p.per_thread = p.one_group ? (T <= 1024 ? 1 : T <= 4096 ? 4 : 16) : (T <= (1 << 18) ? 4 : 16);
+  p.one_group = T <= 4096 && key_bits + p.tbits <= 32;
+  p.per_thread = p.one_group ? (T <= 1024 ? 1 : 4) : T <= 131072 ? 1 : T <= (1 << 18) ? 4 : 8;
   p.groups = (int)cdiv(T, 1024 * p.per_thread);
   p.sum.slices = (int)cdiv(d, 512);
   // about 8 waves to a SIMD, and not under a few tokens or rows to a chunk
@@ -463,16 +490,17 @@ Plan plan(void* ws, int64_t T, int64_t V, int64_t d, bool add) {
 
 template <int E>
 hipError_t sort_passes(const EmbedArgs& a, const Plan& p, int& at, hipStream_t stream) {
+  const dim3 grid((unsigned)p.groups), block(1024);
   for (int k = 0; k < p.passes; ++k) {
     const int to = p.passes == 1 ? 0 : k & 1;
     const SortInput in = k == 0 ? SortInput{nullptr, nullptr} : SortInput{p.key[1 - to], p.pos[1 - to]};
     {
       TimedLaunch tl("embed_bwd_sort", stream);
-      hipLaunchKernelGGL(embed_hist_kernel<E>, dim3((unsigned)p.groups), dim3(1024), 0, stream, a, in, k * p.bits, p.bits, p.hist);
+      hipLaunchKernelGGL(embed_hist_kernel<E>, grid, block, 0, stream, a, in, k * p.bits, p.bits, p.hist);
     }
     TimedLaunch tl("embed_bwd_sort", stream);
-    hipLaunchKernelGGL(embed_scatter_kernel<E>, dim3((unsigned)p.groups), dim3(1024), 0, stream, a, in, k * p.bits, p.bits,
-                       (const uint32_t*)p.hist, p.key[to], p.pos[to]);
+    hipLaunchKernelGGL(embed_scatter_kernel<E>, grid, block, 0, stream, a, in, k * p.bits, p.bits, (const uint32_t*)p.hist, p.key[to],
+                       p.pos[to]);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     at = to;
@@ -484,6 +512,11 @@ template <int E>
 void sort_one_group(const EmbedArgs& a, const Plan& p, hipStream_t stream) {
   TimedLaunch tl("embed_bwd_sort", stream);
   hipLaunchKernelGGL(embed_sort_kernel<E>, dim3(1), dim3(1024), 0, stream, a, p.passes, p.bits, p.tbits, p.key[0], p.pos[0]);
+}
+
+template <class R, bool STREAM>
+void launch_fwd(const EmbedArgs& a, uint32_t parts, unsigned grid, hipStream_t stream) {
+  hipLaunchKernelGGL((embed_fwd_kernel<R, STREAM>), dim3(grid), dim3(256), 0, stream, a, parts);
 }
 
 template <class R>
@@ -503,10 +536,10 @@ hipError_t run_embed_fwd(const EmbedArgs& a, hipStream_t stream) {
   TimedLaunch tl("embed_fwd", stream);
   const uint32_t parts = (uint32_t)cdiv(a.d, 512);
   const unsigned grid = (unsigned)std::min<int64_t>(cdiv(a.T * parts, 16), 1 << 20);
-  if (a.res_f32)
-    hipLaunchKernelGGL(embed_fwd_kernel<float>, dim3(grid), dim3(256), 0, stream, a, parts);
+  if (a.T * a.d < kStreamStores)
+    a.res_f32 ? launch_fwd<float, false>(a, parts, grid, stream) : launch_fwd<uint16_t, false>(a, parts, grid, stream);
   else
-    hipLaunchKernelGGL(embed_fwd_kernel<uint16_t>, dim3(grid), dim3(256), 0, stream, a, parts);
+    a.res_f32 ? launch_fwd<float, true>(a, parts, grid, stream) : launch_fwd<uint16_t, true>(a, parts, grid, stream);
   return hipGetLastError();
 }
 
@@ -516,13 +549,13 @@ hipError_t run_embed_bwd(const EmbedArgs& a, hipStream_t stream) {
   if (a.T > 0) {
     hipError_t e = hipSuccess;
     if (!p.one_group)
-      e = p.per_thread == 4 ? sort_passes<4>(a, p, at, stream) : sort_passes<16>(a, p, at, stream);
+      e = p.per_thread == 1   ? sort_passes<1>(a, p, at, stream)
+          : p.per_thread == 4 ? sort_passes<4>(a, p, at, stream)
+                              : sort_passes<8>(a, p, at, stream);
     else if (p.per_thread == 1)
       sort_one_group<1>(a, p, stream);
-    else if (p.per_thread == 4)
-      sort_one_group<4>(a, p, stream);
     else
-      sort_one_group<16>(a, p, stream);
+      sort_one_group<4>(a, p, stream);
     if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -538,7 +571,7 @@ hipError_t run_embed_bwd(const EmbedArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   TimedLaunch tl("embed_bwd_join", stream);
-  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)p.sum.chunks), dim3(1024), 0, stream, a, p.sum);
+  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)p.sum.chunks, (unsigned)cdiv(a.d, 1024)), dim3(1024), 0, stream, a, p.sum);
   return hipGetLastError();
 }
 

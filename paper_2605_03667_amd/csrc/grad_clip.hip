@@ -24,6 +24,10 @@ namespace {
 constexpr int kTensors = 128;     // per launch: the table below is a kernel argument (< 4 KB)
 constexpr int kPiece = 8192;      // values
 constexpr int kGroups = 2048;     // most workgroups, and partial sums, per launch
+// The squares are read past the caches, except, where there is more than the last-level
+// cache holds, for the last part, which the scaling takes first (1B: all kept 516 us, none
+// 512, 64 MB 502, 128 MB 491, 192 MB 498; 152 MB in all: kept 86, not 77).
+constexpr int64_t kCache = int64_t(256) << 20, kKeep = int64_t(128) << 20;
 
 struct GradTable {
   const void* in[kTensors];
@@ -38,70 +42,121 @@ struct GradTable {
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
-// Values of one thread in a full piece: 32, as 16-byte parts of which part k of all
-// threads is contiguous.
-__device__ __forceinline__ void load_part(const float* p, float (&v)[4]) {
-  const f32x4 q = *(const f32x4_any*)p;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = q[i];
-}
-__device__ __forceinline__ void load_part(const uint16_t* p, float (&v)[8]) {
-  const u32x4 q = *(const u32x4_any*)p;
-  unpack8(make_uint4(q[0], q[1], q[2], q[3]), v);
-}
-__device__ __forceinline__ void store_part(float* p, const float (&v)[4]) {
-  *(f32x4_any*)p = f32x4{v[0], v[1], v[2], v[3]};
-}
-__device__ __forceinline__ void store_part(uint16_t* p, const float (&v)[8]) {
-  *(u32x4_any*)p = u32x4{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3]), bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7])};
-}
 __device__ __forceinline__ float value_of(float e) { return e; }
-__device__ __forceinline__ float value_of(uint16_t e) { return __builtin_bit_cast(float, (uint32_t)e << 16); }
+__device__ __forceinline__ float value_of(uint16_t e) { return as_float((uint32_t)e << 16); }
 __device__ __forceinline__ void set_value(float* p, float v) { *p = v; }
 __device__ __forceinline__ void set_value(uint16_t* p, float v) { *p = (uint16_t)bf16x2_rne(v, 0.f); }
 
-// Squares are taken in 64 bits: exact for every float, and no sum of them overflows.
+// A thread's values of a piece: PARTS parts of 16 bytes, part k of all threads contiguous.
 template <class E>
-__device__ __forceinline__ void square_piece(const E* g, int64_t n, double (&s)[2]) {
-  constexpr int N = 16 / sizeof(E), PARTS = 32 / N;
-  float v[PARTS][N];
-  if (n >= kPiece) {
+struct Part {
+  static constexpr int N = 16 / sizeof(E), PARTS = kPiece / 256 / N;
+  static __device__ __forceinline__ int first(int k) { return (k * 256 + (int)threadIdx.x) * N; }
+  template <bool STREAM>
+  static __device__ __forceinline__ void load(const E* p, float (&v)[N]) {
+    if constexpr (N == 4) {
+      const f32x4 q = load_as<STREAM>((const f32x4_any*)p);
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k) load_part(g + (k * 256 + threadIdx.x) * N, v[k]);
+      for (int i = 0; i < N; ++i) v[i] = q[i];
+    } else {
+      const u32x4 q = load_as<STREAM>((const u32x4_any*)p);
+      unpack8(make_uint4(q[0], q[1], q[2], q[3]), v);
+    }
+  }
+  static __device__ __forceinline__ void store(E* p, const float (&v)[N]) {
+    if constexpr (N == 4)
+      store_as<true>((f32x4_any*)p, (f32x4_any)f32x4{v[0], v[1], v[2], v[3]});
+    else
+      store_as<true>((u32x4_any*)p, (u32x4_any)u32x4{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3]), bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7])});
+  }
+};
+
+// Squares are taken in 64 bits: exact for every float, and no sum of them overflows.
+// (A piece that the tensor's end cuts: the part that it cuts is taken value by value.)
+template <bool STREAM, class E>
+__device__ __forceinline__ void square_piece(const E* g, int n, double (&s)[2]) {
+  using P = Part<E>;
+  auto add = [&](const float (&v)[P::N]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k)
+    for (int i = 0; i < P::N; ++i) s[i & 1] = fma((double)v[i], (double)v[i], s[i & 1]);
+  };
+  if (n == kPiece) {
+    float v[P::PARTS][P::N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) s[i & 1] = fma((double)v[k][i], (double)v[k][i], s[i & 1]);
+    for (int k = 0; k < P::PARTS; ++k) P::template load<STREAM>(g + P::first(k), v[k]);
+#pragma unroll
+    for (int k = 0; k < P::PARTS; ++k) add(v[k]);
     return;
   }
-  for (int64_t i = threadIdx.x; i < n; i += 256) {
+#pragma unroll 4
+  for (int at = P::first(0); at + P::N <= n; at += 256 * P::N) {
+    float v[P::N];
+    P::template load<STREAM>(g + at, v);
+    add(v);
+  }
+  const int i = n / P::N * P::N + (int)threadIdx.x;
+  if (i < n) {
     const double x = value_of(g[i]);
     s[0] = fma(x, x, s[0]);
   }
 }
 
-// Piece c's tensor, walking from tensor k (either way), and whether it is bf16.
-__device__ __forceinline__ int tensor_of(const uint32_t* first, uint32_t c, int k) {
-  while (c >= first[k + 1]) ++k;
-  while (c < first[k]) --k;
-  return k;
+template <class E>
+__device__ __forceinline__ void scale_piece(const E* g, E* out, int n, float f) {
+  using P = Part<E>;
+  auto scaled = [&](int at, float (&v)[P::N]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < P::N; ++i) v[i] *= f;
+    P::store(out + at, v);
+  };
+  if (n == kPiece) {
+    float v[P::PARTS][P::N];
+#pragma unroll
+    for (int k = 0; k < P::PARTS; ++k) P::template load<true>(g + P::first(k), v[k]);
+#pragma unroll
+    for (int k = 0; k < P::PARTS; ++k) scaled(P::first(k), v[k]);
+    return;
+  }
+  for (int at = P::first(0); at + P::N <= n; at += 256 * P::N) {
+    float v[P::N];
+    P::template load<true>(g + at, v);
+    scaled(at, v);
+  }
+  const int i = n / P::N * P::N + (int)threadIdx.x;
+  if (i < n) set_value(out + i, value_of(g[i]) * f);
 }
 
-__global__ __launch_bounds__(256) void grad_square_kernel(const GradTable g, double* part) {
+// Which tensor a piece belongs to: the last one whose first piece is not behind it.
+// Lane l holds the first pieces of the tensors l and l + 64.
+struct Finder {
+  uint32_t f0, f1;
+  __device__ __forceinline__ explicit Finder(const GradTable& g) {
+    const int lane = threadIdx.x & 63;
+    f0 = lane < g.count ? g.first[lane] : ~0u;
+    f1 = lane + 64 < g.count ? g.first[lane + 64] : ~0u;
+  }
+  __device__ __forceinline__ int operator()(uint32_t piece) const {
+    return __popcll(__ballot(f0 <= piece)) + __popcll(__ballot(f1 <= piece)) - 1;
+  }
+};
+
+__global__ __launch_bounds__(256) void grad_square_kernel(const GradTable g, uint32_t keep, double* part) {
   __shared__ double red[4];
-  __shared__ uint32_t first[kTensors + 1];
-  for (int k = threadIdx.x; k <= g.count; k += 256) first[k] = g.first[k];
-  __syncthreads();
-  const uint32_t pieces = first[g.count];
+  const Finder find(g);
+  const uint32_t pieces = g.first[g.count];
   double s[2] = {0.0, 0.0};
-  int k = 0;
   for (uint32_t c = blockIdx.x; c < pieces; c += gridDim.x) {
-    k = __builtin_amdgcn_readfirstlane(tensor_of(first, c, k));
-    const int64_t at = (int64_t)(c - first[k]) * kPiece, n = g.n[k] - at;
-    if (g.bf16[k >> 5] >> (k & 31) & 1u)
-      square_piece((const uint16_t*)g.in[k] + at, n, s);
-    else
-      square_piece((const float*)g.in[k] + at, n, s);
+    const int k = find(c);
+    const int64_t at = (int64_t)(c - g.first[k]) * kPiece;
+    const int n = (int)min(g.n[k] - at, (int64_t)kPiece);
+    // the last `keep` pieces are left in the caches
+    if (g.bf16[k >> 5] >> (k & 31) & 1u) {
+      const uint16_t* p = (const uint16_t*)g.in[k] + at;
+      c + keep < pieces ? square_piece<true>(p, n, s) : square_piece<false>(p, n, s);
+    } else {
+      const float* p = (const float*)g.in[k] + at;
+      c + keep < pieces ? square_piece<true>(p, n, s) : square_piece<false>(p, n, s);
+    }
   }
   const double sum = block_sum<4>(s[0] + s[1], red);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
@@ -120,43 +175,24 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const double* part, int6
   if (threadIdx.x == 0) norm[0] = (float)v;
 }
 
-template <class E>
-__device__ __forceinline__ void scale_piece(const E* g, E* out, int64_t n, float f) {
-  constexpr int N = 16 / sizeof(E), PARTS = 32 / N;
-  if (n >= kPiece) {
-    float v[PARTS][N];
-#pragma unroll
-    for (int k = 0; k < PARTS; ++k) load_part(g + (k * 256 + threadIdx.x) * N, v[k]);
-#pragma unroll
-    for (int k = 0; k < PARTS; ++k) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[k][i] *= f;
-      store_part(out + (k * 256 + threadIdx.x) * N, v[k]);
-    }
-    return;
-  }
-  for (int64_t i = threadIdx.x; i < n; i += 256) set_value(out + i, value_of(g[i]) * f);
-}
-
 // stats NULL: another launch writes them.
 __global__ __launch_bounds__(256) void grad_scale_kernel(const GradTable g, const double* part, int64_t parts, float max_norm, float* stats) {
   __shared__ double red[4];
-  __shared__ uint32_t first[kTensors + 1];
-  for (int k = threadIdx.x; k <= g.count; k += 256) first[k] = g.first[k];
-  const double norm = norm_of(part, parts, red);   // (its barriers are passed before `first` is read)
+  const Finder find(g);
+  const double norm = norm_of(part, parts, red);
   const bool finite = norm < (double)INFINITY, clips = finite && norm > (double)max_norm;
   const float factor = clips ? (float)((double)max_norm / norm) : 1.f;
   if (stats && blockIdx.x == 0 && threadIdx.x == 0) {
     stats[0] = (float)norm;
     stats[1] = finite ? factor : 0.f;
   }
-  const uint32_t pieces = first[g.count];
-  int k = g.count - 1;
+  const uint32_t pieces = g.first[g.count];
   for (uint32_t i = blockIdx.x; i < pieces; i += gridDim.x) {
     const uint32_t c = pieces - 1 - i;
-    k = __builtin_amdgcn_readfirstlane(tensor_of(first, c, k));
+    const int k = find(c);
     if (!clips && g.in[k] == g.out[k]) continue;
-    const int64_t at = (int64_t)(c - first[k]) * kPiece, n = g.n[k] - at;
+    const int64_t at = (int64_t)(c - g.first[k]) * kPiece;
+    const int n = (int)min(g.n[k] - at, (int64_t)kPiece);
     if (g.bf16[k >> 5] >> (k & 31) & 1u)
       scale_piece((const uint16_t*)g.in[k] + at, (uint16_t*)g.out[k] + at, n, factor);
     else
@@ -180,6 +216,18 @@ void fill(GradTable& g, const void* const* in, void* const* out, const int64_t* 
   g.first[g.count] = pieces;
 }
 
+// Pieces at the end of the launch that make up the last `bytes` of it; what is left of them.
+uint32_t last_pieces(const GradTable& g, int64_t& bytes) {
+  uint32_t pieces = 0;
+  for (int k = g.count - 1; k >= 0 && bytes > 0; --k) {
+    const int64_t piece = kPiece * ((g.bf16[k >> 5] >> (k & 31) & 1u) ? 2 : 4), all = g.first[k + 1] - g.first[k];
+    const int64_t some = std::min(all, bytes / piece);
+    pieces += (uint32_t)some;
+    bytes = some < all ? 0 : bytes - some * piece;
+  }
+  return pieces;
+}
+
 int64_t launches(int64_t n) { return (n + kTensors - 1) / kTensors; }
 
 }  // namespace
@@ -189,14 +237,18 @@ size_t grad_workspace_bytes(int64_t n) { return (size_t)launches(n) * kGroups * 
 hipError_t run_grad_norm(const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype, int64_t n, bool clip,
                          float max_norm, float* stats, void* ws, hipStream_t stream) {
   double* part = (double*)ws;
-  int64_t parts = 0;
+  int64_t parts = 0, total = 0;
+  for (int64_t k = 0; k < n; ++k) total += numel[k] * (dtype[k] == ELAS_GRAD_BF16 ? 2 : 4);
   GradTable g;
+  // what the squares leave in the caches: a launch other than the last one keeps nothing
+  int64_t keep = clip && total > kCache ? kKeep : 0;
   for (int64_t k = 0; k < n; k += kTensors) {
     fill(g, grads, out, numel, dtype, k, n);
+    const uint32_t kept = k + kTensors >= n ? last_pieces(g, keep) : 0;
     const unsigned groups = std::min<uint32_t>(g.first[g.count], kGroups);
     if (groups == 0) continue;
     TimedLaunch tl("grad_square", stream);
-    hipLaunchKernelGGL(grad_square_kernel, dim3(groups), dim3(256), 0, stream, g, part + parts);
+    hipLaunchKernelGGL(grad_square_kernel, dim3(groups), dim3(256), 0, stream, g, kept, part + parts);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     parts += groups;

@@ -9,25 +9,37 @@ namespace elas {
 
 namespace {
 
-// ---- rows of up to 2048 W NV features, W = 1, 2 or 4 waves to a row ----------------
-// The row stays in registers, lane l of the row's W waves holding the pieces of 8
-// features l, l + 64 W, ..  (NV of them).
+// ---- rows of up to 512 W NV features, W waves to a row -----------------------------
+// The row stays in registers: NV times 8 features to a lane.  Every operand is read once
+// and the row's sums need no second pass; what bounds the kernels is HBM.  More waves to
+// a row rather than more pieces to a lane (NV = 1 up to 4096 features): 1B backward, 65536
+// tokens: W = 4, NV = 1 315 us, W = 2, NV = 2 385 (it fills the registers, and fewer
+// waves are left to cover the loads).
 
-// Where a thread's row and pieces lie.
-template <int W, int NV>
+// Where a thread's row and pieces lie; loads and stores of piece v.
+template <int W, int NV, bool SPLIT>
 struct RowLanes {
   static constexpr int WAVES = W < 4 ? 4 : W;   // of a workgroup
   static constexpr int ROWS = WAVES / W;        // rows it works on at a time
   int slot;
   uint32_t c[NV];   // (unsigned: an offset beside a uniform address)
-  bool there[NV];
+  bool there[NV], there2[NV];
   __device__ __forceinline__ explicit RowLanes(int d) {
     slot = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W));   // (the same in all of a wave)
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      c[v] = ((v * W * 64) + threadIdx.x % (64 * W)) * 8;
+      c[v] = (v * W + threadIdx.x / 64 % W) * 512 + threadIdx.x % 64 * (SPLIT ? 4 : 8);
       there[v] = c[v] < (uint32_t)d;
+      there2[v] = SPLIT ? c[v] + 256 < (uint32_t)d : there[v];
     }
+  }
+  template <bool STREAM = false, class T>
+  __device__ __forceinline__ void load(Piece<T, SPLIT>& x, const T* row, int v, bool live) const {
+    x.template load<STREAM>(row + c[v], live && there[v], live && there2[v]);
+  }
+  template <bool STREAM = false, class T>
+  __device__ __forceinline__ void store(T* row, const float (&x)[8], int v, bool live) const {
+    Piece<T, SPLIT>::template store<STREAM>(row + c[v], x, live && there[v], live && there2[v]);
   }
 };
 
@@ -53,9 +65,10 @@ __device__ __forceinline__ void row_sums(float (&s)[N], float (&red)[WAVES][N]) 
   }
 }
 
-template <class R, int W, int NV>
+template <class R, int W, int NV, bool STREAM>
 __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_fwd_kernel(const NormJoinArgs a) {
-  using Lanes = RowLanes<W, NV>;
+  constexpr bool SPLIT = sizeof(R) == 4;
+  using Lanes = RowLanes<W, NV, SPLIT>;
   __shared__ float red[2][Lanes::WAVES][1];
   const Lanes l((int)a.d);
   const float inv_d = 1.f / (float)a.d;
@@ -63,14 +76,13 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_fwd_kernel(const No
     const int64_t t = t0 + l.slot, at = t * a.d;
     if (W == 1 && t >= a.T) break;
     const bool live = t < a.T;
-    Piece<R> h[NV];
-    Piece<uint16_t> b[NV], gate[NV];
+    Piece<R, SPLIT> h[NV];
+    Piece<uint16_t, SPLIT> b[NV], gate[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const bool ok = live && l.there[v];
-      h[v].load(((const R*)a.h + at) + l.c[v], ok);
-      if (a.b) b[v].load((a.b + at) + l.c[v], ok);
-      if (a.gate) gate[v].load(a.gate + (a.gate_token ? at : 0) + l.c[v], ok);
+      l.load(h[v], (const R*)a.h + at, v, live);
+      if (a.b) l.load(b[v], a.b + at, v, live);
+      if (a.gate) l.load(gate[v], a.gate + (a.gate_token ? at : 0), v, live);
     }
     float x[NV][8];
     if (a.b) {
@@ -92,8 +104,8 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_fwd_kernel(const No
         float u[8], k[8];
         b[v].get(u);
         if (a.w_post) {
-          Piece<uint16_t> w;
-          w.load(a.w_post + l.c[v], l.there[v]);
+          Piece<uint16_t, SPLIT> w;
+          l.load(w, a.w_post, v, true);
           w.get(k);
 #pragma unroll
           for (int i = 0; i < 8; ++i) u[i] = u[i] * rho * k[i];
@@ -106,7 +118,7 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_fwd_kernel(const No
         h[v].get(x[v]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[v][i] = fmaf(a.res_scale, x[v][i], a.block_scale * u[i]);
-        if (live && l.there[v]) store8(((R*)a.h_out + at) + l.c[v], x[v]);
+        l.template store<STREAM>((R*)a.h_out + at, x[v], v, live);
       }
     } else {
 #pragma unroll
@@ -123,12 +135,12 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_fwd_kernel(const No
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         float k[8];
-        Piece<uint16_t> w;
-        w.load(a.w_pre + l.c[v], l.there[v]);
+        Piece<uint16_t, SPLIT> w;
+        l.load(w, a.w_pre, v, true);
         w.get(k);
 #pragma unroll
         for (int i = 0; i < 8; ++i) k[i] *= x[v][i] * sig;
-        if (live && l.there[v]) store8((a.n + at) + l.c[v], k);
+        l.template store<STREAM>(a.n + at, k, v, live);
       }
     }
     // (a lone second or first sum would leave `red` in use)
@@ -139,35 +151,35 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_fwd_kernel(const No
 // The sums over the tokens: acc[0] of dn xh, acc[1] of G bh (times the token's
 // gate where there is one for each), added up in the workgroup at the end and
 // written to row blockIdx.x of `part`, [grid][2][d].
-template <class R, int W, int NV>
+template <class R, int W, int NV, bool STREAM>
 __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_bwd_kernel(const NormJoinArgs a, float* part) {
-  using Lanes = RowLanes<W, NV>;
+  constexpr bool SPLIT = sizeof(R) == 4;
+  using Lanes = RowLanes<W, NV, SPLIT>;
   __shared__ float red3[Lanes::WAVES][3], red1[Lanes::WAVES][1];
   const Lanes l((int)a.d);
   const float inv_d = 1.f / (float)a.d;
   float acc[2][NV][8] = {};
-  Piece<uint16_t> w_pre[NV], w_post[NV], shared[NV];
+  Piece<uint16_t, SPLIT> w_pre[NV], w_post[NV], shared[NV];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    if (a.w_pre) w_pre[v].load(a.w_pre + l.c[v], l.there[v]);
-    if (a.w_post) w_post[v].load(a.w_post + l.c[v], l.there[v]);
-    if (a.gate && !a.gate_token) shared[v].load(a.gate + l.c[v], l.there[v]);
+    if (a.w_pre) l.load(w_pre[v], a.w_pre, v, true);
+    if (a.w_post) l.load(w_post[v], a.w_post, v, true);
+    if (a.gate && !a.gate_token) l.load(shared[v], a.gate, v, true);
   }
   for (int64_t t0 = (int64_t)blockIdx.x * Lanes::ROWS; t0 < a.T; t0 += (int64_t)gridDim.x * Lanes::ROWS) {
     const int64_t t = t0 + l.slot, at = t * a.d;
-    Piece<R> h[NV], dho[NV];
-    Piece<uint16_t> dn[NV], b[NV], gate[NV];
-    bool ok[NV];
+    Piece<R, SPLIT> h[NV], dho[NV];
+    Piece<uint16_t, SPLIT> dn[NV], b[NV], gate[NV];
+    const bool live = t < a.T;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      ok[v] = t < a.T && l.there[v];
       if (a.w_pre) {
-        h[v].load(((const R*)a.h + at) + l.c[v], ok[v]);
-        dn[v].load((a.dn + at) + l.c[v], ok[v]);
+        l.template load<STREAM>(h[v], (const R*)a.h + at, v, live);
+        l.template load<STREAM>(dn[v], a.dn + at, v, live);
       }
-      if (a.b) b[v].load((a.b + at) + l.c[v], ok[v]);
-      if (a.dh_out) dho[v].load(((const R*)a.dh_out + at) + l.c[v], ok[v]);
-      if (a.gate_token) gate[v].load((a.gate + at) + l.c[v], ok[v]);
+      if (a.b) l.template load<STREAM>(b[v], a.b + at, v, live);
+      if (a.dh_out) l.template load<STREAM>(dho[v], (const R*)a.dh_out + at, v, live);
+      if (a.gate_token) l.template load<STREAM>(gate[v], a.gate + at, v, live);
     }
     float s[3] = {0.f, 0.f, 0.f};   // |h'|^2, q h', |b|^2
 #pragma unroll
@@ -211,10 +223,10 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_bwd_kernel(const No
           g[v][i] = fmaf(sig, fmaf(-ch, xh, q[i] * k[i]), g[v][i]);
         }
       }
-      if (a.dh && ok[v]) {
+      if (a.dh) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) q[i] = a.res_scale * g[v][i];
-        store8(((R*)a.dh + at) + l.c[v], q);
+        l.template store<true>((R*)a.dh + at, q, v, live);
       }
       if (!a.b) continue;
       b[v].get(x);
@@ -222,11 +234,9 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_bwd_kernel(const No
       for (int i = 0; i < 8; ++i) x[i] *= rho;
       if (a.w_post) w_post[v].get(k);
       if (a.gate_token) {
-        if (ok[v]) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) q[i] = a.block_scale * g[v][i] * (a.w_post ? x[i] * k[i] : x[i]);
-          store8(((uint16_t*)a.dgate + at) + l.c[v], q);
-        }
+        for (int i = 0; i < 8; ++i) q[i] = a.block_scale * g[v][i] * (a.w_post ? x[i] * k[i] : x[i]);
+        l.template store<true>((uint16_t*)a.dgate + at, q, v, live);
         gate[v].get(q);
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[v][i] *= q[i];
@@ -262,8 +272,7 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_bwd_kernel(const No
         }
       }
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
-        if (ok[v]) store8((a.db + at) + l.c[v], g[v]);
+      for (int v = 0; v < NV; ++v) l.template store<true>(a.db + at, g[v], v, live);
     }
     // (without a second sum red3 would still be in use)
     if (W > 1 && !a.w_post) __syncthreads();
@@ -279,15 +288,17 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_bwd_kernel(const No
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int v = 0; v < NV; ++v)
-          if (need[k] && l.there[v]) {
-            float* o = (r + 1 == Lanes::ROWS ? part + (int64_t)blockIdx.x * 2 * a.d : sum) + k * a.d + l.c[v];
+          if (need[k]) {
+            float* out = (r + 1 == Lanes::ROWS ? part + (int64_t)blockIdx.x * 2 * a.d : sum) + k * a.d;
             if (r > 0) {
+              Piece<float, SPLIT> before;
               float x[8];
-              load8(sum + k * a.d + l.c[v], x);
+              l.load(before, (const float*)sum + k * a.d, v, true);
+              before.get(x);
 #pragma unroll
               for (int i = 0; i < 8; ++i) acc[k][v][i] = x[i] + acc[k][v][i];
             }
-            store8(o, acc[k][v]);
+            l.store(out, acc[k][v], v, true);
           }
     }
     if (r + 1 < Lanes::ROWS) __syncthreads();
@@ -518,39 +529,45 @@ int64_t bwd_grid(int64_t T, int64_t d, bool res_f32) {
   return std::max<int64_t>(1, std::min<int64_t>(row_groups(T, d), res_f32 ? 512 : 1024));
 }
 
-template <class R>
+// Backward loads go past the caches where the call moves more than the last-level
+// cache's 256 MB (1B, 65536 tokens 316 -> 306 us); in a smaller one they would miss what
+// that cache holds (350M, 8192 tokens 24.8 -> 30.3).  Forward loads never gained (1B 280
+// -> 288).  Stores: kStreamStores in the forward, always in the backward.
+constexpr int64_t kStreamLoads = int64_t(1) << 28;    // bytes
+
+template <class R, bool STREAM>
 void launch_fwd(const NormJoinArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)fwd_grid(a.T, a.d));
   const RowShape s = row_shape(a.d);
   if (s.waves == 1)
-    hipLaunchKernelGGL((join_fwd_kernel<R, 1, 1>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((join_fwd_kernel<R, 1, 1, STREAM>), grid, dim3(256), 0, stream, a);
   else if (s.waves == 2)
-    hipLaunchKernelGGL((join_fwd_kernel<R, 2, 1>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((join_fwd_kernel<R, 2, 1, STREAM>), grid, dim3(256), 0, stream, a);
   else if (s.waves == 4)
-    hipLaunchKernelGGL((join_fwd_kernel<R, 4, 1>), grid, dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((join_fwd_kernel<R, 4, 1, STREAM>), grid, dim3(256), 0, stream, a);
   else if (s.waves == 8 && s.pieces == 1)
-    hipLaunchKernelGGL((join_fwd_kernel<R, 8, 1>), grid, dim3(512), 0, stream, a);
+    hipLaunchKernelGGL((join_fwd_kernel<R, 8, 1, STREAM>), grid, dim3(512), 0, stream, a);
   else if (s.waves == 8)
-    hipLaunchKernelGGL((join_fwd_kernel<R, 8, 2>), grid, dim3(512), 0, stream, a);
+    hipLaunchKernelGGL((join_fwd_kernel<R, 8, 2, STREAM>), grid, dim3(512), 0, stream, a);
   else
     hipLaunchKernelGGL((join_fwd_wide_kernel<R>), grid, dim3(256), 0, stream, a);
 }
 
-template <class R>
+template <class R, bool STREAM>
 void launch_bwd(const NormJoinArgs& a, float* part, hipStream_t stream) {
   const dim3 grid((unsigned)bwd_grid(a.T, a.d, a.res_f32));
   const RowShape s = row_shape(a.d);
   const size_t lds = part ? (size_t)(2 * a.d) * sizeof(float) : 0;   // (where a workgroup takes several rows)
   if (s.waves == 1)
-    hipLaunchKernelGGL((join_bwd_kernel<R, 1, 1>), grid, dim3(256), lds, stream, a, part);
+    hipLaunchKernelGGL((join_bwd_kernel<R, 1, 1, STREAM>), grid, dim3(256), lds, stream, a, part);
   else if (s.waves == 2)
-    hipLaunchKernelGGL((join_bwd_kernel<R, 2, 1>), grid, dim3(256), lds, stream, a, part);
+    hipLaunchKernelGGL((join_bwd_kernel<R, 2, 1, STREAM>), grid, dim3(256), lds, stream, a, part);
   else if (s.waves == 4)
-    hipLaunchKernelGGL((join_bwd_kernel<R, 4, 1>), grid, dim3(256), 0, stream, a, part);
+    hipLaunchKernelGGL((join_bwd_kernel<R, 4, 1, STREAM>), grid, dim3(256), 0, stream, a, part);
   else if (s.waves == 8 && s.pieces == 1)
-    hipLaunchKernelGGL((join_bwd_kernel<R, 8, 1>), grid, dim3(512), 0, stream, a, part);
+    hipLaunchKernelGGL((join_bwd_kernel<R, 8, 1, STREAM>), grid, dim3(512), 0, stream, a, part);
   else if (s.waves == 8)
-    hipLaunchKernelGGL((join_bwd_kernel<R, 8, 2>), grid, dim3(512), 0, stream, a, part);
+    hipLaunchKernelGGL((join_bwd_kernel<R, 8, 2, STREAM>), grid, dim3(512), 0, stream, a, part);
   else
     hipLaunchKernelGGL((join_bwd_wide_kernel<R>), grid, dim3(256), 0, stream, a, part);
 }
@@ -563,10 +580,11 @@ size_t norm_join_bwd_workspace_bytes(int64_t T, int64_t d, bool res_f32) {
 
 hipError_t run_norm_join_fwd(const NormJoinArgs& a, hipStream_t stream) {
   TimedLaunch tl("norm_join_fwd", stream);
+  const bool streams = a.T * a.d >= kStreamStores;
   if (a.res_f32)
-    launch_fwd<float>(a, stream);
+    streams ? launch_fwd<float, true>(a, stream) : launch_fwd<float, false>(a, stream);
   else
-    launch_fwd<uint16_t>(a, stream);
+    streams ? launch_fwd<uint16_t, true>(a, stream) : launch_fwd<uint16_t, false>(a, stream);
   return hipGetLastError();
 }
 
@@ -575,10 +593,14 @@ hipError_t run_norm_join_bwd(const NormJoinArgs& a, hipStream_t stream) {
   float* part = first || second ? (float*)a.ws : nullptr;
   {
     TimedLaunch tl("norm_join_bwd", stream);
+    // bytes of the rows read and written
+    const int64_t res = a.res_f32 ? 4 : 2, per = (a.dh_out ? res : 0) + (a.dh ? res : 0) + (a.w_pre ? 2 + res : 0) + (a.b ? 4 : 0) +
+                                                 (a.gate_token ? 4 : 0);
+    const bool streams = a.T * a.d * per >= kStreamLoads;
     if (a.res_f32)
-      launch_bwd<float>(a, part, stream);
+      streams ? launch_bwd<float, true>(a, part, stream) : launch_bwd<float, false>(a, part, stream);
     else
-      launch_bwd<uint16_t>(a, part, stream);
+      streams ? launch_bwd<uint16_t, true>(a, part, stream) : launch_bwd<uint16_t, false>(a, part, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !part) return e;
   }

@@ -21,6 +21,14 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
   v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
 }
+// STREAM: data that no cache is to keep (non-temporal).
+template <bool STREAM, class V>
+__device__ __forceinline__ void store_as(V* p, V v) {
+  if constexpr (STREAM)
+    __builtin_nontemporal_store(v, p);
+  else
+    *p = v;
+}
 __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
   *(uint4*)p = make_uint4(bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3]), bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7]));
 }
@@ -28,6 +36,19 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
   *(float4*)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
 }
+template <bool STREAM, class V>
+__device__ __forceinline__ V load_as(const V* p) {
+  if constexpr (STREAM)
+    return __builtin_nontemporal_load(p);
+  else
+    return *p;
+}
+
+// Non-temporal outputs from this many values on: the outputs of anything larger than a
+// decode step go past the caches (norm join forward: 8192 tokens of 1B 29.2 -> 23.2 us,
+// 60011 of 350M 109 -> 104; the product that reads them next is as fast or faster), a
+// decode step's stay in L2 for the kernel that follows.
+constexpr int64_t kStreamStores = int64_t(1) << 20;
 
 // (a function: a bit cast of a vector's element itself reads element 0)
 __device__ __forceinline__ float as_float(uint32_t w) { return __builtin_bit_cast(float, w); }
@@ -56,28 +77,64 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
-// 8 consecutive values as they were loaded.
-template <class R>
+// A lane's 8 of the 512 features that a wave takes of a row, as they were loaded.  The
+// 8 are consecutive, or, SPLIT, 4 at 4 lane and 4 at 256 + 4 lane: then every access of a
+// wave is contiguous in float32 too, which non-temporal stores need (65536 x 512 float32
+// values: 28 us plain, 55 us non-temporal with consecutive 8).
+template <class T, bool SPLIT>
 struct Piece;
+
 template <>
-struct Piece<uint16_t> {
-  uint4 q;
-  __device__ __forceinline__ void load(const uint16_t* p, bool there) { q = there ? *(const uint4*)p : make_uint4(0u, 0u, 0u, 0u); }
-  __device__ __forceinline__ void get(float (&v)[8]) const { unpack8(q, v); }
-  // A piece that stays the same over a loop: keeps the compiler from holding it as
-  // 8 floats instead of 4 words.
-  __device__ __forceinline__ void keep_packed() { asm volatile("" : "+v"(q.x), "+v"(q.y), "+v"(q.z), "+v"(q.w)); }
+struct Piece<uint16_t, false> {
+  u32x4 q;
+  template <bool STREAM = false>
+  __device__ __forceinline__ void load(const uint16_t* p, bool there, bool) {
+    q = u32x4{0u, 0u, 0u, 0u};
+    if (there) q = load_as<STREAM>((const u32x4*)p);
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const { unpack8(make_uint4(q[0], q[1], q[2], q[3]), v); }
+  template <bool STREAM>
+  static __device__ __forceinline__ void store(uint16_t* p, const float (&v)[8], bool there, bool) {
+    if (there) store_as<STREAM>((u32x4*)p, u32x4{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3]), bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7])});
+  }
+  // Keeps the compiler from holding the piece as 8 floats instead of 4 words from here on.
+  __device__ __forceinline__ void keep_packed() { asm volatile("" : "+v"(q)); }
 };
 template <>
-struct Piece<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float* p, bool there) {
-    a = there ? *(const float4*)p : make_float4(0.f, 0.f, 0.f, 0.f);
-    b = there ? *(const float4*)(p + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+struct Piece<uint16_t, true> {
+  u32x2 a, b;
+  template <bool STREAM = false>
+  __device__ __forceinline__ void load(const uint16_t* p, bool there, bool there2) {
+    a = b = u32x2{0u, 0u};
+    if (there) a = load_as<STREAM>((const u32x2*)p);
+    if (there2) b = load_as<STREAM>((const u32x2*)(p + 256));
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const { unpack8(make_uint4(a[0], a[1], b[0], b[1]), v); }
+  template <bool STREAM>
+  static __device__ __forceinline__ void store(uint16_t* p, const float (&v)[8], bool there, bool there2) {
+    if (there) store_as<STREAM>((u32x2*)p, u32x2{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])});
+    if (there2) store_as<STREAM>((u32x2*)(p + 256), u32x2{bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7])});
+  }
+  __device__ __forceinline__ void keep_packed() { asm volatile("" : "+v"(a), "+v"(b)); }
+};
+template <bool SPLIT>
+struct Piece<float, SPLIT> {
+  static constexpr int SECOND = SPLIT ? 256 : 4;
+  f32x4 a, b;
+  template <bool STREAM = false>
+  __device__ __forceinline__ void load(const float* p, bool there, bool there2) {
+    a = b = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (there) a = load_as<STREAM>((const f32x4*)p);
+    if (there2) b = load_as<STREAM>((const f32x4*)(p + SECOND));
   }
   __device__ __forceinline__ void get(float (&v)[8]) const {
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+  }
+  template <bool STREAM>
+  static __device__ __forceinline__ void store(float* p, const float (&v)[8], bool there, bool there2) {
+    if (there) store_as<STREAM>((f32x4*)p, f32x4{v[0], v[1], v[2], v[3]});
+    if (there2) store_as<STREAM>((f32x4*)(p + SECOND), f32x4{v[4], v[5], v[6], v[7]});
   }
   __device__ __forceinline__ void keep_packed() {}
 };

@@ -244,7 +244,7 @@ class ElasTensors:
         self._pointers = (_p * n)()
         self._numel = (_i64 * n)()
         self._dtype = (ctypes.c_int32 * n)()
-        self._seen = None
+        self.layout = self._addresses = None
         self.device = self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
 
     def __len__(self):
@@ -252,17 +252,17 @@ class ElasTensors:
 
     def arrays(self):
         """The host arrays of addresses, lengths and types."""
-        seen = [t.data_ptr() for t in self.tensors], [t.numel() for t in self.tensors]
-        if seen != self._seen:
+        ts = self.tensors
+        addresses, numel = list(map(torch.Tensor.data_ptr, ts)), list(map(torch.Tensor.numel, ts))
+        if addresses != self._addresses or numel != self.layout[0]:
             dev = self.device.index
-            for k, t in enumerate(self.tensors):
+            for k, t in enumerate(ts):
                 if t.dtype != _F32 and t.dtype != _BF16:
                     raise ValueError(f"tensor {k} must be torch.float32 or torch.bfloat16, got {t.dtype}")
                 _arg(t, t.shape, t.dtype, -1 if dev is None else dev, f"tensor {k}")
-                self._dtype[k] = ELAS_GRAD_F32 if t.dtype == _F32 else ELAS_GRAD_BF16
-            self._pointers[:] = seen[0]
-            self._numel[:] = seen[1]
-            self._seen = seen
+            dtype = [ELAS_GRAD_F32 if t.dtype == _F32 else ELAS_GRAD_BF16 for t in ts]
+            self._pointers[:], self._numel[:], self._dtype[:] = addresses, numel, dtype
+            self.layout, self._addresses = (numel, dtype), addresses
         return self._pointers, self._numel, self._dtype
 
 
@@ -300,8 +300,8 @@ def elas_grad_clip(grads, max_norm: float, out=None, stats: torch.Tensor | None 
     out_p = None
     if out is not None:
         out = _tensors(out)
-        out_p, out_numel, out_dtype = out.arrays()
-        if len(out) != len(grads) or out.device != dev or out_numel[:] != numel[:] or out_dtype[:] != dtype[:]:
+        out_p = out.arrays()[0]
+        if out.layout != grads.layout or out.device != dev:
             raise ValueError("out must hold tensors of the same types, lengths and device as grads")
     if stats is None:
         stats = torch.empty(2, dtype=_F32, device=dev)
