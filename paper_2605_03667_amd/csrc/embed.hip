@@ -84,16 +84,20 @@ __device__ __forceinline__ void wave_ranks(const uint32_t (&digit)[E], const boo
   int leader[E];
 #pragma unroll
   for (int r = 0; r < E; ++r) {
-    uint64_t same = __ballot(ok[r]);
-    for (int b = 0; b < bits; ++b) {
-      const bool set = (digit[r] >> b) & 1u;
-      const uint64_t m = __ballot(set);
-      same &= set ? m : ~m;
+    const uint64_t all = __ballot(ok[r]);
+    uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);   // lanes with the same digit
+#pragma unroll
+    for (int b = 0; b < 9; ++b) {
+      if (b >= bits) break;
+      const uint32_t mine = (uint32_t)((int32_t)(digit[r] << (31 - b)) >> 31);   // the lane's bit b, in all bits
+      const uint64_t m = __ballot(mine != 0u);
+      lo &= ~((uint32_t)m ^ mine);
+      hi &= ~((uint32_t)(m >> 32) ^ mine);
     }
-    lower[r] = __popcll(same & ((1ull << lane) - 1));
-    leader[r] = __ffsll((unsigned long long)same) - 1;
+    lower[r] = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0u));
+    leader[r] = lo != 0u ? __ffs(lo) - 1 : 31 + __ffs(hi);
     before[r] = 0;
-    if (ok[r] && lower[r] == 0) before[r] = atomicAdd(&count[digit[r]], (uint32_t)__popcll(same));
+    if (ok[r] && lower[r] == 0) before[r] = atomicAdd(&count[digit[r]], (uint32_t)(__popc(lo) + __popc(hi)));
   }
 #pragma unroll
   for (int r = 0; r < E; ++r) rank[r] = __shfl(before[r], ok[r] ? leader[r] : 0) + lower[r];
@@ -102,12 +106,15 @@ __device__ __forceinline__ void wave_ranks(const uint32_t (&digit)[E], const boo
 // Exclusive prefix sums over `bins` <= 512 values, one per thread 0 .. bins - 1.
 __device__ __forceinline__ uint32_t bin_scan(uint32_t v, int bins, uint32_t* tmp) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // inclusive over the wave: inside the rows of 16 lanes, then row 0 into 1 and 2 into 3,
+  // then the first half into the second
   uint32_t s = v;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const uint32_t o = __shfl_up(s, m);
-    if (lane >= m) s += o;
-  }
+  s += __builtin_amdgcn_update_dpp(0, s, 0x111, 0xF, 0xF, true);    // row_shr:1
+  s += __builtin_amdgcn_update_dpp(0, s, 0x112, 0xF, 0xF, true);    // row_shr:2
+  s += __builtin_amdgcn_update_dpp(0, s, 0x114, 0xF, 0xF, true);    // row_shr:4
+  s += __builtin_amdgcn_update_dpp(0, s, 0x118, 0xF, 0xF, true);    // row_shr:8
+  s += __builtin_amdgcn_update_dpp(0, s, 0x142, 0xA, 0xF, false);   // row_bcast:15
+  s += __builtin_amdgcn_update_dpp(0, s, 0x143, 0xC, 0xF, false);   // row_bcast:31
   if (lane == 63 && wave * 64 < bins) tmp[wave] = s;
   __syncthreads();
   uint32_t before = 0;
@@ -130,11 +137,11 @@ __device__ __forceinline__ uint32_t wave_prefixes(uint32_t* count, int bins) {
   return n;
 }
 
-// Up to 1024 E tokens by one workgroup, all passes in shared memory.  Entries are
-// key << tbits | token.
+// Up to 1024 E tokens by one workgroup, all passes in shared memory: `entries` holds key
+// << tbits | token, sorted.
 template <int E>
-__global__ __launch_bounds__(1024) void embed_sort_kernel(const EmbedArgs a, int passes, int bits, int tbits, uint32_t* key_out, uint32_t* pos_out) {
-  __shared__ uint32_t count[16 * kDigits], base[kDigits], tmp[8], entries[1024 * E];
+__device__ __forceinline__ void sort_in_lds(const EmbedArgs& a, int passes, int bits, int tbits, uint32_t* count, uint32_t* base, uint32_t* tmp,
+                                            uint32_t* entries) {
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int T = (int)a.T, bins = 1 << bits;
   uint32_t e[E], digit[E], rank[E];
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(1024) void embed_sort_kernel(const EmbedArgs a, int
     e[r] = ok[r] ? key_at(a, t) << tbits | (uint32_t)t : 0u;
   }
   for (int p = 0; p < passes; ++p) {
-    for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) count[i] = 0;
+    for (int w = threadIdx.x >> bits; w < 16; w += 1024 >> bits) count[w * kDigits + (threadIdx.x & (bins - 1))] = 0;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < E; ++r) digit[r] = (e[r] >> (tbits + p * bits)) & (uint32_t)(bins - 1);
@@ -160,16 +167,9 @@ __global__ __launch_bounds__(1024) void embed_sort_kernel(const EmbedArgs a, int
     for (int r = 0; r < E; ++r)
       if (ok[r]) entries[base[digit[r]] + count[wave * kDigits + digit[r]] + rank[r]] = e[r];
     __syncthreads();
+    if (p + 1 == passes) break;
 #pragma unroll
     for (int r = 0; r < E; ++r) e[r] = entries[(wave * E + r) * 64 + lane];   // (entries past T: not used)
-  }
-#pragma unroll
-  for (int r = 0; r < E; ++r) {
-    const int i = (int)((wave * E + r) * 64 + lane);
-    if (i < T) {
-      key_out[i] = e[r] >> tbits;
-      pos_out[i] = e[r] & ((1u << tbits) - 1);
-    }
   }
 }
 
@@ -253,8 +253,20 @@ __global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, 
 // Adding, only the tokens form the sequence.
 constexpr int kRowWeight = 2;
 
+// The sorted tokens: in memory, or in a workgroup's shared memory.
+struct MemoryTokens {
+  const uint32_t *keys, *positions;
+  __device__ __forceinline__ uint32_t key(int64_t p) const { return keys[p]; }
+  __device__ __forceinline__ uint32_t pos(int64_t p) const { return positions[p]; }
+};
+struct SharedTokens {
+  const uint32_t* entries;
+  int tbits;
+  __device__ __forceinline__ uint32_t key(int64_t p) const { return entries[(int)p] >> tbits; }
+  __device__ __forceinline__ uint32_t pos(int64_t p) const { return entries[(int)p] & ((1u << tbits) - 1); }
+};
+
 struct SumArgs {
-  const uint32_t *key, *pos;   // sorted
   int64_t chunk;               // length of a chunk
   int chunks, slices;          // slices of 512 features
   float* carry;                // [chunks][d]
@@ -262,13 +274,14 @@ struct SumArgs {
 };
 
 // First p in [0, T) with p + weight key[p] >= at, else T.
-__device__ __forceinline__ int64_t first_at(const uint32_t* key, int64_t T, int weight, int64_t at) {
+template <class Tokens>
+__device__ __forceinline__ int64_t first_at(const Tokens& tokens, int64_t T, int weight, int64_t at) {
   const int lane = threadIdx.x & 63;
   int64_t lo = 0, hi = T;
   while (lo < hi) {
     const int64_t step = (hi - lo + 63) / 64;
     const int64_t p = min(lo + (lane + 1) * step, hi) - 1;   // the last of the lane's share
-    const uint64_t m = __ballot(p + (int64_t)weight * key[p] >= at);
+    const uint64_t m = __ballot(p + (int64_t)weight * tokens.key(p) >= at);
     if (m == 0) return hi;
     const int k = __ffsll((unsigned long long)m) - 1;
     lo += k * step;
@@ -281,15 +294,16 @@ struct Cut {
   int64_t p;    // first token
   uint32_t v;   // first row whose end lies behind the cut
 };
-__device__ __forceinline__ Cut cut_at(const EmbedArgs& a, const uint32_t* key, int64_t at) {
+template <class Tokens>
+__device__ __forceinline__ Cut cut_at(const EmbedArgs& a, const Tokens& tokens, int64_t at) {
   const int lane = threadIdx.x & 63;
   const int weight = a.add ? 0 : kRowWeight;
   const uint32_t V = (uint32_t)a.V;
   Cut c;
-  c.p = a.add ? min(at, a.T) : first_at(key, a.T, weight, at);
+  c.p = a.add ? min(at, a.T) : first_at(tokens, a.T, weight, at);
   // the keys of the 32 tokens before and the 32 from the cut on (outside: none of a token's)
   const int64_t q = c.p - 32 + lane;
-  const uint32_t none = V + 1, k = q >= 0 && q < a.T ? key[q] : none;
+  const uint32_t none = V + 1, k = q >= 0 && q < a.T ? tokens.key(q) : none;
   const uint32_t left = __builtin_amdgcn_readlane(k, 31), right = __builtin_amdgcn_readlane(k, 32);
   if (left == right && right < V) {
     // in the middle of a row.  Of one of 32 tokens or fewer both ends are seen from every
@@ -319,15 +333,15 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-template <class R, bool ADD>
-__global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const SumArgs s) {
-  constexpr int U = ADD ? 4 : sizeof(R) == 2 ? 16 : 8;   // tokens on their way at once
-  __shared__ Cut cuts[5];
+// The tasks (a chunk and a slice each) of a workgroup of WAVES waves, one to a wave; U
+// tokens of a task on their way at once.
+template <class R, bool ADD, int WAVES, int U, class Tokens>
+__device__ __forceinline__ void sum_tasks(const EmbedArgs& a, const SumArgs& s, const Tokens& tokens, Cut (&cuts)[WAVES + 1]) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // the workgroup's 4 tasks lie in at most 4 chunks: their cuts, one to a wave
-  const int64_t task0 = (int64_t)blockIdx.x * 4, chunk0 = task0 / s.slices, last = (task0 + 3) / s.slices + 1;
-  for (int i = wave; chunk0 + i <= last; i += 4) {
-    const Cut c = cut_at(a, s.key, (chunk0 + i) * s.chunk);
+  // the tasks lie in at most WAVES chunks: their cuts, one to a wave
+  const int64_t task0 = (int64_t)blockIdx.x * WAVES, chunk0 = task0 / s.slices, last = (task0 + WAVES - 1) / s.slices + 1;
+  for (int i = wave; chunk0 + i <= last; i += WAVES) {
+    const Cut c = cut_at(a, tokens, (chunk0 + i) * s.chunk);
     if (lane == 0) cuts[i] = c;
   }
   __syncthreads();
@@ -353,8 +367,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const
   int64_t p = c0.p;
   for (; p < c1.p; p += 64) {
     const int n = (int)min((int64_t)64, c1.p - p);
-    const uint32_t k = lane < n ? s.key[p + lane] : V, pos = lane < n ? s.pos[p + lane] : 0u;
-    const uint32_t after = ADD && lane < n && p + lane + 1 < a.T ? s.key[p + lane + 1] : V + 1;
+    const uint32_t k = lane < n ? tokens.key(p + lane) : V, pos = lane < n ? tokens.pos(p + lane) : 0u;
+    const uint32_t after = ADD && lane < n && p + lane + 1 < a.T ? tokens.key(p + lane + 1) : V + 1;
     for (int j = 0; j < n; j += U) {
       Piece<R, true> x[U];
       Piece<float, true> old[ADD ? U : 1];
@@ -393,6 +407,22 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const
     Piece<float, true>::store<false>((s.carry + chunk * a.d) + c, acc, there, there2);
   }
   if (slice == 0 && lane == 0) s.carry_row[chunk] = open ? row : ~0u;
+}
+
+template <class R, bool ADD>
+__global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const SumArgs s, const MemoryTokens tokens) {
+  __shared__ Cut cuts[5];
+  sum_tasks<R, ADD, 4, ADD ? 4 : sizeof(R) == 2 ? 16 : 8>(a, s, tokens, cuts);
+}
+
+// Few tokens: every workgroup sorts them for itself, in shared memory, and goes on with
+// its tasks; one launch less, and the cuts are found in shared memory.
+template <class R, bool ADD, int E>
+__global__ __launch_bounds__(1024) void embed_few_kernel(const EmbedArgs a, const SumArgs s, int passes, int bits, int tbits) {
+  __shared__ uint32_t count[16 * kDigits], base[kDigits], tmp[8], entries[1024 * E];
+  __shared__ Cut cuts[17];
+  sort_in_lds<E>(a, passes, bits, tbits, count, base, tmp, entries);
+  sum_tasks<R, ADD, 16, ADD ? 4 : 8>(a, s, SharedTokens{entries, tbits}, cuts);
 }
 
 // Adds the sums of the chunks that left a row open, in their order, to the row.  A
@@ -450,7 +480,7 @@ int bit_length(int64_t v) {
 // Sort and cuts of one call, and its regions of the workspace.
 struct Plan {
   int passes, bits, tbits;
-  bool one_group;      // sorted by one workgroup
+  bool few;            // sorted by every workgroup for itself
   int per_thread;      // tokens of a thread in a pass
   int groups;
   SumArgs sum;
@@ -463,13 +493,14 @@ Plan plan(void* ws, int64_t T, int64_t V, int64_t d, bool add) {
   p.passes = (key_bits + 8) / 9;
   p.bits = (key_bits + p.passes - 1) / p.passes;
   p.tbits = std::max(1, bit_length(T - 1));
-  p.one_group = T <= 4096 && key_bits + p.tbits <= 32;
-  p.per_thread = p.one_group ? (T <= 1024 ? 1 : 4) : T <= 131072 ? 1 : T <= (1 << 18) ? 4 : 8;
+  p.few = T <= 4096 && key_bits + p.tbits <= 32;
+  p.per_thread = p.few ? (T <= 1024 ? 1 : T <= 2048 ? 2 : 4) : T <= 131072 ? 1 : T <= (1 << 18) ? 4 : 8;
   p.groups = (int)cdiv(T, 1024 * p.per_thread);
   p.sum.slices = (int)cdiv(d, 512);
-  // about 8 waves to a SIMD, and not under a few tokens or rows to a chunk
+  // about 8 waves to a SIMD, or 4 where they sort first, and not under a few tokens or
+  // rows to a chunk
   const int64_t length = add ? T : T + kRowWeight * V;
-  p.sum.chunk = std::max<int64_t>(add ? 4 : 16, cdiv(length * p.sum.slices, 8192));
+  p.sum.chunk = std::max<int64_t>(add ? 4 : 16, cdiv(length * p.sum.slices, p.few ? 4096 : 8192));
   p.sum.chunks = (int)cdiv(length, p.sum.chunk);
   size_t used = 0;
   auto take = [&](size_t n) {
@@ -477,11 +508,11 @@ Plan plan(void* ws, int64_t T, int64_t V, int64_t d, bool add) {
     used += (n * sizeof(uint32_t) + 255) / 256 * 256;
     return r;
   };
-  for (int i = 0; i < (p.one_group || p.passes == 1 ? 1 : 2); ++i) {
+  for (int i = 0; i < (p.few ? 0 : p.passes == 1 ? 1 : 2); ++i) {
     p.key[i] = take((size_t)T);
     p.pos[i] = take((size_t)T);
   }
-  if (!p.one_group) p.hist = take((size_t)p.groups << p.bits);
+  if (!p.few) p.hist = take((size_t)p.groups << p.bits);
   p.sum.carry_row = take((size_t)p.sum.chunks);
   p.sum.carry = (float*)take((size_t)(p.sum.chunks * d));
   p.bytes = used;
@@ -508,24 +539,27 @@ hipError_t sort_passes(const EmbedArgs& a, const Plan& p, int& at, hipStream_t s
   return hipSuccess;
 }
 
-template <int E>
-void sort_one_group(const EmbedArgs& a, const Plan& p, hipStream_t stream) {
-  TimedLaunch tl("embed_bwd_sort", stream);
-  hipLaunchKernelGGL(embed_sort_kernel<E>, dim3(1), dim3(1024), 0, stream, a, p.passes, p.bits, p.tbits, p.key[0], p.pos[0]);
-}
-
 template <class R, bool STREAM>
 void launch_fwd(const EmbedArgs& a, uint32_t parts, unsigned grid, hipStream_t stream) {
   hipLaunchKernelGGL((embed_fwd_kernel<R, STREAM>), dim3(grid), dim3(256), 0, stream, a, parts);
 }
 
 template <class R>
-void launch_sum(const EmbedArgs& a, const SumArgs& s, hipStream_t stream) {
+void launch_sum(const EmbedArgs& a, const SumArgs& s, const MemoryTokens& tokens, hipStream_t stream) {
   const dim3 grid((unsigned)cdiv((int64_t)s.chunks * s.slices, 4));
   if (a.add)
-    hipLaunchKernelGGL((embed_sum_kernel<R, true>), grid, dim3(256), 0, stream, a, s);
+    hipLaunchKernelGGL((embed_sum_kernel<R, true>), grid, dim3(256), 0, stream, a, s, tokens);
   else
-    hipLaunchKernelGGL((embed_sum_kernel<R, false>), grid, dim3(256), 0, stream, a, s);
+    hipLaunchKernelGGL((embed_sum_kernel<R, false>), grid, dim3(256), 0, stream, a, s, tokens);
+}
+
+template <class R, int E>
+void launch_few(const EmbedArgs& a, const Plan& p, hipStream_t stream) {
+  const dim3 grid((unsigned)cdiv((int64_t)p.sum.chunks * p.sum.slices, 16));
+  if (a.add)
+    hipLaunchKernelGGL((embed_few_kernel<R, true, E>), grid, dim3(1024), 0, stream, a, p.sum, p.passes, p.bits, p.tbits);
+  else
+    hipLaunchKernelGGL((embed_few_kernel<R, false, E>), grid, dim3(1024), 0, stream, a, p.sum, p.passes, p.bits, p.tbits);
 }
 
 }  // namespace
@@ -544,32 +578,29 @@ hipError_t run_embed_fwd(const EmbedArgs& a, hipStream_t stream) {
 }
 
 hipError_t run_embed_bwd(const EmbedArgs& a, hipStream_t stream) {
-  Plan p = plan(a.ws, a.T, a.V, a.d, a.add);
+  const Plan p = plan(a.ws, a.T, a.V, a.d, a.add);
   int at = 0;
-  if (a.T > 0) {
-    hipError_t e = hipSuccess;
-    if (!p.one_group)
-      e = p.per_thread == 1   ? sort_passes<1>(a, p, at, stream)
-          : p.per_thread == 4 ? sort_passes<4>(a, p, at, stream)
-                              : sort_passes<8>(a, p, at, stream);
-    else if (p.per_thread == 1)
-      sort_one_group<1>(a, p, stream);
-    else
-      sort_one_group<4>(a, p, stream);
-    if (e == hipSuccess) e = hipGetLastError();
+  if (!p.few) {
+    const hipError_t e = p.per_thread == 1   ? sort_passes<1>(a, p, at, stream)
+                         : p.per_thread == 4 ? sort_passes<4>(a, p, at, stream)
+                                             : sort_passes<8>(a, p, at, stream);
     if (e != hipSuccess) return e;
   }
-  p.sum.key = p.key[at];
-  p.sum.pos = p.pos[at];
   {
     TimedLaunch tl("embed_bwd_sum", stream);
-    if (a.res_f32)
-      launch_sum<float>(a, p.sum, stream);
+    const MemoryTokens tokens{p.key[at], p.pos[at]};
+    if (!p.few)
+      a.res_f32 ? launch_sum<float>(a, p.sum, tokens, stream) : launch_sum<uint16_t>(a, p.sum, tokens, stream);
+    else if (p.per_thread == 1)
+      a.res_f32 ? launch_few<float, 1>(a, p, stream) : launch_few<uint16_t, 1>(a, p, stream);
+    else if (p.per_thread == 2)
+      a.res_f32 ? launch_few<float, 2>(a, p, stream) : launch_few<uint16_t, 2>(a, p, stream);
     else
-      launch_sum<uint16_t>(a, p.sum, stream);
+      a.res_f32 ? launch_few<float, 4>(a, p, stream) : launch_few<uint16_t, 4>(a, p, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
+  if (a.T <= 32) return hipSuccess;   // no row is cut
   TimedLaunch tl("embed_bwd_join", stream);
   hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)p.sum.chunks, (unsigned)cdiv(a.d, 1024)), dim3(1024), 0, stream, a, p.sum);
   return hipGetLastError();
