@@ -168,9 +168,10 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_bwd_kernel(const No
   }
   for (int64_t t0 = (int64_t)blockIdx.x * Lanes::ROWS; t0 < a.T; t0 += (int64_t)gridDim.x * Lanes::ROWS) {
     const int64_t t = t0 + l.slot, at = t * a.d;
+    if (W == 1 && t >= a.T) break;
+    const bool live = t < a.T;   // (rows past the end are zeros, with factors 0: they add nothing)
     Piece<R, SPLIT> h[NV], dho[NV];
     Piece<uint16_t, SPLIT> dn[NV], b[NV], gate[NV];
-    const bool live = t < a.T;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       if (a.w_pre) {
@@ -201,7 +202,8 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_bwd_kernel(const No
       }
     }
     if (a.w_pre || a.w_post) row_sums<W>(s, red3);
-    const float sig = 1.f / sqrtf(s[0] * inv_d + a.eps), rho = a.w_post ? 1.f / sqrtf(s[2] * inv_d + a.eps) : 1.f;
+    const float sig = live ? 1.f / sqrtf(s[0] * inv_d + a.eps) : 0.f;
+    const float rho = a.w_post ? (live ? 1.f / sqrtf(s[2] * inv_d + a.eps) : 0.f) : 1.f;
     const float ch = s[1] * sig * inv_d;   // mean of q xh
     float g[NV][8], pb[1] = {0.f};
 #pragma unroll

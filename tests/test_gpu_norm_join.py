@@ -134,6 +134,14 @@ def test_extreme_magnitudes(scale):
     _verify(c, dh, dn, 1.0, scale, 0.0)
 
 
+@pytest.mark.parametrize("T,d", [(1, 512), (3, 512), (21, 768), (1, 1024), (5, 2048), (3, 4096), (1, 8192), (1, 9000)])
+def test_rows_past_the_end_add_nothing(T, d):
+    """eps = 0: a row of zeros has an infinite norm factor, and the rows that a
+    workgroup holds past the last token are such rows."""
+    c, dh, dn = _inputs(T, d, BF, "shared", True, True, 3)
+    _verify(c, dh, dn, 1.0, 0.5, 0.0)
+
+
 def test_zero_rows():
     """A row of zeros has a finite norm factor 1/sqrt(eps)."""
     c, dh, dn = _inputs(9, 512, BF, "token", True, True, 4)
