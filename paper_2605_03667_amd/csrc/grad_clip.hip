@@ -162,10 +162,17 @@ __global__ __launch_bounds__(256) void grad_square_kernel(const GradTable g, uin
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
-// Norm from the partial sums, in the same order in every workgroup.
+// Norm from the partial sums, in the same order in every workgroup; 8 loads of a thread
+// on their way at once.
 __device__ __forceinline__ double norm_of(const double* part, int64_t parts, double* red) {
   double s = 0.0;
-  for (int64_t i = threadIdx.x; i < parts; i += 256) s += part[i];
+  for (int64_t i0 = threadIdx.x; i0 < parts; i0 += kGroups) {
+    double v[kGroups / 256];
+#pragma unroll
+    for (int k = 0; k < kGroups / 256; ++k) v[k] = i0 + k * 256 < parts ? part[i0 + k * 256] : 0.0;
+#pragma unroll
+    for (int k = 0; k < kGroups / 256; ++k) s += v[k];
+  }
   return sqrt(block_sum<4>(s, red));
 }
 

@@ -71,10 +71,20 @@ __device__ __forceinline__ float wave_sum(float v) {
   const auto s32 = __builtin_amdgcn_permlane32_swap(x, x, false, false);
   return as_float(s32[0]) + as_float(s32[1]);
 }
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)w, CTRL, 0xF, 0xF, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(w >> 32), CTRL, 0xF, 0xF, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
-  return v;
+  v += dpp<0xB1>(v);
+  v += dpp<0x4E>(v);
+  v += dpp<0x141>(v);
+  v += dpp<0x140>(v);
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
 }
 
 // A lane's 8 of the 512 features that a wave takes of a row, as they were loaded.  The
