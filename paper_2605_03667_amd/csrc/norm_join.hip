@@ -10,11 +10,24 @@ namespace elas {
 namespace {
 
 // ---- rows of up to 512 W NV features, W waves to a row -----------------------------
-// The row stays in registers: NV times 8 features to a lane.  Every operand is read once
-// and the row's sums need no second pass; what bounds the kernels is HBM.  More waves to
-// a row rather than more pieces to a lane (NV = 1 up to 4096 features): 1B backward, 65536
-// tokens: W = 4, NV = 1 315 us, W = 2, NV = 2 385 (it fills the registers, and fewer
-// waves are left to cover the loads).
+// The row stays in registers, NV times 8 features to a lane: every operand is read once
+// and every output written once, the row's means need no second pass, and what bounds
+// the kernels is HBM.  Forward: two sums over the row (of b^2, then of h'^2) and one
+// pass.  Backward: the three sums that need no other (of h'^2, q h' and b^2) together,
+// then that of p bh; the statistics are computed anew rather than kept by the forward,
+// as the row is at hand and its gradient is then that of the formula at the stored h'.
+// The sums over the tokens stay in registers over all rows of a workgroup; a second,
+// small launch adds up the workgroups' rows of them in a fixed order.
+//
+// W waves to a row rather than more pieces to a lane (NV = 1 up to 4096 features): 1B
+// backward, 65536 tokens: W = 4, NV = 1 315 us; W = 2, NV = 2 385 (it fills the registers,
+// and fewer waves are left to cover the loads).  For the same reason pieces stay packed
+// between their uses (344 -> 315) and gains are read once per workgroup.
+//
+// Measured, bytes that the call cannot do without over its time: forward 1B, 65536 tokens,
+// float32 stream 264 us (6.1 TB/s; a copy of 1 GiB reaches 5.5); 350M, 2000 tokens 6.3 us
+// of kernel; 1B, 16 tokens 3.6.  Backward 1B, 65536 tokens 303 us (5.3 TB/s); 350M, 16381
+// tokens, gate per token, float32 stream 66 us (5.6); 60M, 2048 tokens 5.0 + 3.7 us.
 
 // Where a thread's row and pieces lie; loads and stores of piece v.
 template <int W, int NV, bool SPLIT>
@@ -341,7 +354,8 @@ __global__ __launch_bounds__(256) void join_reduce_kernel(const NormJoinArgs a, 
 }
 
 // ---- wider rows -------------------------------------------------------------------
-// One workgroup per row; the row is read again where a sum over it is needed first.
+// One workgroup per row; the row is read again (from L2) where a sum over it is needed
+// first (16384 features, 8192 rows, bf16: 304 us forward, 811 backward).
 
 // 8 features of the operands at column c of row t (absent: zeros, or ones for factors).
 template <class R>
@@ -521,21 +535,23 @@ int64_t row_groups(int64_t T, int64_t d) {   // workgroups, at one row (or set o
   const int w = row_shape(d).waves, rows = w == 1 ? 4 : w == 2 ? 2 : 1;
   return (T + rows - 1) / rows;
 }
-// Forward: a workgroup per row or set of rows (1B, 65536 tokens, float32 stream: 269 us,
-// with 2048 workgroups that go on to further rows 312).  Backward: each workgroup leaves
-// a row of partial sums, so as many as the card holds at once at most: 4 to a CU, or 2
-// where a float32 stream has twice the bytes in flight for each (1B, 65536 tokens, bf16:
-// 331 us with 512, 315 with 1024, 325 with 2048; 32768 tokens, float32: 267, 287, 294).
+// Forward: a workgroup per row or set of rows (1B, 65536 tokens, float32 stream: 269 us;
+// 2048 workgroups that go on to further rows 312).  Backward: each workgroup leaves a row
+// of partial sums, so no more than the card holds at once, 4 waves to a SIMD, or 2 where a
+// float32 stream has twice the bytes in flight for each (1B, 65536 tokens, bf16: 331 us
+// with 512 workgroups, 315 with 1024, 325 with 2048; 32768 tokens, float32: 267, 287, 294;
+// rows of 4096, bf16: 347 us with 256 workgroups of 8 waves, 352 with 512, 360 with 1024).
 int64_t fwd_grid(int64_t T, int64_t d) { return std::min<int64_t>(row_groups(T, d), 1 << 20); }
 int64_t bwd_grid(int64_t T, int64_t d, bool res_f32) {
-  return std::max<int64_t>(1, std::min<int64_t>(row_groups(T, d), res_f32 ? 512 : 1024));
+  const int waves = row_shape(d).waves == 8 ? 8 : 4;
+  return std::max<int64_t>(1, std::min<int64_t>(row_groups(T, d), (res_f32 ? 2048 : 4096) / waves));
 }
 
 // Backward loads go past the caches where the call moves more than the last-level
 // cache's 256 MB (1B, 65536 tokens 316 -> 306 us); in a smaller one they would miss what
 // that cache holds (350M, 8192 tokens 24.8 -> 30.3).  Forward loads never gained (1B 280
 // -> 288).  Stores: kStreamStores in the forward, always in the backward.
-constexpr int64_t kStreamLoads = int64_t(1) << 28;    // bytes
+constexpr int64_t kStreamLoads = int64_t(1) << 28;   // bytes
 
 template <class R, bool STREAM>
 void launch_fwd(const NormJoinArgs& a, hipStream_t stream) {
