@@ -271,20 +271,20 @@ struct SharedTokens {
 
 struct SumArgs {
   int64_t chunk;               // length of a chunk
-  int chunks, slices;          // slices of 512 features
+  int chunks, slices;          // slices of 512 features (few tokens: of a workgroup)
   float* carry;                // [chunks][d]
   uint32_t* carry_row;         // [chunks]; ~0: none
 };
 
-// First p in [0, T) with p + weight key[p] >= at, else T.
-template <class Tokens>
-__device__ __forceinline__ int64_t first_at(const Tokens& tokens, int64_t T, int weight, int64_t at) {
+// First p in [0, T) from which on `holds` is true, else T; a wave probes 64 places at once.
+template <class F>
+__device__ __forceinline__ int64_t first_where(int64_t T, const F& holds) {
   const int lane = threadIdx.x & 63;
   int64_t lo = 0, hi = T;
   while (lo < hi) {
     const int64_t step = (hi - lo + 63) / 64;
     const int64_t p = min(lo + (lane + 1) * step, hi) - 1;   // the last of the lane's share
-    const uint64_t m = __ballot(p + (int64_t)weight * tokens.key(p) >= at);
+    const uint64_t m = __ballot(holds(p));
     if (m == 0) return hi;
     const int k = __ffsll((unsigned long long)m) - 1;
     lo += k * step;
@@ -294,32 +294,37 @@ __device__ __forceinline__ int64_t first_at(const Tokens& tokens, int64_t T, int
 }
 
 struct Cut {
-  int64_t p;    // first token
-  uint32_t v;   // first row whose end lies behind the cut
+  int64_t p;      // first token
+  uint32_t v;     // first row whose end lies behind the cut
+  uint32_t mid;   // whether the cut is inside row v, with tokens of it on both sides
 };
+// whole: a cut is moved behind the row it falls into, however long that is.
 template <class Tokens>
-__device__ __forceinline__ Cut cut_at(const EmbedArgs& a, const Tokens& tokens, int64_t at) {
+__device__ __forceinline__ Cut cut_at(const EmbedArgs& a, const Tokens& tokens, int64_t at, bool whole) {
   const int lane = threadIdx.x & 63;
   const int weight = a.add ? 0 : kRowWeight;
   const uint32_t V = (uint32_t)a.V;
-  Cut c;
-  c.p = a.add ? min(at, a.T) : first_at(tokens, a.T, weight, at);
+  Cut c{};
+  c.p = a.add ? min(at, a.T) : first_where(a.T, [&](int64_t p) { return p + (int64_t)weight * tokens.key(p) >= at; });
   // the keys of the 32 tokens before and the 32 from the cut on (outside: none of a token's)
   const int64_t q = c.p - 32 + lane;
   const uint32_t none = V + 1, k = q >= 0 && q < a.T ? tokens.key(q) : none;
   const uint32_t left = __builtin_amdgcn_readlane(k, 31), right = __builtin_amdgcn_readlane(k, 32);
   if (left == right && right < V) {
     // in the middle of a row.  Of one of 32 tokens or fewer both ends are seen from every
-    // cut, so that all its cuts are moved; of a longer one none is.
+    // cut, so that all its cuts are moved; of a longer one all are, or none is.
     const uint64_t other = __ballot(k != right);
     const uint32_t below = (uint32_t)other, above = (uint32_t)(other >> 32);
-    c.v = right;
-    if (below != 0 && above != 0) {
-      const int rest = __ffs(above) - 1;
-      if (__clz(below) + rest <= 32) {
-        c.p += rest;
-        c.v = right + 1;
-      }
+    const int rest = __ffs(above) - 1;
+    if (below != 0 && above != 0 && __clz(below) + rest <= 32) {
+      c.p += rest;
+      c.v = right + 1;
+    } else if (whole) {
+      c.p = first_where(a.T, [&](int64_t p) { return tokens.key(p) > right; });
+      c.v = right + 1;
+    } else {
+      c.v = right;
+      c.mid = 1;
     }
     return c;
   }
@@ -336,39 +341,47 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-// The tasks (a chunk and a slice each) of a workgroup of WAVES waves, one to a wave; U
-// tokens of a task on their way at once.
-template <class R, bool ADD, int WAVES, int U, class Tokens>
-__device__ __forceinline__ void sum_tasks(const EmbedArgs& a, const SumArgs& s, const Tokens& tokens, Cut (&cuts)[WAVES + 1]) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // the tasks lie in at most WAVES chunks: their cuts, one to a wave
-  const int64_t task0 = (int64_t)blockIdx.x * WAVES, chunk0 = task0 / s.slices, last = (task0 + WAVES - 1) / s.slices + 1;
-  for (int i = wave; chunk0 + i <= last; i += WAVES) {
-    const Cut c = cut_at(a, tokens, (chunk0 + i) * s.chunk);
-    if (lane == 0) cuts[i] = c;
+// A lane's features of a slice.
+struct Columns {
+  uint32_t c;
+  bool there, there2;
+  __device__ __forceinline__ Columns(const EmbedArgs& a, int slice) {
+    c = (uint32_t)slice * 512 + (threadIdx.x & 63) * 4;
+    there = c < (uint32_t)a.d;
+    there2 = c + 256 < (uint32_t)a.d;
   }
-  __syncthreads();
-  const int64_t task = task0 + wave, chunk = task / s.slices;
-  if (chunk >= s.chunks) return;   // (no barriers below)
-  const int slice = (int)(task - chunk * s.slices);
-  const uint32_t c = (uint32_t)slice * 512 + lane * 4;
-  const bool there = c < (uint32_t)a.d, there2 = c + 256 < (uint32_t)a.d;
-  const int i0 = (int)(chunk - chunk0);
-  const Cut c0 = {uniform(cuts[i0].p), (uint32_t)uniform(cuts[i0].v)}, c1 = {uniform(cuts[i0 + 1].p), (uint32_t)uniform(cuts[i0 + 1].v)};
+};
+
+// What a wave is left with behind its range: the sum over the row that the range's end
+// cuts, and (HOLD, a range that begins inside a row) that over the rest of the row which
+// it begins in.
+struct Open {
+  float acc[8] = {}, head[8] = {};
+  uint32_t row;
+  bool open = false;   // whether the row has tokens here
+};
+
+// Sums between two cuts, U tokens on their way at once.
+template <class R, bool ADD, bool HOLD, int U, class Tokens>
+__device__ __forceinline__ Open sum_range(const EmbedArgs& a, const Tokens& tokens, const Cut& c0, const Cut& c1, const Columns& col) {
+  const int lane = threadIdx.x & 63;
   const uint32_t V = (uint32_t)a.V;
-  float acc[8] = {};
-  uint32_t row = c0.v;   // the row being added up
-  bool open = false;     // whether it has tokens here
+  Open o;
+  o.row = c0.v;
   auto store = [&](uint32_t v, const Piece<float, true>& old) __attribute__((always_inline)) {
-    float o[8];
-    if (ADD) old.get(o);
+    if (HOLD && c0.mid && v == c0.v) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = ADD ? fmaf(a.scale, acc[i], o[i]) : a.scale * acc[i], acc[i] = 0.f;
-    Piece<float, true>::store<!ADD>((a.dtable + (int64_t)v * a.d) + c, o, there, there2);
+      for (int i = 0; i < 8; ++i) o.head[i] = o.acc[i], o.acc[i] = 0.f;
+      return;
+    }
+    float x[8];
+    if (ADD) old.get(x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = ADD ? fmaf(a.scale, o.acc[i], x[i]) : a.scale * o.acc[i], o.acc[i] = 0.f;
+    Piece<float, true>::store<!ADD>((a.dtable + (int64_t)v * a.d) + col.c, x, col.there, col.there2);
   };
   const Piece<float, true> nothing = {};
-  int64_t p = c0.p;
-  for (; p < c1.p; p += 64) {
+  for (int64_t p = c0.p; p < c1.p; p += 64) {
     const int n = (int)min((int64_t)64, c1.p - p);
     const uint32_t k = lane < n ? tokens.key(p + lane) : V, pos = lane < n ? tokens.pos(p + lane) : 0u;
     const uint32_t after = ADD && lane < n && p + lane + 1 < a.T ? tokens.key(p + lane + 1) : V + 1;
@@ -380,52 +393,123 @@ __device__ __forceinline__ void sum_tasks(const EmbedArgs& a, const SumArgs& s, 
         const uint32_t ku = __builtin_amdgcn_readlane(k, j + u);   // (past n: V)
         const int64_t t = __builtin_amdgcn_readlane(pos, j + u);
         if (ku >= V) continue;
-        x[u].load(((const R*)a.dx + t * a.d) + c, there, there2);
-        if (ADD && __builtin_amdgcn_readlane(after, j + u) != ku) old[ADD ? u : 0].load((a.dtable + (int64_t)ku * a.d) + c, there, there2);
+        x[u].load(((const R*)a.dx + t * a.d) + col.c, col.there, col.there2);
+        if (ADD && __builtin_amdgcn_readlane(after, j + u) != ku)
+          old[ADD ? u : 0].load((a.dtable + (int64_t)ku * a.d) + col.c, col.there, col.there2);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const uint32_t ku = __builtin_amdgcn_readlane(k, j + u);
         if (ku >= V) continue;
         if (!ADD)
-          for (; row < ku; ++row, open = false) store(row, nothing);
+          for (; o.row < ku; ++o.row, o.open = false) store(o.row, nothing);
         float v[8];
         x[u].get(v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] += v[i];
-        row = ku;
-        open = true;
+        for (int i = 0; i < 8; ++i) o.acc[i] += v[i];
+        o.row = ku;
+        o.open = true;
         if (ADD && __builtin_amdgcn_readlane(after, j + u) != ku) {
           store(ku, old[ADD ? u : 0]);
-          open = false;
+          o.open = false;
         }
       }
     }
   }
   if (!ADD)
-    for (; row < c1.v; ++row, open = false) store(row, nothing);
-  if (open) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] *= a.scale;
-    Piece<float, true>::store<false>((s.carry + chunk * a.d) + c, acc, there, there2);
-  }
-  if (slice == 0 && lane == 0) s.carry_row[chunk] = open ? row : ~0u;
+    for (; o.row < c1.v; ++o.row, o.open = false) store(o.row, nothing);
+  return o;
 }
 
+__device__ __forceinline__ Cut uniform(const Cut& c) { return {uniform(c.p), (uint32_t)uniform(c.v), (uint32_t)uniform(c.mid)}; }
+
+// One task (a chunk and a slice) to a wave.
 template <class R, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const SumArgs s, const MemoryTokens tokens) {
   __shared__ Cut cuts[5];
-  sum_tasks<R, ADD, 4, ADD ? 4 : sizeof(R) == 2 ? 16 : 8>(a, s, tokens, cuts);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // the 4 tasks lie in at most 4 chunks: their cuts, one to a wave
+  const int64_t task0 = (int64_t)blockIdx.x * 4, chunk0 = task0 / s.slices, last = (task0 + 3) / s.slices + 1;
+  for (int i = wave; chunk0 + i <= last; i += 4) {
+    const Cut c = cut_at(a, tokens, (chunk0 + i) * s.chunk, false);
+    if (lane == 0) cuts[i] = c;
+  }
+  __syncthreads();
+  const int64_t task = task0 + wave, chunk = task / s.slices;
+  if (chunk >= s.chunks) return;
+  const int slice = (int)(task - chunk * s.slices), i = (int)(chunk - chunk0);
+  const Columns col(a, slice);
+  Open o = sum_range<R, ADD, false, ADD ? 4 : sizeof(R) == 2 ? 16 : 8>(a, tokens, uniform(cuts[i]), uniform(cuts[i + 1]), col);
+  if (o.open) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o.acc[k] *= a.scale;
+    Piece<float, true>::store<false>((s.carry + chunk * a.d) + col.c, o.acc, col.there, col.there2);
+  }
+  if (slice == 0 && lane == 0) s.carry_row[chunk] = o.open ? o.row : ~0u;
 }
 
-// Few tokens: every workgroup sorts them for itself, in shared memory, and goes on with
-// its tasks; one launch less, and the cuts are found in shared memory.
+// Few tokens: every workgroup sorts them for itself, in shared memory, and takes a chunk
+// of whole rows; its 16 waves take the slices (s.slices of them, 16 at most) of 16 /
+// s.slices equal shares of it each.  Rows cut between shares are joined in shared memory, so
+// that one launch does it all: the wave that ends such a row holds its own part, and adds
+// those of the shares before it in their order.  (60M, 2048 tokens, added: 16.6 us; with
+// the rows joined by embed_join_kernel 18.7; with the sort a launch of its own 23.)
 template <class R, bool ADD, int E>
 __global__ __launch_bounds__(1024) void embed_few_kernel(const EmbedArgs a, const SumArgs s, int passes, int bits, int tbits) {
-  __shared__ uint32_t count[16 * kDigits], base[kDigits], tmp[8], entries[1024 * E];
+  __shared__ __attribute__((aligned(16))) uint32_t count[16 * kDigits];
+  __shared__ uint32_t base[kDigits], tmp[8], entries[1024 * E];
   __shared__ Cut cuts[17];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int shares = 16 / s.slices, share = wave / s.slices;
+  const bool works = share < shares;   // (16 may not be a multiple of the slices)
   sort_in_lds<E>(a, passes, bits, tbits, count, base, tmp, entries);
-  sum_tasks<R, ADD, 16, ADD ? 4 : 8>(a, s, SharedTokens{entries, tbits}, cuts);
+  const SharedTokens tokens{entries, tbits};
+  const Cut first = cut_at(a, tokens, blockIdx.x * s.chunk, true), last = cut_at(a, tokens, (blockIdx.x + 1) * s.chunk, true);
+  if (wave <= shares) {
+    Cut c = wave == 0 ? first : last;
+    if (wave > 0 && wave < shares) {
+      const int weight = ADD ? 0 : kRowWeight;
+      const int64_t at0 = first.p + (int64_t)weight * first.v, at1 = last.p + (int64_t)weight * last.v;
+      c = cut_at(a, tokens, at0 + (at1 - at0) * wave / shares, false);
+      if (c.p < first.p || (c.p == first.p && c.v < first.v)) c = first;
+      if (c.p > last.p || (c.p == last.p && c.v > last.v)) c = last;
+    }
+    if (lane == 0) cuts[wave] = c;
+  }
+  if (shares == 16 && wave == 0 && lane == 0) cuts[16] = last;
+  __syncthreads();
+  const Columns col(a, (int)blockIdx.y * s.slices + wave - share * s.slices);
+  Open o;
+  Cut c0{}, c1{};
+  if (works) {
+    c0 = uniform(cuts[share]), c1 = uniform(cuts[share + 1]);
+    o = sum_range<R, ADD, true, ADD ? 4 : 8>(a, tokens, c0, c1, col);
+  }
+  float(*carry)[512] = (float(*)[512])count;   // (the counters are free)
+  const int l = lane * 4;
+  if (c1.mid) Piece<float, true>::store<false>(carry[wave] + l, o.acc, true, true);
+  __syncthreads();
+  // on with the wave that ends the row its range began in: c1 is not inside the same row
+  if (!c0.mid || (c1.mid && c1.v == c0.v)) return;
+  int i = share - 1;   // the first share with a part of the row
+  while (cuts[i].mid && cuts[i].v == c0.v) --i;
+  float sum[8] = {};
+  for (; i < share; ++i) {
+    Piece<float, true> x;
+    float v[8];
+    x.load(carry[wave - (share - i) * s.slices] + l, true, true);
+    x.get(v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] += v[k];
+  }
+  float* out = (a.dtable + (int64_t)c0.v * a.d) + col.c;
+  Piece<float, true> old;
+  old.load(out, ADD && col.there, ADD && col.there2);
+  float x[8];
+  old.get(x);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x[k] = fmaf(a.scale, sum[k] + o.head[k], x[k]);
+  Piece<float, true>::store<!ADD>(out, x, col.there, col.there2);
 }
 
 // Adds the sums of the chunks that left a row open, in their order, to the row.  A
@@ -486,6 +570,7 @@ struct Plan {
   bool few;            // sorted by every workgroup for itself
   int per_thread;      // tokens of a thread in a pass
   int groups;
+  int slice_groups;    // few: of sum.slices each
   SumArgs sum;
   uint32_t *key[2], *pos[2], *hist;
   size_t bytes;
@@ -500,11 +585,21 @@ Plan plan(void* ws, int64_t T, int64_t V, int64_t d, bool add) {
   p.per_thread = p.few ? (T <= 1024 ? 1 : T <= 2048 ? 2 : 4) : T <= 131072 ? 1 : T <= (1 << 18) ? 4 : 8;
   p.groups = (int)cdiv(T, 1024 * p.per_thread);
   p.sum.slices = (int)cdiv(d, 512);
-  // about 8 waves to a SIMD, or 4 where they sort first, and not under a few tokens or
-  // rows to a chunk
+  // about 8 waves to a SIMD, and not under a few tokens or rows to each; where every
+  // workgroup sorts first, one of 16 waves to a CU
   const int64_t length = add ? T : T + kRowWeight * V;
-  p.sum.chunk = std::max<int64_t>(add ? 4 : 16, cdiv(length * p.sum.slices, p.few ? 4096 : 8192));
-  p.sum.chunks = (int)cdiv(length, p.sum.chunk);
+  const int64_t least = add ? 4 : 16;
+  if (p.few) {
+    // all slices of a row in one workgroup where rows are written (1B, 30 tokens: 56 us, one
+    // slice 61); one slice, and a long row shared by all 16 waves, where tokens are added (1B,
+    // 4096 tokens: 32 and 26)
+    p.slice_groups = add ? p.sum.slices : (int)cdiv(p.sum.slices, 16);
+    p.sum.slices = (int)cdiv(p.sum.slices, p.slice_groups);
+    p.sum.chunk = std::max<int64_t>(16 / p.sum.slices * least, cdiv(length * p.slice_groups, 256));
+  } else {
+    p.sum.chunk = std::max<int64_t>(least, cdiv(length * p.sum.slices, 8192));
+  }
+  p.sum.chunks = (int)std::max<int64_t>(1, cdiv(length, p.sum.chunk));
   size_t used = 0;
   auto take = [&](size_t n) {
     uint32_t* r = ws ? (uint32_t*)((char*)ws + used) : nullptr;
@@ -516,8 +611,10 @@ Plan plan(void* ws, int64_t T, int64_t V, int64_t d, bool add) {
     p.pos[i] = take((size_t)T);
   }
   if (!p.few) p.hist = take((size_t)p.groups << p.bits);
-  p.sum.carry_row = take((size_t)p.sum.chunks);
-  p.sum.carry = (float*)take((size_t)(p.sum.chunks * d));
+  if (!p.few) {
+    p.sum.carry_row = take((size_t)p.sum.chunks);
+    p.sum.carry = (float*)take((size_t)(p.sum.chunks * d));
+  }
   p.bytes = used;
   return p;
 }
@@ -558,7 +655,7 @@ void launch_sum(const EmbedArgs& a, const SumArgs& s, const MemoryTokens& tokens
 
 template <class R, int E>
 void launch_few(const EmbedArgs& a, const Plan& p, hipStream_t stream) {
-  const dim3 grid((unsigned)cdiv((int64_t)p.sum.chunks * p.sum.slices, 16));
+  const dim3 grid((unsigned)p.sum.chunks, (unsigned)p.slice_groups);
   if (a.add)
     hipLaunchKernelGGL((embed_few_kernel<R, true, E>), grid, dim3(1024), 0, stream, a, p.sum, p.passes, p.bits, p.tbits);
   else
@@ -603,7 +700,7 @@ hipError_t run_embed_bwd(const EmbedArgs& a, hipStream_t stream) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.T <= 32) return hipSuccess;   // no row is cut
+  if (p.few) return hipSuccess;
   TimedLaunch tl("embed_bwd_join", stream);
   hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)p.sum.chunks, (unsigned)cdiv(a.d, 1024)), dim3(1024), 0, stream, a, p.sum);
   return hipGetLastError();

@@ -23,7 +23,7 @@ namespace elas {
 
 namespace {
 
-constexpr int kTensors = 128;     // per launch: the table below is a kernel argument (< 4 KB)
+constexpr int kTensors = 128;     // per launch, at most
 constexpr int kPiece = 8192;      // values
 constexpr int kGroups = 2048;     // most workgroups, and partial sums, per launch
 // The squares are read past the caches, except, where there is more than the last-level
@@ -31,13 +31,22 @@ constexpr int kGroups = 2048;     // most workgroups, and partial sums, per laun
 // 512, 64 MB 502, 128 MB 491, 192 MB 498; 152 MB in all: kept 86, not 77).
 constexpr int64_t kCache = int64_t(256) << 20, kKeep = int64_t(128) << 20;
 
-struct GradTable {
-  const void* in[kTensors];
-  void* out[kTensors];
-  int64_t n[kTensors];
-  uint32_t first[kTensors + 1];   // number of each tensor's first piece; [count] = pieces in all
-  uint32_t bf16[kTensors / 32];   // bit k: tensor k is bf16
+// The tensors of a launch, as a kernel argument of room for CAP: what a launch costs the
+// host grows by 0.7 us for each KB of it.
+template <int CAP>
+struct Tensors {
+  const void* in[CAP];
+  uint32_t first[CAP + 1];   // number of each tensor's first piece; [count] = pieces in all
+  uint32_t bf16[CAP / 32];   // bit k: tensor k is bf16
+  uint16_t last[CAP];        // values of its last piece
   int count;
+  __device__ __forceinline__ bool is_bf16(int k) const { return bf16[k >> 5] >> (k & 31) & 1u; }
+  // values of piece c, which is tensor k's
+  __device__ __forceinline__ int values(uint32_t c, int k) const { return c + 1 < first[k + 1] ? kPiece : (int)last[k]; }
+};
+template <int CAP>
+struct Outputs {
+  void* out[CAP];
 };
 
 // (tensors need their element's alignment only: 16-byte accesses at any such address)
@@ -130,29 +139,31 @@ __device__ __forceinline__ void scale_piece(const E* g, E* out, int n, float f) 
 
 // Which tensor a piece belongs to: the last one whose first piece is not behind it.
 // Lane l holds the first pieces of the tensors l and l + 64.
+template <int CAP>
 struct Finder {
-  uint32_t f0, f1;
-  __device__ __forceinline__ explicit Finder(const GradTable& g) {
+  uint32_t f0, f1 = ~0u;
+  __device__ __forceinline__ explicit Finder(const Tensors<CAP>& g) {
     const int lane = threadIdx.x & 63;
     f0 = lane < g.count ? g.first[lane] : ~0u;
-    f1 = lane + 64 < g.count ? g.first[lane + 64] : ~0u;
+    if (CAP > 64) f1 = lane + 64 < g.count ? g.first[lane + 64] : ~0u;
   }
   __device__ __forceinline__ int operator()(uint32_t piece) const {
-    return __popcll(__ballot(f0 <= piece)) + __popcll(__ballot(f1 <= piece)) - 1;
+    return __popcll(__ballot(f0 <= piece)) + (CAP > 64 ? __popcll(__ballot(f1 <= piece)) : 0) - 1;
   }
 };
 
-__global__ __launch_bounds__(256) void grad_square_kernel(const GradTable g, uint32_t keep, double* part) {
+template <int CAP>
+__global__ __launch_bounds__(256) void grad_square_kernel(const Tensors<CAP> g, uint32_t keep, double* part) {
   __shared__ double red[4];
-  const Finder find(g);
+  const Finder<CAP> find(g);
   const uint32_t pieces = g.first[g.count];
   double s[2] = {0.0, 0.0};
   for (uint32_t c = blockIdx.x; c < pieces; c += gridDim.x) {
     const int k = find(c);
     const int64_t at = (int64_t)(c - g.first[k]) * kPiece;
-    const int n = (int)min(g.n[k] - at, (int64_t)kPiece);
+    const int n = g.values(c, k);
     // the last `keep` pieces are left in the caches
-    if (g.bf16[k >> 5] >> (k & 31) & 1u) {
+    if (g.is_bf16(k)) {
       const uint16_t* p = (const uint16_t*)g.in[k] + at;
       c + keep < pieces ? square_piece<true>(p, n, s) : square_piece<false>(p, n, s);
     } else {
@@ -185,9 +196,10 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const double* part, int6
 }
 
 // stats NULL: another launch writes them.
-__global__ __launch_bounds__(256) void grad_scale_kernel(const GradTable g, const double* part, int64_t parts, float max_norm, float* stats) {
+template <int CAP>
+__global__ __launch_bounds__(256) void grad_scale_kernel(const Tensors<CAP> g, const Outputs<CAP> o, const double* part, int64_t parts, float max_norm, float* stats) {
   __shared__ double red[4];
-  const Finder find(g);
+  const Finder<CAP> find(g);
   const double norm = norm_of(part, parts, red);
   const bool finite = norm < (double)INFINITY, clips = finite && norm > (double)max_norm;
   const float factor = clips ? (float)((double)max_norm / norm) : 1.f;
@@ -199,34 +211,50 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(const GradTable g, cons
   for (uint32_t i = blockIdx.x; i < pieces; i += gridDim.x) {
     const uint32_t c = pieces - 1 - i;
     const int k = find(c);
-    if (!clips && g.in[k] == g.out[k]) continue;
+    if (!clips && g.in[k] == o.out[k]) continue;
     const int64_t at = (int64_t)(c - g.first[k]) * kPiece;
-    const int n = (int)min(g.n[k] - at, (int64_t)kPiece);
-    if (g.bf16[k >> 5] >> (k & 31) & 1u)
-      scale_piece((const uint16_t*)g.in[k] + at, (uint16_t*)g.out[k] + at, n, factor);
+    const int n = g.values(c, k);
+    if (g.is_bf16(k))
+      scale_piece((const uint16_t*)g.in[k] + at, (uint16_t*)o.out[k] + at, n, factor);
     else
-      scale_piece((const float*)g.in[k] + at, (float*)g.out[k] + at, n, factor);
+      scale_piece((const float*)g.in[k] + at, (float*)o.out[k] + at, n, factor);
   }
 }
 
-// The table of the tensors k0 .. of one launch (empty ones take no piece).
-void fill(GradTable& g, const void* const* in, void* const* out, const int64_t* numel, const int32_t* dtype, int64_t k0, int64_t n) {
-  g.count = (int)std::min<int64_t>(kTensors, n - k0);
+// ---- host -----------------------------------------------------------------------------
+
+struct GradCall {
+  const void* const* in;
+  void* const* out;
+  const int64_t* numel;
+  const int32_t* dtype;
+  int64_t n;
+  float max_norm;
+  float* stats;
+  double* part;
+  hipStream_t stream;
+};
+
+// The tensors k0 .. of one launch (empty ones take no piece).
+template <int CAP>
+void fill(Tensors<CAP>& g, const GradCall& c, int64_t k0, int count) {
+  g.count = count;
   uint32_t pieces = 0;
-  for (int k = 0; k < kTensors / 32; ++k) g.bf16[k] = 0;
-  for (int k = 0; k < g.count; ++k) {
-    g.in[k] = in[k0 + k];
-    g.out[k] = out ? out[k0 + k] : nullptr;
-    g.n[k] = numel[k0 + k];
+  for (int k = 0; k < CAP / 32; ++k) g.bf16[k] = 0;
+  for (int k = 0; k < count; ++k) {
+    const int64_t n = c.numel[k0 + k], of = (n + kPiece - 1) / kPiece;
+    g.in[k] = c.in[k0 + k];
     g.first[k] = pieces;
-    pieces += (uint32_t)((g.n[k] + kPiece - 1) / kPiece);
-    if (dtype[k0 + k] == ELAS_GRAD_BF16) g.bf16[k >> 5] |= 1u << (k & 31);
+    g.last[k] = (uint16_t)(n - (of - 1) * kPiece);
+    pieces += (uint32_t)of;
+    if (c.dtype[k0 + k] == ELAS_GRAD_BF16) g.bf16[k >> 5] |= 1u << (k & 31);
   }
-  g.first[g.count] = pieces;
+  g.first[count] = pieces;
 }
 
-// Pieces at the end of the launch that make up the last `bytes` of it; what is left of them.
-uint32_t last_pieces(const GradTable& g, int64_t& bytes) {
+// Pieces at the end of the launch that make up the last `bytes` of it.
+template <int CAP>
+uint32_t last_pieces(const Tensors<CAP>& g, int64_t bytes) {
   uint32_t pieces = 0;
   for (int k = g.count - 1; k >= 0 && bytes > 0; --k) {
     const int64_t piece = kPiece * ((g.bf16[k >> 5] >> (k & 31) & 1u) ? 2 : 4), all = g.first[k + 1] - g.first[k];
@@ -237,6 +265,30 @@ uint32_t last_pieces(const GradTable& g, int64_t& bytes) {
   return pieces;
 }
 
+// One launch over the tensors k0 .. k0 + count; adds its partial sums to `parts`.
+template <int CAP>
+hipError_t launch_square(const GradCall& c, int64_t k0, int count, int64_t keep, int64_t& parts) {
+  Tensors<CAP> g;
+  fill(g, c, k0, count);
+  const unsigned groups = std::min<uint32_t>(g.first[count], kGroups);
+  if (groups == 0) return hipSuccess;
+  TimedLaunch tl("grad_square", c.stream);
+  hipLaunchKernelGGL(grad_square_kernel<CAP>, dim3(groups), dim3(256), 0, c.stream, g, last_pieces(g, keep), c.part + parts);
+  parts += groups;
+  return hipGetLastError();
+}
+template <int CAP>
+hipError_t launch_scale(const GradCall& c, int64_t k0, int count, int64_t parts) {
+  Tensors<CAP> g;
+  fill(g, c, k0, count);
+  Outputs<CAP> o;
+  for (int k = 0; k < count; ++k) o.out[k] = c.out[k0 + k];
+  TimedLaunch tl("grad_scale", c.stream);
+  hipLaunchKernelGGL(grad_scale_kernel<CAP>, dim3(std::max(1u, std::min<uint32_t>(g.first[count], kGroups))), dim3(256), 0, c.stream, g, o,
+                     (const double*)c.part, parts, c.max_norm, k0 == 0 ? c.stats : nullptr);
+  return hipGetLastError();
+}
+
 int64_t launches(int64_t n) { return (n + kTensors - 1) / kTensors; }
 
 }  // namespace
@@ -245,35 +297,30 @@ size_t grad_workspace_bytes(int64_t n) { return (size_t)launches(n) * kGroups * 
 
 hipError_t run_grad_norm(const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype, int64_t n, bool clip,
                          float max_norm, float* stats, void* ws, hipStream_t stream) {
-  double* part = (double*)ws;
+  const GradCall c{grads, out, numel, dtype, n, max_norm, stats, (double*)ws, stream};
   int64_t parts = 0, total = 0;
   for (int64_t k = 0; k < n; ++k) total += numel[k] * (dtype[k] == ELAS_GRAD_BF16 ? 2 : 4);
-  GradTable g;
-  // what the squares leave in the caches: a launch other than the last one keeps nothing
-  int64_t keep = clip && total > kCache ? kKeep : 0;
   for (int64_t k = 0; k < n; k += kTensors) {
-    fill(g, grads, out, numel, dtype, k, n);
-    const uint32_t kept = k + kTensors >= n ? last_pieces(g, keep) : 0;
-    const unsigned groups = std::min<uint32_t>(g.first[g.count], kGroups);
-    if (groups == 0) continue;
-    TimedLaunch tl("grad_square", stream);
-    hipLaunchKernelGGL(grad_square_kernel, dim3(groups), dim3(256), 0, stream, g, kept, part + parts);
-    const hipError_t e = hipGetLastError();
+    const int count = (int)std::min<int64_t>(kTensors, n - k);
+    // (a launch other than the last one leaves nothing in the caches)
+    const int64_t keep = clip && total > kCache && k + kTensors >= n ? kKeep : 0;
+    const hipError_t e = count <= 32   ? launch_square<32>(c, k, count, keep, parts)
+                         : count <= 64 ? launch_square<64>(c, k, count, keep, parts)
+                                       : launch_square<kTensors>(c, k, count, keep, parts);
     if (e != hipSuccess) return e;
-    parts += groups;
   }
   if (!clip) {
     TimedLaunch tl("grad_norm", stream);
-    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, stream, part, parts, stats);
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, stream, (const double*)c.part, parts, stats);
     return hipGetLastError();
   }
   // (one launch at least, which writes the statistics where there are no values)
   for (int64_t l = std::max<int64_t>(launches(n), 1) - 1; l >= 0; --l) {
-    fill(g, grads, out, numel, dtype, l * kTensors, n);
-    TimedLaunch tl("grad_scale", stream);
-    hipLaunchKernelGGL(grad_scale_kernel, dim3(std::max(1u, std::min<uint32_t>(g.first[g.count], kGroups))), dim3(256), 0, stream, g, part,
-                       parts, max_norm, l == 0 ? stats : nullptr);
-    const hipError_t e = hipGetLastError();
+    const int64_t k = l * kTensors;
+    const int count = (int)std::min<int64_t>(kTensors, n - k);
+    const hipError_t e = count <= 32   ? launch_scale<32>(c, k, count, parts)
+                         : count <= 64 ? launch_scale<64>(c, k, count, parts)
+                                       : launch_scale<kTensors>(c, k, count, parts);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

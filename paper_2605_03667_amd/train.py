@@ -9,6 +9,7 @@ not passed in, and take the current stream.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -128,6 +129,7 @@ def elas_norm_join_fwd(h, b=None, gate=None, w_post=None, w_pre=None, res_scale:
     return out
 
 
+@functools.lru_cache(maxsize=1024)   # (of the sizes alone)
 def elas_norm_join_bwd_workspace_bytes(T: int, d: int, flags: int = 0) -> int:
     return lib().elas_norm_join_bwd_workspace_bytes(T, d, flags)
 
@@ -203,6 +205,7 @@ def elas_embed_fwd(ids, table, scale: float = 1.0, dtype: torch.dtype = torch.bf
     return out
 
 
+@functools.lru_cache(maxsize=1024)   # (of the sizes alone)
 def elas_embed_bwd_workspace_bytes(T: int, V: int, d: int, flags: int = 0) -> int:
     return lib().elas_embed_bwd_workspace_bytes(T, V, d, flags)
 
@@ -270,6 +273,7 @@ def _tensors(t) -> ElasTensors:
     return t if isinstance(t, ElasTensors) else ElasTensors(t)
 
 
+@functools.lru_cache(maxsize=1024)   # (of the sizes alone)
 def elas_grad_workspace_bytes(n: int) -> int:
     return lib().elas_grad_workspace_bytes(n)
 

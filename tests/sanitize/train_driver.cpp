@@ -44,7 +44,8 @@ int main() {
   EXPECT(elas_embed_fwd(A, a, 4, 10, 16, INFINITY, 0, A, nullptr) == ELAS_ERR_SHAPE);
   EXPECT(elas_embed_fwd((char*)A + 4, a, 4, 10, 16, 1.f, ELAS_IDS_I64, A, nullptr) == ELAS_ERR_ALIGN);
   EXPECT(elas_embed_fwd(A, a, 4, 10, 16, 1.f, ELAS_EMBED_ADD, A, nullptr) == ELAS_ERR_FLAGS);
-  EXPECT(elas_embed_bwd(A, A, 4, 10, 16, 1.f, 0, f, A, 0, nullptr) == ELAS_ERR_WORKSPACE);
+  EXPECT(elas_embed_bwd(A, A, 5000, 10, 16, 1.f, 0, f, A, 0, nullptr) == ELAS_ERR_WORKSPACE);
+  EXPECT(elas_embed_bwd_workspace_bytes(4096, 32000, 512, 0) == 0);
   EXPECT(elas_embed_bwd(A, A, 4, 10, 16, 1.f, 0, nullptr, A, 1 << 30, nullptr) == ELAS_ERR_NULL);
   EXPECT(elas_embed_bwd(nullptr, nullptr, 0, 10, 16, 1.f, ELAS_EMBED_ADD, nullptr, nullptr, 0, nullptr) == ELAS_OK);
 

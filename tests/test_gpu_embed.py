@@ -122,6 +122,25 @@ def test_same_bits_every_time_and_in_any_workspace():
         assert torch.equal(elas.elas_embed_bwd(ids, dx, V, 1.5, workspace=ws), ref)
 
 
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("T", [33, 64, 1024, 1025, 2049, 4096, 4097])
+def test_long_rows_among_short_ones(T, add):
+    """Rows of one, 32, 33 and many tokens side by side, cut between waves and workgroups."""
+    g = np.random.default_rng(T)
+    V, d = 600, 520
+    sizes = g.choice([1, 2, 31, 32, 33, 64, 65, 500], 400)
+    ids = np.repeat(g.permutation(V)[:400], sizes)[:T]
+    ids = np.concatenate([ids, np.full(T - len(ids), V - 1)])
+    ids = g.permutation(ids)
+    dx = _dx(T, d, BF, T)
+    before = _dx(V, d, F32, 3)
+    table = before.clone() if add else torch.full((V, d), float("nan"), device=DEV)
+    got = elas.elas_embed_bwd(torch.from_numpy(ids).to(DEV), dx, V, 0.5, dtable=table, accumulate=add)
+    _check_grad(ids, dx, V, 0.5, got, before if add else None)
+    again = before.clone() if add else torch.empty_like(table)
+    assert torch.equal(elas.elas_embed_bwd(torch.from_numpy(ids).to(DEV), dx, V, 0.5, dtable=again, accumulate=add), got)
+
+
 def test_nonfinite_gradients_stay_in_their_row():
     T, V, d = 5000, 300, 128
     ids_np = _ids("words", T, V, 4)

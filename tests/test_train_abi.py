@@ -100,7 +100,7 @@ def test_embed_refusals():
     assert fwd(T=0, ids=None, table=None, x=None) == 0
 
     def bwd(**kw):
-        a = dict(ids=A, dx=A, T=4, V=10, d=16, scale=1.0, flags=0, dtable=A, ws=A, wsb=elas.elas_embed_bwd_workspace_bytes(4, 10, 16, 0))
+        a = dict(ids=A, dx=A, T=5000, V=10, d=16, scale=1.0, flags=0, dtable=A, ws=A, wsb=elas.elas_embed_bwd_workspace_bytes(5000, 10, 16, 0))
         a.update(kw)
         return elas.lib().elas_embed_bwd(*a.values(), None)
 
