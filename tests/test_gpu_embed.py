@@ -100,7 +100,7 @@ def test_gradient(T, V, d, kind, add):
 
 
 @pytest.mark.parametrize("T,V,d,res,i64", [(2048, 32000, 512, BF, True), (511, 32000, 768, F32, False), (4096, 70000, 264, BF, False),
-                                           (300, 2 ** 21 + 5, 8, F32, True), (300, 50, 2048, BF, True), (100, 40, 2056, F32, False),
+                                           (300, 2 ** 21 + 5, 8, F32, True), (600, 2 ** 23 + 1, 8, BF, False), (300, 50, 2048, BF, True), (100, 40, 2056, F32, False),
                                            (40, 9, 65536, BF, True), (16384, 32000, 64, BF, False), (16385, 32000, 64, BF, False),
                                            (70001, 5000, 32, BF, True)])
 def test_gradient_sizes(T, V, d, res, i64):
