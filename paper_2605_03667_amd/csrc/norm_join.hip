@@ -163,9 +163,10 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_fwd_kernel(const No
 
 // The sums over the tokens: acc[0] of dn xh, acc[1] of G bh (times the token's
 // gate where there is one for each), added up in the workgroup at the end and
-// written to row blockIdx.x of `part`, [grid][2][d].
+// written to row blockIdx.x of `part`, [grid][2][d].  Held to 128 registers (NV = 1), 4
+// waves to a SIMD: a few more cost a fourth of the waves (130M, 20011 tokens 39 us and 47).
 template <class R, int W, int NV, bool STREAM>
-__global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_bwd_kernel(const NormJoinArgs a, float* part) {
+__global__ __launch_bounds__(64 * (W < 4 ? 4 : W), NV == 1 ? 4 : 2) void join_bwd_kernel(const NormJoinArgs a, float* part) {
   constexpr bool SPLIT = sizeof(R) == 4;
   using Lanes = RowLanes<W, NV, SPLIT>;
   __shared__ float red3[Lanes::WAVES][3], red1[Lanes::WAVES][1];
