@@ -102,7 +102,7 @@ struct NormJoinArgs {
 };
 
 // norm_join.hip
-size_t norm_join_bwd_workspace_bytes(int64_t T, int64_t d, bool res_f32);
+size_t norm_join_bwd_workspace_bytes(int64_t T, int64_t d);
 hipError_t run_norm_join_fwd(const NormJoinArgs& a, hipStream_t stream);
 hipError_t run_norm_join_bwd(const NormJoinArgs& a, hipStream_t stream);
 

@@ -538,15 +538,24 @@ int64_t row_groups(int64_t T, int64_t d) {   // workgroups, at one row (or set o
 }
 // Forward: a workgroup per row or set of rows (1B, 65536 tokens, float32 stream: 269 us;
 // 2048 workgroups that go on to further rows 312).  Backward: each workgroup leaves a row
-// of partial sums, so no more than the card holds at once, 4 waves to a SIMD, or 2 where a
-// float32 stream has twice the bytes in flight for each (1B, 65536 tokens, bf16: 331 us
-// with 512 workgroups, 315 with 1024, 325 with 2048; 32768 tokens, float32: 267, 287, 294;
-// rows of 4096, bf16: 347 us with 256 workgroups of 8 waves, 352 with 512, 360 with 1024).
+// of partial sums, so no more than the card holds at once; of these, 3 waves to a SIMD, or 2
+// where a value of a row has 10 bytes or more to read.  More waves have more rows on their
+// way than the memory serves well, and it is whole waves to each SIMD that load it evenly:
+// 1B, 65536 tokens, bf16 (8 bytes): 2 waves 324 us, 2.5 305, 3 286, 3.5 332, 4 300; 350M,
+// 16381 tokens, float32, gate per token (14 bytes): 1.5 waves 73, 2 66, 3 71, 4 74.
 int64_t fwd_grid(int64_t T, int64_t d) { return std::min<int64_t>(row_groups(T, d), 1 << 20); }
-int64_t bwd_grid(int64_t T, int64_t d, bool res_f32) {
-  const int waves = row_shape(d).waves == 8 ? 8 : 4;
-  return std::max<int64_t>(1, std::min<int64_t>(row_groups(T, d), (res_f32 ? 2048 : 4096) / waves));
+int64_t bwd_grid(int64_t T, int64_t d, int waves_per_simd) {
+  const int waves = row_shape(d).waves == 8 ? 8 : 4;   // of a workgroup
+  return std::max<int64_t>(1, std::min<int64_t>(row_groups(T, d), 1024 * waves_per_simd / waves));
 }
+constexpr int kMostWaves = 3;
+// Bytes of a row's value that the backward reads, and that it writes.
+int bwd_reads(const NormJoinArgs& a) {
+  const int res = a.res_f32 ? 4 : 2;
+  return (a.dh_out ? res : 0) + (a.w_pre ? 2 + res : 0) + (a.b ? 2 : 0) + (a.gate_token ? 2 : 0);
+}
+int bwd_writes(const NormJoinArgs& a) { return (a.dh ? a.res_f32 ? 4 : 2 : 0) + (a.b ? 2 : 0) + (a.gate_token ? 2 : 0); }
+int64_t bwd_grid(const NormJoinArgs& a) { return bwd_grid(a.T, a.d, bwd_reads(a) >= 10 ? 2 : kMostWaves); }
 
 // Backward loads go past the caches where the call moves more than the last-level
 // cache's 256 MB (1B, 65536 tokens 316 -> 306 us); in a smaller one they would miss what
@@ -574,7 +583,7 @@ void launch_fwd(const NormJoinArgs& a, hipStream_t stream) {
 
 template <class R, bool STREAM>
 void launch_bwd(const NormJoinArgs& a, float* part, hipStream_t stream) {
-  const dim3 grid((unsigned)bwd_grid(a.T, a.d, a.res_f32));
+  const dim3 grid((unsigned)bwd_grid(a));
   const RowShape s = row_shape(a.d);
   const size_t lds = part ? (size_t)(2 * a.d) * sizeof(float) : 0;   // (where a workgroup takes several rows)
   if (s.waves == 1)
@@ -593,9 +602,7 @@ void launch_bwd(const NormJoinArgs& a, float* part, hipStream_t stream) {
 
 }  // namespace
 
-size_t norm_join_bwd_workspace_bytes(int64_t T, int64_t d, bool res_f32) {
-  return (size_t)(bwd_grid(T, d, res_f32) * 2 * d) * sizeof(float);
-}
+size_t norm_join_bwd_workspace_bytes(int64_t T, int64_t d) { return (size_t)(bwd_grid(T, d, kMostWaves) * 2 * d) * sizeof(float); }
 
 hipError_t run_norm_join_fwd(const NormJoinArgs& a, hipStream_t stream) {
   TimedLaunch tl("norm_join_fwd", stream);
@@ -612,10 +619,7 @@ hipError_t run_norm_join_bwd(const NormJoinArgs& a, hipStream_t stream) {
   float* part = first || second ? (float*)a.ws : nullptr;
   {
     TimedLaunch tl("norm_join_bwd", stream);
-    // bytes of the rows read and written
-    const int64_t res = a.res_f32 ? 4 : 2, per = (a.dh_out ? res : 0) + (a.dh ? res : 0) + (a.w_pre ? 2 + res : 0) + (a.b ? 4 : 0) +
-                                                 (a.gate_token ? 4 : 0);
-    const bool streams = a.T * a.d * per >= kStreamLoads;
+    const bool streams = a.T * a.d * (bwd_reads(a) + bwd_writes(a)) >= kStreamLoads;
     if (a.res_f32)
       streams ? launch_bwd<float, true>(a, part, stream) : launch_bwd<float, false>(a, part, stream);
     else
@@ -626,7 +630,7 @@ hipError_t run_norm_join_bwd(const NormJoinArgs& a, hipStream_t stream) {
   TimedLaunch tl("norm_join_bwd_sums", stream);
   const int64_t c0 = first ? 0 : a.d, c1 = second ? 2 * a.d : a.d;
   hipLaunchKernelGGL(join_reduce_kernel, dim3((unsigned)((c1 - c0 + 31) / 32)), dim3(256), 0, stream, a, (const float*)part,
-                     (int)bwd_grid(a.T, a.d, a.res_f32), c0, c1);
+                     (int)bwd_grid(a), c0, c1);
   return hipGetLastError();
 }
 

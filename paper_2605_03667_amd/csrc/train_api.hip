@@ -122,8 +122,9 @@ int elas_norm_join_fwd(const void* h, const uint16_t* b, const uint16_t* gate, c
 }
 
 size_t elas_norm_join_bwd_workspace_bytes(int64_t T, int64_t d, uint32_t flags) {
+  (void)flags;
   if (T < 0 || d <= 0) return 0;
-  return elas::norm_join_bwd_workspace_bytes(T, d, (flags & ELAS_RES_F32) != 0);
+  return elas::norm_join_bwd_workspace_bytes(T, d);
 }
 
 int elas_norm_join_bwd(const void* dh_out, const uint16_t* dn, const void* h_out, const uint16_t* b, const uint16_t* gate,
@@ -171,7 +172,7 @@ int elas_norm_join_bwd(const void* dh_out, const uint16_t* dn, const void* h_out
     if (dw_post) ELAS_CHECK(check_ptr(dw_post, "dw_post"));
     if (dw_pre) ELAS_CHECK(check_ptr(dw_pre, "dw_pre"));
   }
-  ELAS_CHECK(check_workspace(workspace, workspace_bytes, elas::norm_join_bwd_workspace_bytes(T, d, (flags & ELAS_RES_F32) != 0)));
+  ELAS_CHECK(check_workspace(workspace, workspace_bytes, elas::norm_join_bwd_workspace_bytes(T, d)));
   elas::NormJoinArgs a{};
   a.T = T; a.d = d; a.h = h_out; a.b = b; a.gate = gate; a.w_post = w_post; a.w_pre = w_pre;
   a.res_scale = b ? res_scale : 1.f; a.block_scale = block_scale; a.eps = eps;
