@@ -26,7 +26,7 @@ namespace {
 //
 // Measured, bytes that the call cannot do without over its time: forward 1B, 65536 tokens,
 // float32 stream 264 us (6.1 TB/s; a copy of 1 GiB reaches 5.5); 350M, 2000 tokens 6.3 us
-// of kernel; 1B, 16 tokens 3.6.  Backward 1B, 65536 tokens 303 us (5.3 TB/s); 350M, 16381
+// of kernel; 1B, 16 tokens 3.6.  Backward 1B, 65536 tokens 285 us (5.7 TB/s); 350M, 16381
 // tokens, gate per token, float32 stream 66 us (5.6); 60M, 2048 tokens 5.0 + 3.7 us.
 
 // Where a thread's row and pieces lie; loads and stores of piece v.
@@ -163,10 +163,10 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_fwd_kernel(const No
 
 // The sums over the tokens: acc[0] of dn xh, acc[1] of G bh (times the token's
 // gate where there is one for each), added up in the workgroup at the end and
-// written to row blockIdx.x of `part`, [grid][2][d].  Held to 128 registers (NV = 1), 4
-// waves to a SIMD: a few more cost a fourth of the waves (130M, 20011 tokens 39 us and 47).
+// written to row blockIdx.x of `part`, [grid][2][d].  Held to the registers that leave
+// a SIMD the 3 waves that the grid has for it (NV = 1; at 128, for 4, no faster).
 template <class R, int W, int NV, bool STREAM>
-__global__ __launch_bounds__(64 * (W < 4 ? 4 : W), NV == 1 ? 4 : 2) void join_bwd_kernel(const NormJoinArgs a, float* part) {
+__global__ __launch_bounds__(64 * (W < 4 ? 4 : W), NV == 1 ? 3 : 2) void join_bwd_kernel(const NormJoinArgs a, float* part) {
   constexpr bool SPLIT = sizeof(R) == 4;
   using Lanes = RowLanes<W, NV, SPLIT>;
   __shared__ float red3[Lanes::WAVES][3], red1[Lanes::WAVES][1];
