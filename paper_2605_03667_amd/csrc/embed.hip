@@ -513,47 +513,54 @@ __global__ __launch_bounds__(1024) void embed_few_kernel(const EmbedArgs a, cons
 }
 
 // Adds the sums of the chunks that left a row open, in their order, to the row.  A
-// workgroup looks after the run of such chunks that begins at its own, for 1024
-// columns; its 4 quarters take a share of the run each.
-__global__ __launch_bounds__(1024) void embed_join_kernel(const EmbedArgs a, const SumArgs s) {
-  __shared__ float4 red[3][256];
-  const int lane = threadIdx.x & 63, c0 = blockIdx.x;
-  // rows of the chunk before, of this one and of the next 62
-  const int q0 = c0 - 1 + lane;
+// workgroup looks after the runs of such chunks that begin at one of kJoinChunks, for
+// 256 columns; its kJoinShares waves take an equal share of a run each.  Most chunks leave
+// no row open, and what counts is how few waves are launched to find that: 1B, 65536 tokens,
+// all launches of the gradient 133.0 us, 134.2 with a chunk to a workgroup, 136.4 with 8 (whose
+// runs are then joined one after the other), 134.8 with 8 waves; 60M 49.3, 50.1, 49.0, 49.3.
+constexpr int kJoinChunks = 4, kJoinShares = 4;
+__global__ __launch_bounds__(64 * kJoinShares) void embed_join_kernel(const EmbedArgs a, const SumArgs s) {
+  __shared__ float4 red[2][kJoinShares][64];
+  const int lane = threadIdx.x & 63, share = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int first = blockIdx.x * kJoinChunks;
+  // rows of the chunk before, of these and of the next
+  const int q0 = first - 1 + lane;
   const uint32_t near = q0 >= 0 && q0 < s.chunks ? s.carry_row[q0] : ~0u;
-  const uint32_t row = __builtin_amdgcn_readlane(near, 1);
-  if (row == ~0u || __builtin_amdgcn_readlane(near, 0) == row) return;
-  uint64_t other = __ballot(near != row) & ~1ull;
-  int n = 0;   // chunks of the run
-  for (int q = c0 - 1; other == 0;) {
-    q += 64;
-    n = q - c0;
-    other = __ballot(!(q + lane < s.chunks && s.carry_row[q + lane] == row));
-  }
-  n = n > 0 ? n + __ffsll((unsigned long long)other) - 1 : __ffsll((unsigned long long)other) - 2;
-  const int quarter = threadIdx.x >> 8, i = threadIdx.x & 255;
-  const int b = c0 + (int)((int64_t)n * quarter / 4), e = c0 + (int)((int64_t)n * (quarter + 1) / 4);
-  const int64_t c = (int64_t)blockIdx.y * 1024 + i * 4;
+  const uint32_t before = __shfl_up(near, 1);
+  uint64_t heads = __ballot(near != ~0u && near != before) & ((1ull << kJoinChunks) - 1) << 1;
+  const int64_t c = (int64_t)blockIdx.y * 256 + lane * 4;
   const bool there = c < a.d;
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (there) {
+  for (int turn = 0; heads; turn ^= 1, heads &= heads - 1) {
+    const int at = __ffsll((unsigned long long)heads) - 1, c0 = first - 1 + at;
+    const uint32_t row = __builtin_amdgcn_readlane(near, at);
+    uint64_t other = __ballot(near != row) >> at << at;
+    int end = first - 1;   // behind the run's last chunk
+    while (other == 0) {
+      end += 64;
+      other = __ballot(!(end + lane < s.chunks && s.carry_row[end + lane] == row));
+    }
+    end += __ffsll((unsigned long long)other) - 1;
+    const int n = end - c0;
+    const int b = c0 + (int)((int64_t)n * share / kJoinShares), e = c0 + (int)((int64_t)n * (share + 1) / kJoinShares);
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f), *out = (float4*)(a.dtable + (int64_t)row * a.d + c);
+    const float4 o = there && share == 0 ? *out : x;
+    if (there) {
 #pragma unroll 8
-    for (int k = b; k < e; ++k) {
-      const float4 y = *(const float4*)(s.carry + (int64_t)k * a.d + c);
+      for (int k = b; k < e; ++k) {
+        const float4 y = *(const float4*)(s.carry + (int64_t)k * a.d + c);
+        x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+      }
+    }
+    red[turn][share][lane] = x;
+    __syncthreads();   // (two buffers: the next turn's writes do not meet this one's reads)
+    if (share > 0 || !there) continue;
+#pragma unroll
+    for (int q = 1; q < kJoinShares; ++q) {
+      const float4 y = red[turn][q][lane];
       x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
     }
+    *out = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
   }
-  if (quarter > 0) red[quarter - 1][i] = x;
-  __syncthreads();
-  if (quarter > 0 || !there) return;
-  float4* out = (float4*)(a.dtable + (int64_t)row * a.d + c);
-  const float4 o = *out;
-#pragma unroll
-  for (int q = 0; q < 3; ++q) {
-    const float4 y = red[q][i];
-    x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
-  }
-  *out = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
 }
 
 // ---- host -----------------------------------------------------------------------------
@@ -702,7 +709,8 @@ hipError_t run_embed_bwd(const EmbedArgs& a, hipStream_t stream) {
   }
   if (p.few) return hipSuccess;
   TimedLaunch tl("embed_bwd_join", stream);
-  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)p.sum.chunks, (unsigned)cdiv(a.d, 1024)), dim3(1024), 0, stream, a, p.sum);
+  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)cdiv(p.sum.chunks, kJoinChunks), (unsigned)cdiv(a.d, 256)), dim3(64 * kJoinShares),
+                     0, stream, a, p.sum);
   return hipGetLastError();
 }
 
