@@ -9,9 +9,9 @@
 // order) and then walks the sorted tokens and the table's rows together.  The sort
 // works on 4 to 8 bytes a token and is bound by latency and launches; the sum reads dx
 // and writes the table once and is bound by HBM.  1B, 65536 tokens whose ids fall off
-// like words: 133 us, of which the sort 2 (4.7 + 6.2), the sum 109 (4.9 TB/s), the
-// joining of cut rows 7; with one id for all tokens 149.  60M, 2048 tokens, added: 16.6 us
-// in one launch, about half of it the sort.
+// like words: 133 us, of which the sort 2 (4.7 + 6.0), the sum 108 (4.9 TB/s), the
+// joining of cut rows 6; with one id for all tokens 123.  Up to 4096 tokens one launch does
+// it all (60M, 2048 tokens, added: 11.0 us).
 #include <algorithm>
 
 #include "internal.h"
@@ -140,39 +140,32 @@ __device__ __forceinline__ uint32_t wave_prefixes(uint32_t* count, int bins) {
   return n;
 }
 
-// Up to 1024 E tokens by one workgroup, all passes in shared memory: `entries` holds key
-// << tbits | token, sorted.
+// n <= 1024 E entries (key << tbits | token) of one workgroup, all passes in shared memory.
 template <int E>
-__device__ __forceinline__ void sort_in_lds(const EmbedArgs& a, int passes, int bits, int tbits, uint32_t* count, uint32_t* base, uint32_t* tmp,
+__device__ __forceinline__ void sort_in_lds(int n, int passes, int bits, int tbits, uint32_t* count, uint32_t* base, uint32_t* tmp,
                                             uint32_t* entries) {
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int T = (int)a.T, bins = 1 << bits;
+  const int bins = 1 << bits;
   uint32_t e[E], digit[E], rank[E];
   bool ok[E];
 #pragma unroll
-  for (int r = 0; r < E; ++r) {
-    const int t = (int)((wave * E + r) * 64 + lane);
-    ok[r] = t < T;
-    e[r] = ok[r] ? key_at(a, t) << tbits | (uint32_t)t : 0u;
-  }
+  for (int r = 0; r < E; ++r) ok[r] = (int)((wave * E + r) * 64 + lane) < n;
   for (int p = 0; p < passes; ++p) {
     for (int w = threadIdx.x >> bits; w < 16; w += 1024 >> bits) count[w * kDigits + (threadIdx.x & (bins - 1))] = 0;
+#pragma unroll
+    for (int r = 0; r < E; ++r) e[r] = entries[(wave * E + r) * 64 + lane];   // (entries past n: not used)
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < E; ++r) digit[r] = (e[r] >> (tbits + p * bits)) & (uint32_t)(bins - 1);
     wave_ranks<E>(digit, ok, bits, count + wave * kDigits, rank);
     __syncthreads();
-    const uint32_t n = wave_prefixes(count, bins);
-    const uint32_t first = bin_scan(n, bins, tmp);
+    const uint32_t first = bin_scan(wave_prefixes(count, bins), bins, tmp);
     if ((int)threadIdx.x < bins) base[threadIdx.x] = first;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < E; ++r)
       if (ok[r]) entries[base[digit[r]] + count[wave * kDigits + digit[r]] + rank[r]] = e[r];
     __syncthreads();
-    if (p + 1 == passes) break;
-#pragma unroll
-    for (int r = 0; r < E; ++r) e[r] = entries[(wave * E + r) * 64 + lane];   // (entries past T: not used)
   }
 }
 
@@ -269,6 +262,21 @@ struct SharedTokens {
   __device__ __forceinline__ uint32_t pos(int64_t p) const { return entries[(int)p] & ((1u << tbits) - 1); }
 };
 
+// The table's row behind a row's number: itself, or one of those of workgroup `group`
+// among 2^bits, which has one of every 2^bits consecutive rows (another one each time, so
+// that ids at equal distances do not meet in one workgroup).
+struct AllRows {
+  __device__ __forceinline__ int64_t operator()(uint32_t v) const { return v; }
+};
+struct GroupRows {
+  uint32_t group;
+  int bits;
+  __device__ __forceinline__ uint32_t mask() const { return (1u << bits) - 1; }
+  __device__ __forceinline__ int64_t operator()(uint32_t v) const { return (int64_t)v << bits | ((group ^ v ^ v >> bits) & mask()); }
+  __device__ __forceinline__ bool has(uint32_t key) const { return ((key ^ key >> bits ^ key >> 2 * bits) & mask()) == group; }
+  __device__ __forceinline__ uint32_t number(int64_t V) const { return (uint32_t)(V >> bits) + ((*this)((uint32_t)(V >> bits)) < V); }
+};
+
 struct SumArgs {
   int64_t chunk;               // length of a chunk
   int chunks, slices;          // slices of 512 features (few tokens: of a workgroup)
@@ -298,9 +306,8 @@ struct Cut {
   uint32_t v;     // first row whose end lies behind the cut
   uint32_t mid;   // whether the cut is inside row v, with tokens of it on both sides
 };
-// whole: a cut is moved behind the row it falls into, however long that is.
 template <class Tokens>
-__device__ __forceinline__ Cut cut_at(const EmbedArgs& a, const Tokens& tokens, int64_t at, bool whole) {
+__device__ __forceinline__ Cut cut_at(const EmbedArgs& a, const Tokens& tokens, int64_t at) {
   const int lane = threadIdx.x & 63;
   const int weight = a.add ? 0 : kRowWeight;
   const uint32_t V = (uint32_t)a.V;
@@ -318,9 +325,6 @@ __device__ __forceinline__ Cut cut_at(const EmbedArgs& a, const Tokens& tokens, 
     const int rest = __ffs(above) - 1;
     if (below != 0 && above != 0 && __clz(below) + rest <= 32) {
       c.p += rest;
-      c.v = right + 1;
-    } else if (whole) {
-      c.p = first_where(a.T, [&](int64_t p) { return tokens.key(p) > right; });
       c.v = right + 1;
     } else {
       c.v = right;
@@ -362,8 +366,9 @@ struct Open {
 };
 
 // Sums between two cuts, U tokens on their way at once.
-template <class R, bool ADD, bool HOLD, int U, class Tokens>
-__device__ __forceinline__ Open sum_range(const EmbedArgs& a, const Tokens& tokens, const Cut& c0, const Cut& c1, const Columns& col) {
+template <class R, bool ADD, bool HOLD, int U, class Tokens, class Rows>
+__device__ __forceinline__ Open sum_range(const EmbedArgs& a, const Tokens& tokens, const Rows& rows, const Cut& c0, const Cut& c1,
+                                          const Columns& col) {
   const int lane = threadIdx.x & 63;
   const uint32_t V = (uint32_t)a.V;
   Open o;
@@ -378,7 +383,7 @@ __device__ __forceinline__ Open sum_range(const EmbedArgs& a, const Tokens& toke
     if (ADD) old.get(x);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = ADD ? fmaf(a.scale, o.acc[i], x[i]) : a.scale * o.acc[i], o.acc[i] = 0.f;
-    Piece<float, true>::store<!ADD>((a.dtable + (int64_t)v * a.d) + col.c, x, col.there, col.there2);
+    Piece<float, true>::store<!ADD>((a.dtable + rows(v) * a.d) + col.c, x, col.there, col.there2);
   };
   const Piece<float, true> nothing = {};
   for (int64_t p = c0.p; p < c1.p; p += 64) {
@@ -395,7 +400,7 @@ __device__ __forceinline__ Open sum_range(const EmbedArgs& a, const Tokens& toke
         if (ku >= V) continue;
         x[u].load(((const R*)a.dx + t * a.d) + col.c, col.there, col.there2);
         if (ADD && __builtin_amdgcn_readlane(after, j + u) != ku)
-          old[ADD ? u : 0].load((a.dtable + (int64_t)ku * a.d) + col.c, col.there, col.there2);
+          old[ADD ? u : 0].load((a.dtable + rows(ku) * a.d) + col.c, col.there, col.there2);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -431,7 +436,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const
   // the 4 tasks lie in at most 4 chunks: their cuts, one to a wave
   const int64_t task0 = (int64_t)blockIdx.x * 4, chunk0 = task0 / s.slices, last = (task0 + 3) / s.slices + 1;
   for (int i = wave; chunk0 + i <= last; i += 4) {
-    const Cut c = cut_at(a, tokens, (chunk0 + i) * s.chunk, false);
+    const Cut c = cut_at(a, tokens, (chunk0 + i) * s.chunk);
     if (lane == 0) cuts[i] = c;
   }
   __syncthreads();
@@ -439,7 +444,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const
   if (chunk >= s.chunks) return;
   const int slice = (int)(task - chunk * s.slices), i = (int)(chunk - chunk0);
   const Columns col(a, slice);
-  Open o = sum_range<R, ADD, false, ADD ? 4 : sizeof(R) == 2 ? 16 : 8>(a, tokens, uniform(cuts[i]), uniform(cuts[i + 1]), col);
+  Open o = sum_range<R, ADD, false, ADD ? 4 : sizeof(R) == 2 ? 16 : 8>(a, tokens, AllRows{}, uniform(cuts[i]), uniform(cuts[i + 1]), col);
   if (o.open) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) o.acc[k] *= a.scale;
@@ -448,42 +453,86 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const EmbedArgs a, const
   if (slice == 0 && lane == 0) s.carry_row[chunk] = o.open ? o.row : ~0u;
 }
 
-// Few tokens: every workgroup sorts them for itself, in shared memory, and takes a chunk
-// of whole rows; its 16 waves take the slices (s.slices of them, 16 at most) of 16 /
-// s.slices equal shares of it each.  Rows cut between shares are joined in shared memory, so
-// that one launch does it all: the wave that ends such a row holds its own part, and adds
-// those of the shares before it in their order.  (60M, 2048 tokens, added: 16.6 us; with
-// the rows joined by embed_join_kernel 18.7; with the sort a launch of its own 23.)
+// Few tokens: a workgroup has one of every 2^gbits rows, looks through all ids for theirs,
+// sorts those in shared memory, and walks them and its rows with its 16 waves: the slices
+// (s.slices of them, 16 at most) of 16 / s.slices equal shares each.  Rows cut between
+// shares are joined in shared memory, so that one launch does it all: the wave that ends
+// such a row holds its own part, and adds those of the shares before it in their order.
+// (60M, 2048 tokens, added: 11.0 us; where every workgroup sorts all tokens for itself
+// 16.5, with the sort a launch of its own 23.)
+constexpr int kRanked = 512;   // entries, up to which a place is found by comparing with all
 template <class R, bool ADD, int E>
-__global__ __launch_bounds__(1024) void embed_few_kernel(const EmbedArgs a, const SumArgs s, int passes, int bits, int tbits) {
-  __shared__ __attribute__((aligned(16))) uint32_t count[16 * kDigits];
-  __shared__ uint32_t base[kDigits], tmp[8], entries[1024 * E];
+__global__ __launch_bounds__(1024) void embed_few_kernel(const EmbedArgs a, const SumArgs s, int gbits, int passes, int bits, int tbits) {
+  __shared__ __attribute__((aligned(16))) uint32_t count[16 * kDigits], entries[1024 * E + 4];
+  __shared__ uint32_t base[kDigits], tmp[16];
   __shared__ Cut cuts[17];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const GroupRows rows{blockIdx.x, gbits};
+  uint32_t e[E];
+  uint64_t mine[E];
+  int found = 0;
+#pragma unroll
+  for (int r = 0; r < E; ++r) {
+    const int64_t t = (wave * E + r) * 64 + lane;
+    const uint32_t key = t < a.T ? key_at(a, t) : (uint32_t)a.V;
+    mine[r] = __ballot(key < (uint32_t)a.V && rows.has(key));
+    e[r] = key >> gbits << tbits | (uint32_t)t;
+    found += __popcll(mine[r]);
+  }
+  if (lane == 0) tmp[wave] = (uint32_t)found;
+  __syncthreads();
+  int at = 0, n = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    at += w < wave ? (int)tmp[w] : 0;
+    n += (int)tmp[w];
+  }
+  n = __builtin_amdgcn_readfirstlane(n);
+  if (ADD && n == 0) return;
+#pragma unroll
+  for (int r = 0; r < E; ++r) {
+    if (mine[r] >> lane & 1)
+      entries[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(mine[r] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mine[r], 0u))] = e[r];
+    at += __popcll(mine[r]);
+  }
+  if (threadIdx.x < 4) entries[n + threadIdx.x] = ~0u;
+  __syncthreads();
+  if (n <= kRanked) {
+    // each entry's place: the number of those below it
+    uint32_t own = 0, place = 0;
+    if (wave * 64 < n) {
+      own = entries[threadIdx.x];
+#pragma unroll 4
+      for (int k = 0; k < n; k += 4) {
+        const uint4 o = *(const uint4*)(entries + k);
+        place += (o.x < own) + (o.y < own) + (o.z < own) + (o.w < own);
+      }
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < n) entries[place] = own;
+    __syncthreads();
+  } else {
+    sort_in_lds<E>(n, passes, bits, tbits, count, base, tmp, entries);
+  }
+  EmbedArgs here = a;   // the workgroup's own tokens and rows
+  here.T = n;
+  here.V = rows.number(a.V);
+  const SharedTokens tokens{entries, tbits};
   const int shares = 16 / s.slices, share = wave / s.slices;
   const bool works = share < shares;   // (16 may not be a multiple of the slices)
-  sort_in_lds<E>(a, passes, bits, tbits, count, base, tmp, entries);
-  const SharedTokens tokens{entries, tbits};
-  const Cut first = cut_at(a, tokens, blockIdx.x * s.chunk, true), last = cut_at(a, tokens, (blockIdx.x + 1) * s.chunk, true);
-  if (wave <= shares) {
-    Cut c = wave == 0 ? first : last;
-    if (wave > 0 && wave < shares) {
-      const int weight = ADD ? 0 : kRowWeight;
-      const int64_t at0 = first.p + (int64_t)weight * first.v, at1 = last.p + (int64_t)weight * last.v;
-      c = cut_at(a, tokens, at0 + (at1 - at0) * wave / shares, false);
-      if (c.p < first.p || (c.p == first.p && c.v < first.v)) c = first;
-      if (c.p > last.p || (c.p == last.p && c.v > last.v)) c = last;
-    }
+  if (wave < shares) {
+    Cut c{};
+    if (wave > 0) c = cut_at(here, tokens, (here.T + (ADD ? 0 : kRowWeight) * here.V) * wave / shares);
     if (lane == 0) cuts[wave] = c;
   }
-  if (shares == 16 && wave == 0 && lane == 0) cuts[16] = last;
+  if (threadIdx.x == 0) cuts[shares] = {here.T, (uint32_t)here.V, 0};
   __syncthreads();
   const Columns col(a, (int)blockIdx.y * s.slices + wave - share * s.slices);
   Open o;
   Cut c0{}, c1{};
   if (works) {
     c0 = uniform(cuts[share]), c1 = uniform(cuts[share + 1]);
-    o = sum_range<R, ADD, true, ADD ? 4 : 8>(a, tokens, c0, c1, col);
+    o = sum_range<R, ADD, true, ADD ? 4 : 8>(here, tokens, rows, c0, c1, col);
   }
   float(*carry)[512] = (float(*)[512])count;   // (the counters are free)
   const int l = lane * 4;
@@ -502,7 +551,7 @@ __global__ __launch_bounds__(1024) void embed_few_kernel(const EmbedArgs a, cons
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[k] += v[k];
   }
-  float* out = (a.dtable + (int64_t)c0.v * a.d) + col.c;
+  float* out = (a.dtable + rows(c0.v) * a.d) + col.c;
   Piece<float, true> old;
   old.load(out, ADD && col.there, ADD && col.there2);
   float x[8];
@@ -574,8 +623,9 @@ int bit_length(int64_t v) {
 // Sort and cuts of one call, and its regions of the workspace.
 struct Plan {
   int passes, bits, tbits;
-  bool few;            // sorted by every workgroup for itself
+  bool few;            // one launch, embed_few_kernel
   int per_thread;      // tokens of a thread in a pass
+  int gbits;           // few: 2^gbits workgroups to a slice group
   int groups;
   int slice_groups;    // few: of sum.slices each
   SumArgs sum;
@@ -588,24 +638,32 @@ Plan plan(void* ws, int64_t T, int64_t V, int64_t d, bool add) {
   p.passes = (key_bits + 8) / 9;
   p.bits = (key_bits + p.passes - 1) / p.passes;
   p.tbits = std::max(1, bit_length(T - 1));
-  p.few = T <= 4096 && key_bits + p.tbits <= 32;
-  p.per_thread = p.few ? (T <= 1024 ? 1 : T <= 2048 ? 2 : 4) : T <= 131072 ? 1 : T <= (1 << 18) ? 4 : 8;
-  p.groups = (int)cdiv(T, 1024 * p.per_thread);
   p.sum.slices = (int)cdiv(d, 512);
-  // about 8 waves to a SIMD, and not under a few tokens or rows to each; where every
-  // workgroup sorts first, one of 16 waves to a CU
-  const int64_t length = add ? T : T + kRowWeight * V;
-  const int64_t least = add ? 4 : 16;
+  // Few tokens, added: a slice to a workgroup, about 16 tokens to each (1B, 2048 tokens: with
+  // 64 the same, 17.2 us; 60M 11.0 and 11.9), all of them on the card at once (1B 17 and 29).
+  // Written: all slices of a row in one (1B, 4096 tokens: 50 us, one slice 67), and a workgroup
+  // for every 32768 values of the table, so that those with the long rows have little else to
+  // do and the others go on (1B 50, with twice the rows 53, with 8 times 72; 60M 20.2, with
+  // half the rows 25.2, with twice 23.3), or as many as adding has, if those are more (256
+  // rows of 64, 4096 tokens: 10.9 us, in one workgroup 82).
+  p.slice_groups = add ? p.sum.slices : (int)cdiv(p.sum.slices, 16);
+  const int by_tokens = std::max(0, std::min(8 - bit_length(p.slice_groups - 1), bit_length(T / 16)));
+  p.gbits = add ? by_tokens : std::min(12, std::max(by_tokens, bit_length(V * d / 32768)));
+  const int few_bits = bit_length((V - 1) >> p.gbits);   // of a row's number in its workgroup
+  p.few = T <= 4096 && few_bits + p.tbits <= 32;
   if (p.few) {
-    // all slices of a row in one workgroup where rows are written (1B, 30 tokens: 56 us, one
-    // slice 61); one slice, and a long row shared by all 16 waves, where tokens are added (1B,
-    // 4096 tokens: 32 and 26)
-    p.slice_groups = add ? p.sum.slices : (int)cdiv(p.sum.slices, 16);
+    p.passes = (few_bits + 8) / 9;
+    p.bits = p.passes ? (few_bits + p.passes - 1) / p.passes : 0;
+    p.per_thread = T <= 1024 ? 1 : T <= 2048 ? 2 : 4;
     p.sum.slices = (int)cdiv(p.sum.slices, p.slice_groups);
-    p.sum.chunk = std::max<int64_t>(16 / p.sum.slices * least, cdiv(length * p.slice_groups, 256));
-  } else {
-    p.sum.chunk = std::max<int64_t>(least, cdiv(length * p.sum.slices, 8192));
+    return p;
   }
+  p.per_thread = T <= 131072 ? 1 : T <= (1 << 18) ? 4 : 8;
+  p.groups = (int)cdiv(T, 1024 * p.per_thread);
+  // about 8 waves to a SIMD (1B, 65536 tokens: 133 us, 4 waves 139; 60M 49.3 and 46.6), and
+  // not under a few tokens or rows to each
+  const int64_t length = add ? T : T + kRowWeight * V;
+  p.sum.chunk = std::max<int64_t>(add ? 4 : 16, cdiv(length * p.sum.slices, 8192));
   p.sum.chunks = (int)std::max<int64_t>(1, cdiv(length, p.sum.chunk));
   size_t used = 0;
   auto take = [&](size_t n) {
@@ -613,15 +671,13 @@ Plan plan(void* ws, int64_t T, int64_t V, int64_t d, bool add) {
     used += (n * sizeof(uint32_t) + 255) / 256 * 256;
     return r;
   };
-  for (int i = 0; i < (p.few ? 0 : p.passes == 1 ? 1 : 2); ++i) {
+  for (int i = 0; i < (p.passes == 1 ? 1 : 2); ++i) {
     p.key[i] = take((size_t)T);
     p.pos[i] = take((size_t)T);
   }
-  if (!p.few) p.hist = take((size_t)p.groups << p.bits);
-  if (!p.few) {
-    p.sum.carry_row = take((size_t)p.sum.chunks);
-    p.sum.carry = (float*)take((size_t)(p.sum.chunks * d));
-  }
+  p.hist = take((size_t)p.groups << p.bits);
+  p.sum.carry_row = take((size_t)p.sum.chunks);
+  p.sum.carry = (float*)take((size_t)(p.sum.chunks * d));
   p.bytes = used;
   return p;
 }
@@ -662,11 +718,11 @@ void launch_sum(const EmbedArgs& a, const SumArgs& s, const MemoryTokens& tokens
 
 template <class R, int E>
 void launch_few(const EmbedArgs& a, const Plan& p, hipStream_t stream) {
-  const dim3 grid((unsigned)p.sum.chunks, (unsigned)p.slice_groups);
+  const dim3 grid(1u << p.gbits, (unsigned)p.slice_groups);
   if (a.add)
-    hipLaunchKernelGGL((embed_few_kernel<R, true, E>), grid, dim3(1024), 0, stream, a, p.sum, p.passes, p.bits, p.tbits);
+    hipLaunchKernelGGL((embed_few_kernel<R, true, E>), grid, dim3(1024), 0, stream, a, p.sum, p.gbits, p.passes, p.bits, p.tbits);
   else
-    hipLaunchKernelGGL((embed_few_kernel<R, false, E>), grid, dim3(1024), 0, stream, a, p.sum, p.passes, p.bits, p.tbits);
+    hipLaunchKernelGGL((embed_few_kernel<R, false, E>), grid, dim3(1024), 0, stream, a, p.sum, p.gbits, p.passes, p.bits, p.tbits);
 }
 
 }  // namespace

@@ -141,6 +141,24 @@ def test_long_rows_among_short_ones(T, add):
     assert torch.equal(elas.elas_embed_bwd(torch.from_numpy(ids).to(DEV), dx, V, 0.5, dtable=again, accumulate=add), got)
 
 
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("T", [511, 512, 513, 4096])
+@pytest.mark.parametrize("kind", ["folded", "distance"])
+def test_ids_that_meet_in_one_workgroup(T, add, kind):
+    """Few tokens: the rows are dealt out to 256 workgroups (added) or 512 (written) by their
+    ids' bits folded together; ids whose fold is the same, and ids at equal distances."""
+    V, d = 2 ** 20 + 3, 8
+    bits = 8 if add else 9
+    g = np.random.default_rng(T)
+    q = g.integers(0, (V >> bits) - 1, T)
+    ids = q << bits | ((q ^ q >> bits ^ 5) & ((1 << bits) - 1)) if kind == "folded" else q << bits
+    dx = _dx(T, d, BF, T)
+    before = _dx(V, d, F32, 3)
+    table = before.clone() if add else torch.full((V, d), float("nan"), device=DEV)
+    got = elas.elas_embed_bwd(torch.from_numpy(ids).to(DEV), dx, V, 0.5, dtable=table, accumulate=add)
+    _check_grad(ids, dx, V, 0.5, got, before if add else None)
+
+
 def test_nonfinite_gradients_stay_in_their_row():
     T, V, d = 5000, 300, 128
     ids_np = _ids("words", T, V, 4)
