@@ -159,6 +159,19 @@ def test_ids_that_meet_in_one_workgroup(T, add, kind):
     _check_grad(ids, dx, V, 0.5, got, before if add else None)
 
 
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("kind", ["uniform", "words", "one", "padding", "ends", "runs"])
+@pytest.mark.parametrize("T", [4097, 5151, 8191, 8192, 8193])
+def test_between_one_launch_and_the_radix_sort(T, kind, add):
+    V, d = 2500, 40
+    ids = _ids(kind, T, V, T)
+    dx = _dx(T, d, F32, T)
+    before = _dx(V, d, F32, 3)
+    table = before.clone() if add else torch.full((V, d), float("nan"), device=DEV)
+    got = elas.elas_embed_bwd(torch.from_numpy(ids).to(DEV), dx, V, 0.5, dtable=table, accumulate=add)
+    _check_grad(ids, dx, V, 0.5, got, before if add else None)
+
+
 def test_nonfinite_gradients_stay_in_their_row():
     T, V, d = 5000, 300, 128
     ids_np = _ids("words", T, V, 4)
