@@ -239,7 +239,8 @@ def elas_embed_bwd(ids, dx, V: int, scale: float = 1.0, dtable: torch.Tensor | N
 class ElasTensors:
     """A list of GPU tensors (float32 or bf16, contiguous, any shapes) as the C ABI
     takes it.  A program that uses the same tensors every step makes it once; the
-    tensors are held, and their addresses and lengths are read again at every call."""
+    tensors are held, and their addresses, lengths, types and layouts are read again
+    at every call (a tensor's ``data`` may have been replaced since)."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -256,16 +257,16 @@ class ElasTensors:
     def arrays(self):
         """The host arrays of addresses, lengths and types."""
         ts = self.tensors
-        addresses, numel = list(map(torch.Tensor.data_ptr, ts)), list(map(torch.Tensor.numel, ts))
-        if addresses != self._addresses or numel != self.layout[0]:
+        addresses, layout = list(map(torch.Tensor.data_ptr, ts)), (list(map(torch.Tensor.numel, ts)), [t.dtype for t in ts])
+        if addresses != self._addresses or layout != self.layout or not all(map(torch.Tensor.is_contiguous, ts)):
             dev = self.device.index
             for k, t in enumerate(ts):
                 if t.dtype != _F32 and t.dtype != _BF16:
                     raise ValueError(f"tensor {k} must be torch.float32 or torch.bfloat16, got {t.dtype}")
                 _arg(t, t.shape, t.dtype, -1 if dev is None else dev, f"tensor {k}")
-            dtype = [ELAS_GRAD_F32 if t.dtype == _F32 else ELAS_GRAD_BF16 for t in ts]
-            self._pointers[:], self._numel[:], self._dtype[:] = addresses, numel, dtype
-            self.layout, self._addresses = (numel, dtype), addresses
+            self._pointers[:], self._numel[:] = addresses, layout[0]
+            self._dtype[:] = [ELAS_GRAD_F32 if t == _F32 else ELAS_GRAD_BF16 for t in layout[1]]
+            self.layout, self._addresses = layout, addresses
         return self._pointers, self._numel, self._dtype
 
 

@@ -132,6 +132,21 @@ def test_handle_follows_its_tensors():
     assert elas.elas_grad_norm(h)[0] == 40
 
 
+def test_handle_refuses_what_its_tensors_became():
+    """Another type or another order of the same values in the same memory."""
+    t = torch.ones((4, 8), device=DEV)
+    h = elas.ElasTensors([t])
+    assert elas.elas_grad_norm(h)[0] == 32.0 ** 0.5
+    t.t_()
+    with pytest.raises(ValueError, match="contiguous"):
+        elas.elas_grad_norm(h)
+    t.t_()
+    assert elas.elas_grad_norm(h)[0] == 32.0 ** 0.5
+    t.data = t.data.view(torch.int32)
+    with pytest.raises(ValueError, match="float32 or torch.bfloat16"):
+        elas.elas_grad_clip(h, 1.0)
+
+
 def test_same_bits_every_time():
     g = _tensors([300000, 77, 1 << 20], [F32, BF], 9, 1)
     first = elas.elas_grad_norm(g)
