@@ -9,8 +9,9 @@
 // long tensor and a hundred short ones load the card alike.  Bound by HBM: one read for
 // the norm, one read and one write for the scaling.  The scaling takes the pieces in
 // the opposite order, so that it begins with what the caches still hold (985 MB: 570 us,
-// in the same order 578).  985 MB in 193 tensors: 495 us, 6.0 TB/s over the three; 15.5 MB
-// in 49 tensors: 5.8 + 8.8 us of kernels, 17.8 us a call; the norm alone of 985 MB 156 us (6.3 TB/s).
+// in the same order 578).  985 MB in 193 tensors: 493 us, 6.0 TB/s over the three; 15.5 MB
+// in 49 tensors: 5.8 + 9.1 us of kernels, 23 us a call (the tensors' addresses, lengths,
+// types and layouts are read in every one); the norm alone of 985 MB 156 us (6.3 TB/s).
 #include <math.h>
 
 #include <algorithm>

@@ -27,7 +27,7 @@ namespace {
 // Measured, bytes that the call cannot do without over its time: forward 1B, 65536 tokens,
 // float32 stream 264 us (6.1 TB/s; a copy of 1 GiB reaches 5.5); 350M, 2000 tokens 6.3 us
 // of kernel; 1B, 16 tokens 3.6.  Backward 1B, 65536 tokens 285 us (5.7 TB/s); 350M, 16381
-// tokens, gate per token, float32 stream 66 us (5.6); 60M, 2048 tokens 5.0 + 3.7 us.
+// tokens, gate per token, float32 stream 66 us (5.6); 60M, 2048 tokens 4.9 + 3.4 us.
 
 // Where a thread's row and pieces lie; loads and stores of piece v.
 template <int W, int NV, bool SPLIT>
