@@ -50,7 +50,8 @@ struct Outputs {
   void* out[CAP];
 };
 
-// (tensors need their element's alignment only: 16-byte accesses at any such address)
+// Tensors need their element's alignment only: 16-byte accesses at any such address.  (As a
+// template argument these types would lose their alignment, so every access names its type.)
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
@@ -67,19 +68,20 @@ struct Part {
   template <bool STREAM>
   static __device__ __forceinline__ void load(const E* p, float (&v)[N]) {
     if constexpr (N == 4) {
-      const f32x4 q = load_as<STREAM>((const f32x4_any*)p);
+      const f32x4 q = STREAM ? __builtin_nontemporal_load((const f32x4_any*)p) : *(const f32x4_any*)p;
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] = q[i];
     } else {
-      const u32x4 q = load_as<STREAM>((const u32x4_any*)p);
+      const u32x4 q = STREAM ? __builtin_nontemporal_load((const u32x4_any*)p) : *(const u32x4_any*)p;
       unpack8(make_uint4(q[0], q[1], q[2], q[3]), v);
     }
   }
   static __device__ __forceinline__ void store(E* p, const float (&v)[N]) {
     if constexpr (N == 4)
-      store_as<true>((f32x4_any*)p, (f32x4_any)f32x4{v[0], v[1], v[2], v[3]});
+      __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, (f32x4_any*)p);
     else
-      store_as<true>((u32x4_any*)p, (u32x4_any)u32x4{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3]), bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7])});
+      __builtin_nontemporal_store(u32x4{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3]), bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7])},
+                                  (u32x4_any*)p);
   }
 };
 
