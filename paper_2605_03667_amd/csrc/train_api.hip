@@ -174,10 +174,14 @@ int elas_norm_join_bwd(const void* dh_out, const uint16_t* dn, const void* h_out
   }
   ELAS_CHECK(check_workspace(workspace, workspace_bytes, elas::norm_join_bwd_workspace_bytes(T, d)));
   elas::NormJoinArgs a{};
-  a.T = T; a.d = d; a.h = h_out; a.b = b; a.gate = gate; a.w_post = w_post; a.w_pre = w_pre;
+  a.T = T; a.d = d;
   a.res_scale = b ? res_scale : 1.f; a.block_scale = block_scale; a.eps = eps;
   a.res_f32 = (flags & ELAS_RES_F32) != 0; a.gate_token = gate_token;
-  a.dh_out = dh_out; a.dn = dn; a.dh = dh; a.db = db; a.dgate = dgate; a.dw_post = dw_post; a.dw_pre = dw_pre;
+  if (T > 0) {   // (without tokens no operand is checked, nor read: the sums are zeros whatever a gain holds)
+    a.h = h_out; a.b = b; a.gate = gate; a.w_post = w_post; a.w_pre = w_pre;
+    a.dh_out = dh_out; a.dn = dn; a.dh = dh; a.db = db;
+  }
+  a.dgate = dgate; a.dw_post = dw_post; a.dw_pre = dw_pre;
   a.ws = workspace;
   return device_status(elas::run_norm_join_bwd(a, (hipStream_t)stream), "norm join backward launch");
 }

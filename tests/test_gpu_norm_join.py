@@ -230,3 +230,18 @@ def test_gradient_against_differences():
         if got[key].dtype == BF:
             bound += np.sum(np.abs(u) * (ot.EPSBF16 * np.abs(_np(got[key])) + ot.TINY_BF16)) * 1.01
         assert abs(diff - np.sum(u * _np(got[key]))) <= bound, key
+
+
+@pytest.mark.parametrize("d", [24, 520, 768, 2048, 4096, 8192, 8200])
+def test_no_tokens_with_nonfinite_gains(d):
+    """The sums over no tokens are zeros, whatever the gains and the gate hold."""
+    for value in (float("inf"), float("nan")):
+        for res in (BF, F32):
+            c, dh, dn = _inputs(0, d, res, "shared", True, True, 1)
+            for k in ("gate", "w_post", "w_pre"):
+                c[k].fill_(value)
+            grads = {k: torch.full((d,), 7.0, device=DEV) for k in ("dgate", "dw_post", "dw_pre")}
+            got = elas.elas_norm_join_bwd(dh, dn, c["h"], **{k: c[k] for k in OPERANDS},
+                                          grads=dict(grads, dh=torch.empty_like(dh), db=torch.empty_like(dn)))
+            for k in grads:
+                assert torch.equal(got[k], torch.zeros_like(got[k])), (k, value)

@@ -1,0 +1,27 @@
+"""What the entry points of include/elas_train.h hand on to their launch sequences:
+the ABI layer compiled with launch sequences that only record their arguments.
+CPU only."""
+import os
+import subprocess
+
+import pytest
+
+from paper_2605_03667_amd import build
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HIPCC = "/opt/rocm/bin/hipcc"
+
+pytestmark = [pytest.mark.skipif(not os.path.exists(HIPCC), reason="ROCm toolchain absent"), pytest.mark.slow]
+
+
+def test_arguments_handed_on(tmp_path):
+    objs = []
+    for src in (os.path.join(build.CSRC, "train_api.hip"), os.path.join(ROOT, "tests", "sanitize", "train_calls.cpp")):
+        objs.append(str(tmp_path / (os.path.basename(src) + ".o")))
+        r = subprocess.run([HIPCC, "-x", "hip", "--cuda-host-only", *build.FLAGS, "-O1", "-c", src, "-o", objs[-1]], capture_output=True, text=True)
+        assert r.returncode == 0, r.stderr[-3000:]
+    exe = str(tmp_path / "train_calls")
+    r = subprocess.run([HIPCC, *objs, "-o", exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0 and "train calls: 0 failures" in r.stdout, r.stdout + r.stderr
