@@ -76,12 +76,13 @@ def _required(t, name):
 
 
 def _scratch(workspace, need: int, device: torch.device):
-    """The caller's workspace (bytes) or a new one: the tensor, its address and size."""
+    """The caller's workspace (bytes, on the operands' GPU ``device``) or a new one:
+    the tensor, its address and size."""
     if workspace is None:
         workspace = _workspace(need, device)
     if workspace is None:
         return None, None, 0
-    return workspace, _arg(workspace, (workspace.numel(),), torch.uint8, workspace.get_device(), "workspace"), workspace.numel()
+    return workspace, _arg(workspace, (workspace.numel(),), torch.uint8, device.index, "workspace"), workspace.numel()
 
 
 def _res_flag(dtype: torch.dtype, name: str) -> int:

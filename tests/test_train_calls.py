@@ -1,19 +1,20 @@
 """What the entry points of include/elas_train.h hand on to their launch sequences:
-the ABI layer compiled with launch sequences that only record their arguments.
-CPU only."""
+the ABI layer compiled with launch sequences that only record their arguments; and
+what the binding takes as a workspace.  CPU only."""
 import os
 import subprocess
 
 import pytest
+import torch
 
-from paper_2605_03667_amd import build
+from paper_2605_03667_amd import build, train
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HIPCC = "/opt/rocm/bin/hipcc"
 
-pytestmark = [pytest.mark.skipif(not os.path.exists(HIPCC), reason="ROCm toolchain absent"), pytest.mark.slow]
 
-
+@pytest.mark.slow
+@pytest.mark.skipif(not os.path.exists(HIPCC), reason="ROCm toolchain absent")
 def test_arguments_handed_on(tmp_path):
     objs = []
     for src in (os.path.join(build.CSRC, "train_api.hip"), os.path.join(ROOT, "tests", "sanitize", "train_calls.cpp")):
@@ -25,3 +26,17 @@ def test_arguments_handed_on(tmp_path):
     assert r.returncode == 0, r.stderr[-3000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0 and "train calls: 0 failures" in r.stdout, r.stdout + r.stderr
+
+
+class _OnDevice(torch.Tensor):
+    """Bytes that call themselves a tensor on GPU 1."""
+
+    def get_device(self):
+        return 1
+
+
+def test_workspace_on_the_operands_device():
+    ws = torch.zeros(64, dtype=torch.uint8).as_subclass(_OnDevice)
+    assert train._scratch(ws, 64, torch.device("cuda", 1))[2] == 64
+    with pytest.raises(ValueError, match="workspace must be a GPU tensor on device 0"):
+        train._scratch(ws, 64, torch.device("cuda", 0))
