@@ -7,7 +7,8 @@
  * device pointers owned by the caller, bf16 as uint16_t bit patterns, dense
  * row-major tensors, 16-byte aligned pointers (except where stated), arguments
  * checked on the host before anything is enqueued, everything asynchronous on
- * `stream`, nothing allocated.
+ * `stream`, nothing allocated.  The workspace sizes of sizes that no call takes
+ * are 0.
  */
 #ifndef ELAS_TRAIN_H
 #define ELAS_TRAIN_H

@@ -13,10 +13,12 @@ using elas::fail;
 namespace {
 
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;
+constexpr int64_t kMaxWidth = 65536;
+constexpr int64_t kMaxTensors = (int64_t(1) << 20) - 1;
 
 int check_rows(int64_t T, int64_t d) {
   if (T < 0 || T > kMaxRows) return fail(ELAS_ERR_SHAPE, "T=%lld out of range", (long long)T);
-  if (d <= 0 || d % 8 || d > 65536)
+  if (d <= 0 || d % 8 || d > kMaxWidth)
     return fail(ELAS_ERR_SHAPE, "d=%lld must be a positive multiple of 8, at most 65536", (long long)d);
   return ELAS_OK;
 }
@@ -69,7 +71,7 @@ int check_embed(int64_t T, int64_t V, int64_t d, float scale, uint32_t flags, ui
 }
 
 int check_grads(const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype, int64_t n) {
-  if (n < 0 || n >= (int64_t(1) << 20)) return fail(ELAS_ERR_SHAPE, "n=%lld out of range", (long long)n);
+  if (n < 0 || n > kMaxTensors) return fail(ELAS_ERR_SHAPE, "n=%lld out of range", (long long)n);
   if (n == 0) return ELAS_OK;
   if (!grads || !numel || !dtype) return fail(ELAS_ERR_NULL, "grads, numel or dtype is NULL");
   int64_t total = 0;
@@ -123,7 +125,7 @@ int elas_norm_join_fwd(const void* h, const uint16_t* b, const uint16_t* gate, c
 
 size_t elas_norm_join_bwd_workspace_bytes(int64_t T, int64_t d, uint32_t flags) {
   (void)flags;
-  if (T < 0 || d <= 0) return 0;
+  if (T < 0 || T > kMaxRows || d <= 0 || d > kMaxWidth) return 0;
   return elas::norm_join_bwd_workspace_bytes(T, d);
 }
 
@@ -201,7 +203,7 @@ int elas_embed_fwd(const void* ids, const uint16_t* table, int64_t T, int64_t V,
 }
 
 size_t elas_embed_bwd_workspace_bytes(int64_t T, int64_t V, int64_t d, uint32_t flags) {
-  if (T < 0 || V <= 0 || d <= 0) return 0;
+  if (T < 0 || T > kMaxRows || V <= 0 || V > kMaxRows || d <= 0 || d > kMaxWidth) return 0;
   return elas::embed_bwd_workspace_bytes(T, V, d, (flags & ELAS_EMBED_ADD) != 0);
 }
 
@@ -224,7 +226,7 @@ int elas_embed_bwd(const void* ids, const void* dx, int64_t T, int64_t V, int64_
   return device_status(elas::run_embed_bwd(a, (hipStream_t)stream), "embedding gradient launch");
 }
 
-size_t elas_grad_workspace_bytes(int64_t n) { return n < 0 ? 0 : elas::grad_workspace_bytes(n); }
+size_t elas_grad_workspace_bytes(int64_t n) { return n < 0 || n > kMaxTensors ? 0 : elas::grad_workspace_bytes(n); }
 
 int elas_grad_norm(const void* const* grads, const int64_t* numel, const int32_t* dtype, int64_t n, float* norm, void* workspace,
                    size_t workspace_bytes, void* stream) {

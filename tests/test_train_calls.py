@@ -1,12 +1,13 @@
 """What the entry points of include/elas_train.h hand on to their launch sequences:
 the ABI layer compiled with launch sequences that only record their arguments; and
-what the binding takes as a workspace.  CPU only."""
+workspaces, their sizes and the device they must be on.  CPU only."""
 import os
 import subprocess
 
 import pytest
 import torch
 
+import paper_2605_03667_amd as elas
 from paper_2605_03667_amd import build, train
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -40,3 +41,21 @@ def test_workspace_on_the_operands_device():
     assert train._scratch(ws, 64, torch.device("cuda", 1))[2] == 64
     with pytest.raises(ValueError, match="workspace must be a GPU tensor on device 0"):
         train._scratch(ws, 64, torch.device("cuda", 0))
+
+
+@pytest.mark.skipif(not os.path.exists(elas.LIB_PATH), reason="libelas.so not built")
+def test_workspace_of_sizes_out_of_range():
+    """No call takes these sizes; planning for them would leave the range of its integers."""
+    big = 2 ** 63 - 1
+    for T, d in ((big, 16), (1 << 31, 16), (4, big - 7), (4, 65544), (-1, 16), (4, 0)):
+        assert elas.elas_norm_join_bwd_workspace_bytes(T, d) == 0
+        for V in (10, 32000):
+            assert elas.elas_embed_bwd_workspace_bytes(T, V, d) == 0
+    for V in (big, 1 << 31, 0, -1):
+        assert elas.elas_embed_bwd_workspace_bytes(5000, V, 16) == 0
+    for n in (big, 1 << 20, -1):
+        assert elas.elas_grad_workspace_bytes(n) == 0
+    # the largest that are taken
+    assert elas.elas_norm_join_bwd_workspace_bytes((1 << 31) - 1, 65536) > 0
+    assert elas.elas_embed_bwd_workspace_bytes((1 << 31) - 1, (1 << 31) - 1, 65536) > 0
+    assert elas.elas_grad_workspace_bytes((1 << 20) - 1) > 0
