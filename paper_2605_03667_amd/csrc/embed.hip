@@ -176,17 +176,25 @@ struct SortInput {
 };
 __device__ __forceinline__ uint32_t input_key(const EmbedArgs& a, const SortInput& in, int64_t t) { return in.key ? in.key[t] : key_at(a, t); }
 
+// A workgroup's tokens are `tiles` consecutive ones of 1024 E (one, but where E is 8): every
+// scattering workgroup reads all workgroups' counts, so that there are kSortGroups of them
+// at most, two to a CU, whatever the number of tokens.
+constexpr int kSortGroups = 512;
+
 // hist[workgroup][digit]
 template <int E>
-__global__ __launch_bounds__(1024) void embed_hist_kernel(const EmbedArgs a, SortInput in, int shift, int bits, uint32_t* hist) {
+__global__ __launch_bounds__(1024) void embed_hist_kernel(const EmbedArgs a, SortInput in, int shift, int bits, int tiles, uint32_t* hist) {
   __shared__ uint32_t count[kDigits];
   const int bins = 1 << bits;
   if ((int)threadIdx.x < bins) count[threadIdx.x] = 0;
   __syncthreads();
+  for (int tile = 0; tile < (E == 8 ? tiles : 1); ++tile) {
+    const int64_t t0 = ((int64_t)blockIdx.x * (E == 8 ? tiles : 1) + tile) * (1024 * E);
 #pragma unroll
-  for (int r = 0; r < E; ++r) {
-    const int64_t t = (int64_t)blockIdx.x * (1024 * E) + r * 1024 + threadIdx.x;
-    if (t < a.T) atomicAdd(&count[(input_key(a, in, t) >> shift) & (uint32_t)(bins - 1)], 1u);
+    for (int r = 0; r < E; ++r) {
+      const int64_t t = t0 + r * 1024 + threadIdx.x;
+      if (t < a.T) atomicAdd(&count[(input_key(a, in, t) >> shift) & (uint32_t)(bins - 1)], 1u);
+    }
   }
   __syncthreads();
   if ((int)threadIdx.x < bins) hist[(int64_t)blockIdx.x * bins + threadIdx.x] = count[threadIdx.x];
@@ -195,20 +203,24 @@ __global__ __launch_bounds__(1024) void embed_hist_kernel(const EmbedArgs a, Sor
 // (Counting the next pass's digits here, with atomics, instead of in a launch of their own
 // was measured: 48 us instead of 10 + 5 at 65536 tokens, most of which share few digits.)
 template <int E>
-__global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, SortInput in, int shift, int bits, const uint32_t* hist,
-                                                             uint32_t* key_out, uint32_t* pos_out) {
+__global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, SortInput in, int shift, int bits, int tiles,
+                                                             const uint32_t* hist, uint32_t* key_out, uint32_t* pos_out) {
   __shared__ uint32_t count[16 * kDigits], base[kDigits], tmp[8];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int bins = 1 << bits;
   uint32_t k[E], pos[E], digit[E], rank[E];
   bool ok[E];
+  auto load = [&](int tile) __attribute__((always_inline)) {
+    const int64_t t0 = ((int64_t)blockIdx.x * (E == 8 ? tiles : 1) + tile) * (1024 * E);
 #pragma unroll
-  for (int r = 0; r < E; ++r) {
-    const int64_t t = (int64_t)blockIdx.x * (1024 * E) + (wave * E + r) * 64 + lane;
-    ok[r] = t < a.T;
-    k[r] = ok[r] ? input_key(a, in, t) : 0u;
-    pos[r] = ok[r] && in.pos ? in.pos[t] : (uint32_t)t;
-  }
+    for (int r = 0; r < E; ++r) {
+      const int64_t t = t0 + (wave * E + r) * 64 + lane;
+      ok[r] = t < a.T;
+      k[r] = ok[r] ? input_key(a, in, t) : 0u;
+      pos[r] = ok[r] && in.pos ? in.pos[t] : (uint32_t)t;
+    }
+  };
+  load(0);
   for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) count[i] = 0;
   // the digit's tokens in all workgroups and in those before this one
   uint32_t all = 0, before = 0;
@@ -222,18 +234,26 @@ __global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, 
   }
   const uint32_t first = bin_scan(all, bins, tmp);   // (its barrier: the counters are cleared)
   if ((int)threadIdx.x < bins) base[threadIdx.x] = first + before;
+  for (int tile = 0;;) {
 #pragma unroll
-  for (int r = 0; r < E; ++r) digit[r] = (k[r] >> shift) & (uint32_t)(bins - 1);
-  wave_ranks<E>(digit, ok, bits, count + wave * kDigits, rank);
-  __syncthreads();
-  wave_prefixes(count, bins);
-  __syncthreads();
+    for (int r = 0; r < E; ++r) digit[r] = (k[r] >> shift) & (uint32_t)(bins - 1);
+    wave_ranks<E>(digit, ok, bits, count + wave * kDigits, rank);
+    __syncthreads();
+    const uint32_t n = wave_prefixes(count, bins);
+    __syncthreads();
 #pragma unroll
-  for (int r = 0; r < E; ++r) {
-    if (!ok[r]) continue;
-    const uint32_t at = base[digit[r]] + count[wave * kDigits + digit[r]] + rank[r];
-    key_out[at] = k[r];
-    pos_out[at] = pos[r];
+    for (int r = 0; r < E; ++r) {
+      if (!ok[r]) continue;
+      const uint32_t at = base[digit[r]] + count[wave * kDigits + digit[r]] + rank[r];
+      key_out[at] = k[r];
+      pos_out[at] = pos[r];
+    }
+    if (E != 8 || ++tile == tiles) break;
+    load(tile);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) count[i] = 0;
+    if ((int)threadIdx.x < bins) base[threadIdx.x] += n;   // the next tile's lie behind this one's
+    __syncthreads();
   }
 }
 
@@ -660,7 +680,8 @@ int bit_length(int64_t v) {
 struct Plan {
   int passes, bits, tbits;
   bool few;            // one launch, embed_few_kernel
-  int per_thread;      // tokens of a thread in a pass
+  int per_thread;      // tokens of a thread in a tile
+  int tiles;           // of a workgroup
   int gbits;           // few: 2^gbits workgroups to a slice group
   int groups;
   int slice_groups;    // few: of sum.slices each
@@ -695,7 +716,9 @@ Plan plan(void* ws, int64_t T, int64_t V, int64_t d, bool add) {
     return p;
   }
   p.per_thread = T <= 131072 ? 1 : T <= (1 << 18) ? 4 : 8;
-  p.groups = (int)cdiv(T, 1024 * p.per_thread);
+  const int64_t tiles = cdiv(T, 1024 * p.per_thread);
+  p.tiles = (int)cdiv(tiles, kSortGroups);   // (up to 2^18 tokens there are fewer than that)
+  p.groups = (int)cdiv(tiles, p.tiles);
   // about 8 waves to a SIMD (1B, 65536 tokens: 133 us, 4 waves 139; 60M 49.3 and 46.6), and
   // not under a few tokens or rows to each
   const int64_t length = add ? T : T + kRowWeight * V;
@@ -726,11 +749,11 @@ hipError_t sort_passes(const EmbedArgs& a, const Plan& p, int& at, hipStream_t s
     const SortInput in = k == 0 ? SortInput{nullptr, nullptr} : SortInput{p.key[1 - to], p.pos[1 - to]};
     {
       TimedLaunch tl("embed_bwd_sort", stream);
-      hipLaunchKernelGGL(embed_hist_kernel<E>, grid, block, 0, stream, a, in, k * p.bits, p.bits, p.hist);
+      hipLaunchKernelGGL(embed_hist_kernel<E>, grid, block, 0, stream, a, in, k * p.bits, p.bits, p.tiles, p.hist);
     }
     TimedLaunch tl("embed_bwd_sort", stream);
-    hipLaunchKernelGGL(embed_scatter_kernel<E>, grid, block, 0, stream, a, in, k * p.bits, p.bits, (const uint32_t*)p.hist, p.key[to],
-                       p.pos[to]);
+    hipLaunchKernelGGL(embed_scatter_kernel<E>, grid, block, 0, stream, a, in, k * p.bits, p.bits, p.tiles, (const uint32_t*)p.hist,
+                       p.key[to], p.pos[to]);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     at = to;

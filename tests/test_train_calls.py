@@ -59,3 +59,14 @@ def test_workspace_of_sizes_out_of_range():
     assert elas.elas_norm_join_bwd_workspace_bytes((1 << 31) - 1, 65536) > 0
     assert elas.elas_embed_bwd_workspace_bytes((1 << 31) - 1, (1 << 31) - 1, 65536) > 0
     assert elas.elas_grad_workspace_bytes((1 << 20) - 1) > 0
+
+
+@pytest.mark.skipif(not os.path.exists(elas.LIB_PATH), reason="libelas.so not built")
+def test_sort_workspace_does_not_grow_with_the_square():
+    """Every workgroup of the sort reads all workgroups' counts (up to 2 KB each), so the
+    counts may not grow with the tokens: beside 16 bytes a token there are those and the
+    open sums of about 8192 chunks."""
+    for T in (1 << 22, 1 << 26, (1 << 31) - 1):
+        for V in (100, 32000, 1 << 27):
+            for flags in (0, elas.ELAS_EMBED_ADD):
+                assert elas.elas_embed_bwd_workspace_bytes(T, V, 8, flags) - 16 * T <= (1 << 20) + 9000 * 9 * 4 + 4096
