@@ -245,3 +245,14 @@ def test_no_tokens_with_nonfinite_gains(d):
                                           grads=dict(grads, dh=torch.empty_like(dh), db=torch.empty_like(dn)))
             for k in grads:
                 assert torch.equal(got[k], torch.zeros_like(got[k])), (k, value)
+
+
+@pytest.mark.parametrize("res", [BF, F32])
+@pytest.mark.parametrize("gate", ["shared", "token"])
+@pytest.mark.parametrize("post,pre", [(True, True), (False, True), (True, False)])
+@pytest.mark.parametrize("T,d", [(3100, 520), (1600, 1032), (800, 2056), (800, 4104), (800, 8200)])
+def test_several_rows_to_a_workgroup(T, d, post, pre, gate, res):
+    """More rows than the backward's workgroups take at once, at every number of waves
+    and pieces to a row (2, 4, 8 waves; 8 waves of two pieces; wider rows)."""
+    c, dh, dn = _inputs(T, d, res, gate, post, pre, T + d)
+    _verify(c, dh, dn, 0.75, 0.5, 1e-6)
