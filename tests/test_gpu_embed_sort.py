@@ -64,3 +64,25 @@ def test_order_of_several_tiles():
     got = elas.elas_embed_bwd(ids, dx, V)
     order = torch.argsort(ids, stable=True)
     assert torch.equal(elas.elas_embed_bwd(ids[order].contiguous(), dx[order].contiguous(), V), got)
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("kind", ["words", "uniform", "high"])
+@pytest.mark.parametrize("T", [131072, 131073, 262144, 262145, 1000003])
+def test_tokens_to_a_thread(T, kind, add):
+    """1 token of a tile to a thread up to 131072, 4 up to 262144, then 8."""
+    _check(T, 32000, kind, add, F32 if T % 2 else BF)
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("kind", ["words", "uniform", "high"])
+@pytest.mark.parametrize("V", [2 ** 18, 2 ** 27])
+@pytest.mark.parametrize("T", [8193, 20000, 140000])
+def test_three_and_four_passes(T, V, kind, add):
+    _check(T, V, kind, add)
+
+
+def test_one_pass():
+    for T in (8193, 131073, 300000):
+        for V in (1, 2, 511):
+            _check(T, V, "uniform", False)
