@@ -164,9 +164,10 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void join_fwd_kernel(const No
 // The sums over the tokens: acc[0] of dn xh, acc[1] of G bh (times the token's
 // gate where there is one for each), added up in the workgroup at the end and
 // written to row blockIdx.x of `part`, [grid][2][d].  Held to the registers that leave
-// a SIMD the 3 waves that the grid has for it (NV = 1; at 128, for 4, no faster).
+// a SIMD the waves that the grid has for it: 3, or 4 of workgroups of 8 (NV = 1; where it has
+// 3, at 128 registers, for 4, no faster), else 2.
 template <class R, int W, int NV, bool STREAM>
-__global__ __launch_bounds__(64 * (W < 4 ? 4 : W), NV == 1 ? 3 : 2) void join_bwd_kernel(const NormJoinArgs a, float* part) {
+__global__ __launch_bounds__(64 * (W < 4 ? 4 : W), NV > 1 ? 2 : W == 8 ? 4 : 3) void join_bwd_kernel(const NormJoinArgs a, float* part) {
   constexpr bool SPLIT = sizeof(R) == 4;
   using Lanes = RowLanes<W, NV, SPLIT>;
   __shared__ float red3[Lanes::WAVES][3], red1[Lanes::WAVES][1];
@@ -538,15 +539,21 @@ int64_t row_groups(int64_t T, int64_t d) {   // workgroups, at one row (or set o
 }
 // Forward: a workgroup per row or set of rows (1B, 65536 tokens, float32 stream: 269 us;
 // 2048 workgroups that go on to further rows 312).  Backward: each workgroup leaves a row
-// of partial sums, so no more than the card holds at once; of these, 3 waves to a SIMD, or 2
-// where a value of a row has 10 bytes or more to read.  More waves have more rows on their
-// way than the memory serves well, and it is whole waves to each SIMD that load it evenly:
-// 1B, 65536 tokens, bf16 (8 bytes): 2 waves 324 us, 2.5 305, 3 286, 3.5 332, 4 300; 350M,
-// 16381 tokens, float32, gate per token (14 bytes): 1.5 waves 73, 2 66, 3 71, 4 74.
+// of partial sums, so no more than the card holds at once; of these, of 4 waves each, 3 waves
+// to a SIMD, or 2 where a value of a row has 10 bytes or more to read.  More waves have more
+// rows on their way than the memory serves well, and it is whole waves to each SIMD that load
+// it evenly: 1B, 65536 tokens, bf16 (8 bytes): 2 waves 324 us, 2.5 305, 3 286, 3.5 332, 4 300;
+// 350M, 16381 tokens, float32, gate per token (14 bytes): 1.5 waves 73, 2 66, 3 71, 4 74.
+// Workgroups of 8 waves put 2 on every SIMD, so it is whole workgroups to each CU: 2, and 1
+// where the pieces' registers leave no room for a second.  Without post-norm and gate, bf16,
+// 256 workgroups / 384 / 512: rows of 2056 (32768) 256 / 211 / 166 us; 4096 (32768) 339 / 278 /
+// 275; 8192 (16384, two pieces) 308 / 370 / 311; with post-norm, gate per token and float32,
+// where 4-wave workgroups gain by having fewer: 396 / 315 / 286, 564 / 582 / 543, 520 / 598 / 530.
 int64_t fwd_grid(int64_t T, int64_t d) { return std::min<int64_t>(row_groups(T, d), 1 << 20); }
 int64_t bwd_grid(int64_t T, int64_t d, int waves_per_simd) {
-  const int waves = row_shape(d).waves == 8 ? 8 : 4;   // of a workgroup
-  return std::max<int64_t>(1, std::min<int64_t>(row_groups(T, d), 1024 * waves_per_simd / waves));
+  const RowShape s = row_shape(d);
+  const int to_a_cu = s.waves != 8 ? waves_per_simd : s.pieces == 1 ? 2 : 1;
+  return std::max<int64_t>(1, std::min<int64_t>(row_groups(T, d), 256 * to_a_cu));
 }
 constexpr int kMostWaves = 3;
 // Bytes of a row's value that the backward reads, and that it writes.

@@ -70,3 +70,12 @@ def test_sort_workspace_does_not_grow_with_the_square():
         for V in (100, 32000, 1 << 27):
             for flags in (0, elas.ELAS_EMBED_ADD):
                 assert elas.elas_embed_bwd_workspace_bytes(T, V, 8, flags) - 16 * T <= (1 << 20) + 9000 * 9 * 4 + 4096
+
+
+@pytest.mark.skipif(not os.path.exists(elas.LIB_PATH), reason="libelas.so not built")
+def test_norm_join_workgroups_fill_the_card_evenly():
+    """The backward's workgroups, one row of sums in the workspace each: a whole number of them
+    to each of the 256 CUs where there are rows for that."""
+    for d in (8, 512, 520, 1024, 1032, 2048, 2056, 4096, 4104, 6144, 8192, 8200, 65536):
+        rows, rest = divmod(elas.elas_norm_join_bwd_workspace_bytes(1 << 20, d), 2 * d * 4)
+        assert rest == 0 and rows % 256 == 0, d
