@@ -136,10 +136,12 @@ int elas_embed_bwd(const void* ids, const void* dx, int64_t T, int64_t V, int64_
  * dtype        HOST array of n types (ELAS_GRAD_F32 / ELAS_GRAD_BF16).
  * The three arrays are read before the call returns.  Tensors need the alignment
  * of their element only.
- * Squares and sums are held in 64 bits, so that no norm of finite values
- * overflows before it is rounded to float32; the order of the sum is fixed.
- * Where the norm is infinite or NaN the factor is 0 and the values are passed on
- * unscaled, so that a program can see what they hold and skip the step.
+ * Squares, sums and the norm are held in 64 bits, so that no norm of finite values
+ * overflows before it is rounded to float32; the order of the sum is fixed.  A norm
+ * beyond float32's range is reported as infinite and the factor, rounded to float32,
+ * with it, but the values are scaled by the factor of the 64-bit norm.
+ * Where a value is infinite or NaN the norm is, the factor is 0, and the values are
+ * passed on unscaled, so that a program can see what they hold and skip the step.
  * norm / stats: device float32 [1] / [2], 4-byte aligned.
  * Requires 0 <= n < 2^20, fewer than 2^44 values in all, max_norm >= 0 (+inf: never
  * clips).  workspace >= elas_grad_workspace_bytes(n) bytes.

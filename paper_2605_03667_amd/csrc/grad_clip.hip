@@ -115,12 +115,23 @@ __device__ __forceinline__ void square_piece(const E* g, int n, double (&s)[2]) 
   }
 }
 
+// A factor as the product of a normal float32 and a power of two, 1 where it is normal itself:
+// below 2^-126 a float32 has fewer bits, and none at all for a norm of values near 2^128.
+struct Factor {
+  float f, power;
+  __device__ __forceinline__ explicit Factor(double v) {
+    power = v < 0x1p-126 ? 0x1p-126f : 1.f;
+    f = (float)(v / (double)power);
+  }
+  __device__ __forceinline__ float operator()(float v) const { return v * f * power; }
+};
+
 template <class E>
-__device__ __forceinline__ void scale_piece(const E* g, E* out, int n, float f) {
+__device__ __forceinline__ void scale_piece(const E* g, E* out, int n, const Factor& f) {
   using P = Part<E>;
   auto scaled = [&](int at, float (&v)[P::N]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < P::N; ++i) v[i] *= f;
+    for (int i = 0; i < P::N; ++i) v[i] = f(v[i]);
     P::store(out + at, v);
   };
   if (n == kPiece) {
@@ -137,7 +148,7 @@ __device__ __forceinline__ void scale_piece(const E* g, E* out, int n, float f) 
     scaled(at, v);
   }
   const int i = n / P::N * P::N + (int)threadIdx.x;
-  if (i < n) set_value(out + i, value_of(g[i]) * f);
+  if (i < n) set_value(out + i, f(value_of(g[i])));
 }
 
 // Which tensor a piece belongs to: the last one whose first piece is not behind it.
@@ -205,10 +216,11 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(const Tensors<CAP> g, c
   const Finder<CAP> find(g);
   const double norm = norm_of(part, parts, red);
   const bool finite = norm < (double)INFINITY, clips = finite && norm > (double)max_norm;
-  const float factor = clips ? (float)((double)max_norm / norm) : 1.f;
+  const double factor = clips ? (double)max_norm / norm : 1.0;
+  const Factor scale(factor);
   if (stats && blockIdx.x == 0 && threadIdx.x == 0) {
     stats[0] = (float)norm;
-    stats[1] = finite ? factor : 0.f;
+    stats[1] = finite ? (float)factor : 0.f;
   }
   const uint32_t pieces = g.first[g.count];
   for (uint32_t i = blockIdx.x; i < pieces; i += gridDim.x) {
@@ -218,9 +230,9 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(const Tensors<CAP> g, c
     const int64_t at = (int64_t)(c - g.first[k]) * kPiece;
     const int n = g.values(c, k);
     if (g.is_bf16(k))
-      scale_piece((const uint16_t*)g.in[k] + at, (uint16_t*)o.out[k] + at, n, factor);
+      scale_piece((const uint16_t*)g.in[k] + at, (uint16_t*)o.out[k] + at, n, scale);
     else
-      scale_piece((const float*)g.in[k] + at, (float*)o.out[k] + at, n, factor);
+      scale_piece((const float*)g.in[k] + at, (float*)o.out[k] + at, n, scale);
   }
 }
 

@@ -152,3 +152,15 @@ def test_same_bits_every_time():
     first = elas.elas_grad_norm(g)
     for _ in range(3):
         assert torch.equal(elas.elas_grad_norm(elas.ElasTensors(g)), first)
+
+
+def test_factors_below_float32s_normal_range():
+    """max_norm / norm under 2^-126, where float32 has few bits or none: the values are
+    scaled by it all the same.  A rounding of the factor and one of the product, 2^-24 each."""
+    for value, max_norm in ((3e38, 1e-6), (3e38, 1e-3), (1e30, 1e-10), (-2e38, 3e-7)):
+        g = [torch.full((33,), value, device=DEV), torch.full((9000,), value, device=DEV)]
+        exact = np.copysign(float(np.float32(max_norm)) / 9033 ** 0.5, value)     # (every value is the same)
+        stats = elas.elas_grad_clip(g, max_norm)
+        assert 0 <= float(stats[1]) < 2.0 ** -126
+        for t in g:
+            assert ((t.double() - exact).abs() <= 2.02 * 2.0 ** -24 * abs(exact)).all(), (value, max_norm, float(t[0]), exact)
