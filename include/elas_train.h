@@ -131,7 +131,8 @@ int elas_embed_bwd(const void* ids, const void* dx, int64_t T, int64_t V, int64_
  *
  * grads, out   HOST arrays of n device pointers; out[k] has grads[k]'s type and
  *              length and is either grads[k] (in place) or overlaps no tensor.
- *              out NULL: in place.
+ *              out NULL: in place.  What is written overlaps no other tensor of
+ *              the lists: a tensor given twice would be scaled in a race.
  * numel        HOST array of n lengths >= 0 (a tensor of length 0 may be NULL).
  * dtype        HOST array of n types (ELAS_GRAD_F32 / ELAS_GRAD_BF16).
  * The three arrays are read before the call returns.  Tensors need the alignment

@@ -250,13 +250,15 @@ class ElasTensors:
         self._numel = (_i64 * n)()
         self._dtype = (ctypes.c_int32 * n)()
         self.layout = self._addresses = None
+        self._apart = False
         self.device = self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
 
     def __len__(self):
         return len(self.tensors)
 
-    def arrays(self):
-        """The host arrays of addresses, lengths and types."""
+    def arrays(self, written: bool = False):
+        """The host arrays of addresses, lengths and types; of tensors that the call
+        writes, no two may overlap."""
         ts = self.tensors
         addresses, layout = list(map(torch.Tensor.data_ptr, ts)), (list(map(torch.Tensor.numel, ts)), [t.dtype for t in ts])
         if addresses != self._addresses or layout != self.layout or not all(map(torch.Tensor.is_contiguous, ts)):
@@ -267,7 +269,12 @@ class ElasTensors:
                 _arg(t, t.shape, t.dtype, -1 if dev is None else dev, f"tensor {k}")
             self._pointers[:], self._numel[:] = addresses, layout[0]
             self._dtype[:] = [ELAS_GRAD_F32 if t == _F32 else ELAS_GRAD_BF16 for t in layout[1]]
-            self.layout, self._addresses = layout, addresses
+            self.layout, self._addresses, self._apart = layout, addresses, False
+        if written and not self._apart:
+            spans = sorted((a, a + n * t.itemsize) for a, n, t in zip(addresses, *layout) if n)
+            if any(end > start for (_, end), (start, _) in zip(spans, spans[1:])):
+                raise ValueError("tensors that are written must not overlap (one of them given twice?)")
+            self._apart = True
         return self._pointers, self._numel, self._dtype
 
 
@@ -298,15 +305,16 @@ def elas_grad_clip(grads, max_norm: float, out=None, stats: torch.Tensor | None 
                    workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Scales ``grads`` (a list of tensors or an ElasTensors) by factor =
     min(1, max_norm / norm), in place or into the tensors ``out`` of the same types
-    and lengths.  Returns stats, float32 [2] on the GPU: norm and factor.  Where the
-    norm is not finite the factor is 0 and the values are passed on unscaled."""
+    and lengths; no tensor that is written may overlap another.  Returns stats,
+    float32 [2] on the GPU: norm and factor.  Where a value is not finite the factor
+    is 0 and the values are passed on unscaled."""
     grads = _tensors(grads)
     dev = grads.device
-    pointers, numel, dtype = grads.arrays()
+    pointers, numel, dtype = grads.arrays(written=out is None)
     out_p = None
     if out is not None:
         out = _tensors(out)
-        out_p = out.arrays()[0]
+        out_p = out.arrays(written=True)[0]
         if out.layout != grads.layout or out.device != dev:
             raise ValueError("out must hold tensors of the same types, lengths and device as grads")
     if stats is None:

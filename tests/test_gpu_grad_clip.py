@@ -164,3 +164,24 @@ def test_factors_below_float32s_normal_range():
         assert 0 <= float(stats[1]) < 2.0 ** -126
         for t in g:
             assert ((t.double() - exact).abs() <= 2.02 * 2.0 ** -24 * abs(exact)).all(), (value, max_norm, float(t[0]), exact)
+
+
+def test_overlapping_tensors():
+    """What is written may not overlap (it would be scaled in a race); what is only read may."""
+    x = torch.ones(100, device=DEV)
+    for pair in ([x, x], [x, x[50:]], [x[:51], x[50:]], [x, x[99:], x[:0]]):
+        keep = x.clone()
+        with pytest.raises(ValueError, match="overlap"):
+            elas.elas_grad_clip(pair, 1.0)
+        with pytest.raises(ValueError, match="overlap"):
+            elas.elas_grad_clip([torch.ones_like(t) for t in pair], 1.0, out=pair)
+        assert torch.equal(x, keep)
+        out = [torch.zeros_like(t) for t in pair]
+        stats = elas.elas_grad_clip(pair, 1e9, out=out)
+        assert float(stats[0]) == pytest.approx(sum(t.numel() for t in pair) ** 0.5, rel=2.0 ** -22)
+        assert all(torch.equal(o, t) for o, t in zip(out, pair)) and elas.elas_grad_norm(pair)[0] == stats[0]
+    h = elas.ElasTensors([x[:50], x[50:], x[:0]])
+    assert elas.elas_grad_clip(h, 5.0)[1] == 0.5 and (x == 0.5).all()
+    h.tensors[1].set_(x[25:75])
+    with pytest.raises(ValueError, match="overlap"):
+        elas.elas_grad_clip(h, 5.0)
