@@ -176,20 +176,22 @@ struct SortInput {
 };
 __device__ __forceinline__ uint32_t input_key(const EmbedArgs& a, const SortInput& in, int64_t t) { return in.key ? in.key[t] : key_at(a, t); }
 
-// A workgroup's tokens are `tiles` consecutive ones of 1024 E (one, but where E is 8): every
+// A workgroup takes a tile of 1024 E tokens, or, MANY, `tiles` consecutive ones: every
 // scattering workgroup reads all workgroups' counts, so that there are kSortGroups of them
-// at most, two to a CU, whatever the number of tokens.
+// at most, two to a CU, whatever the number of tokens (60M's vocabulary, rows of 64: 32 M
+// tokens 2.9 ms, a tile to each of 4096 workgroups 4.9; 8 M 0.81 and 0.86; 4 M, of 512 tiles,
+// 0.47 with the loop over them and 0.42 without).
 constexpr int kSortGroups = 512;
 
 // hist[workgroup][digit]
-template <int E>
+template <int E, bool MANY>
 __global__ __launch_bounds__(1024) void embed_hist_kernel(const EmbedArgs a, SortInput in, int shift, int bits, int tiles, uint32_t* hist) {
   __shared__ uint32_t count[kDigits];
   const int bins = 1 << bits;
   if ((int)threadIdx.x < bins) count[threadIdx.x] = 0;
   __syncthreads();
-  for (int tile = 0; tile < (E == 8 ? tiles : 1); ++tile) {
-    const int64_t t0 = ((int64_t)blockIdx.x * (E == 8 ? tiles : 1) + tile) * (1024 * E);
+  for (int tile = 0; tile < (MANY ? tiles : 1); ++tile) {
+    const int64_t t0 = ((int64_t)blockIdx.x * (MANY ? tiles : 1) + tile) * (1024 * E);
 #pragma unroll
     for (int r = 0; r < E; ++r) {
       const int64_t t = t0 + r * 1024 + threadIdx.x;
@@ -202,16 +204,16 @@ __global__ __launch_bounds__(1024) void embed_hist_kernel(const EmbedArgs a, Sor
 
 // (Counting the next pass's digits here, with atomics, instead of in a launch of their own
 // was measured: 48 us instead of 10 + 5 at 65536 tokens, most of which share few digits.)
-template <int E>
-__global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, SortInput in, int shift, int bits, int tiles,
-                                                             const uint32_t* hist, uint32_t* key_out, uint32_t* pos_out) {
+template <int E, bool MANY>
+__global__ __launch_bounds__(1024, MANY ? 8 : 4) void embed_scatter_kernel(const EmbedArgs a, SortInput in, int shift, int bits, int tiles,
+                                                                           const uint32_t* hist, uint32_t* key_out, uint32_t* pos_out) {
   __shared__ uint32_t count[16 * kDigits], base[kDigits], tmp[8];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int bins = 1 << bits;
   uint32_t k[E], pos[E], digit[E], rank[E];
   bool ok[E];
   auto load = [&](int tile) __attribute__((always_inline)) {
-    const int64_t t0 = ((int64_t)blockIdx.x * (E == 8 ? tiles : 1) + tile) * (1024 * E);
+    const int64_t t0 = ((int64_t)blockIdx.x * (MANY ? tiles : 1) + tile) * (1024 * E);
 #pragma unroll
     for (int r = 0; r < E; ++r) {
       const int64_t t = t0 + (wave * E + r) * 64 + lane;
@@ -220,7 +222,7 @@ __global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, 
       pos[r] = ok[r] && in.pos ? in.pos[t] : (uint32_t)t;
     }
   };
-  load(0);
+  if (!MANY) load(0);   // (in the loop otherwise: both would not leave room for two workgroups)
   for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) count[i] = 0;
   // the digit's tokens in all workgroups and in those before this one
   uint32_t all = 0, before = 0;
@@ -235,6 +237,7 @@ __global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, 
   const uint32_t first = bin_scan(all, bins, tmp);   // (its barrier: the counters are cleared)
   if ((int)threadIdx.x < bins) base[threadIdx.x] = first + before;
   for (int tile = 0;;) {
+    if (MANY) load(tile);
 #pragma unroll
     for (int r = 0; r < E; ++r) digit[r] = (k[r] >> shift) & (uint32_t)(bins - 1);
     wave_ranks<E>(digit, ok, bits, count + wave * kDigits, rank);
@@ -248,8 +251,7 @@ __global__ __launch_bounds__(1024) void embed_scatter_kernel(const EmbedArgs a, 
       key_out[at] = k[r];
       pos_out[at] = pos[r];
     }
-    if (E != 8 || ++tile == tiles) break;
-    load(tile);
+    if (!MANY || ++tile == tiles) break;
     __syncthreads();
     for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) count[i] = 0;
     if ((int)threadIdx.x < bins) base[threadIdx.x] += n;   // the next tile's lie behind this one's
@@ -741,7 +743,7 @@ Plan plan(void* ws, int64_t T, int64_t V, int64_t d, bool add) {
   return p;
 }
 
-template <int E>
+template <int E, bool MANY = false>
 hipError_t sort_passes(const EmbedArgs& a, const Plan& p, int& at, hipStream_t stream) {
   const dim3 grid((unsigned)p.groups), block(1024);
   for (int k = 0; k < p.passes; ++k) {
@@ -749,10 +751,10 @@ hipError_t sort_passes(const EmbedArgs& a, const Plan& p, int& at, hipStream_t s
     const SortInput in = k == 0 ? SortInput{nullptr, nullptr} : SortInput{p.key[1 - to], p.pos[1 - to]};
     {
       TimedLaunch tl("embed_bwd_sort", stream);
-      hipLaunchKernelGGL(embed_hist_kernel<E>, grid, block, 0, stream, a, in, k * p.bits, p.bits, p.tiles, p.hist);
+      hipLaunchKernelGGL((embed_hist_kernel<E, MANY>), grid, block, 0, stream, a, in, k * p.bits, p.bits, p.tiles, p.hist);
     }
     TimedLaunch tl("embed_bwd_sort", stream);
-    hipLaunchKernelGGL(embed_scatter_kernel<E>, grid, block, 0, stream, a, in, k * p.bits, p.bits, p.tiles, (const uint32_t*)p.hist,
+    hipLaunchKernelGGL((embed_scatter_kernel<E, MANY>), grid, block, 0, stream, a, in, k * p.bits, p.bits, p.tiles, (const uint32_t*)p.hist,
                        p.key[to], p.pos[to]);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -814,7 +816,8 @@ hipError_t run_embed_bwd(const EmbedArgs& a, hipStream_t stream) {
     const hipError_t e = a.T <= kPlaced      ? place(a, p, stream)
                          : p.per_thread == 1 ? sort_passes<1>(a, p, at, stream)
                          : p.per_thread == 4 ? sort_passes<4>(a, p, at, stream)
-                                             : sort_passes<8>(a, p, at, stream);
+                         : p.tiles == 1      ? sort_passes<8>(a, p, at, stream)
+                                             : sort_passes<8, true>(a, p, at, stream);
     if (e != hipSuccess) return e;
   }
   {
