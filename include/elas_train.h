@@ -53,8 +53,8 @@ extern "C" {
  * h_out may be h, and n may be b (each row is read before it is written);
  * otherwise outputs overlap nothing.
  * All arithmetic and both means are float32 (a row of b or h' whose squares leave
- * its range has an infinite mean); h' and n are rounded once, n from the unrounded
- * h'.  A token whose row holds an infinity or NaN affects its own row only.
+ * its range has an infinite mean, or, with eps 0, a mean of 0); h' and n are rounded
+ * once, n from the unrounded h'.  A token whose row holds an infinity or NaN affects its own row only.
  * Requires T >= 0, d > 0, d % 8 == 0, d <= 65536, eps >= 0, finite scales.
  * T == 0 is a no-op (pointers are then not inspected and may be NULL).
  */

@@ -9,7 +9,7 @@
 // order) and then walks the sorted tokens and the table's rows together.  The sort
 // works on 4 to 8 bytes a token and is bound by latency and launches; the sum reads dx
 // and writes the table once and is bound by HBM.  1B, 65536 tokens whose ids fall off
-// like words: 133 us, of which the sort 2 (4.7 + 6.0), the sum 108 (4.9 TB/s), the
+// like words: 134 us, of which the sort 2 (4.7 + 6.3), the sum 109 (4.9 TB/s), the
 // joining of cut rows 6; with one id for all tokens 123.  Up to 4096 tokens one launch does
 // it all (60M, 2048 tokens, added: 11.0 us), up to 8192 three do.
 #include <algorithm>

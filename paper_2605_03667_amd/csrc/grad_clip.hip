@@ -9,9 +9,10 @@
 // long tensor and a hundred short ones load the card alike.  Bound by HBM: one read for
 // the norm, one read and one write for the scaling.  The scaling takes the pieces in
 // the opposite order, so that it begins with what the caches still hold (985 MB: 570 us,
-// in the same order 578).  985 MB in 193 tensors: 493 us, 6.0 TB/s over the three; 15.5 MB
-// in 49 tensors: 5.8 + 9.1 us of kernels, 23 us a call (the tensors' addresses, lengths,
-// types and layouts are read in every one); the norm alone of 985 MB 156 us (6.3 TB/s).
+// in the same order 578: measured before the last part was kept, below).  985 MB in 193
+// tensors: 490 us, 6.0 TB/s over the three; 15.5 MB in 49 tensors: 5.7 + 9.1 us of kernels, 24 us
+// a call (the tensors' addresses, lengths, types and layouts are read in every one); the norm
+// alone of 985 MB 156 us (6.3 TB/s).
 #include <math.h>
 
 #include <algorithm>

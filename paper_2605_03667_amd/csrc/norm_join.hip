@@ -19,15 +19,18 @@ namespace {
 // The sums over the tokens stay in registers over all rows of a workgroup; a second,
 // small launch adds up the workgroups' rows of them in a fixed order.
 //
-// W waves to a row rather than more pieces to a lane (NV = 1 up to 4096 features): 1B
-// backward, 65536 tokens: W = 4, NV = 1 315 us; W = 2, NV = 2 385 (it fills the registers,
-// and fewer waves are left to cover the loads).  For the same reason pieces stay packed
-// between their uses (344 -> 315) and gains are read once per workgroup.
+// W waves to a row rather than more pieces to a lane (NV = 1 up to 4096 features), for the
+// registers: the backward has 115 of them with one piece, 165 with two.  (1B backward, 65536
+// tokens, bf16: W = 4, NV = 1 285 us; W = 2, NV = 2 with 768 workgroups, of which 512 fit at
+// once, 275, with 512 291; other widths and the float32 stream were not measured so.)  For the
+// same reason pieces stay packed between their uses (without that 135 and 246 registers, and
+// spills at W = 8; 1B 285 us either way) and gains are read once per workgroup.
 //
-// Measured, bytes that the call cannot do without over its time: forward 1B, 65536 tokens,
-// float32 stream 264 us (6.1 TB/s; a copy of 1 GiB reaches 5.5); 350M, 2000 tokens 6.3 us
-// of kernel; 1B, 16 tokens 3.6.  Backward 1B, 65536 tokens 285 us (5.7 TB/s); 350M, 16381
-// tokens, gate per token, float32 stream 66 us (5.6); 60M, 2048 tokens 4.9 + 3.4 us.
+// Measured, bytes that the call cannot do without over the call's time: forward 1B, 65536
+// tokens, float32 stream 265 us (6.1 TB/s; a copy of 1 GiB reaches 5.5); 350M, 2000 tokens
+// 6.2 us of kernel; 1B, 16 tokens 3.7.  Backward 1B, 65536 tokens 290 us (5.6 TB/s; kernels 281
+// + 5); 350M, 16381 tokens, gate per token, float32 stream 67 us (5.5); 60M, 2048 tokens
+// 5.0 + 3.4 us of kernels.
 
 // Where a thread's row and pieces lie; loads and stores of piece v.
 template <int W, int NV, bool SPLIT>
@@ -565,9 +568,9 @@ int bwd_writes(const NormJoinArgs& a) { return (a.dh ? a.res_f32 ? 4 : 2 : 0) + 
 int64_t bwd_grid(const NormJoinArgs& a) { return bwd_grid(a.T, a.d, bwd_reads(a) >= 10 ? 2 : kMostWaves); }
 
 // Backward loads go past the caches where the call moves more than the last-level
-// cache's 256 MB (1B, 65536 tokens 316 -> 306 us); in a smaller one they would miss what
-// that cache holds (350M, 8192 tokens 24.8 -> 30.3).  Forward loads never gained (1B 280
-// -> 288).  Stores: kStreamStores in the forward, always in the backward.
+// cache's 256 MB (1B, 65536 tokens 298 -> 285 us; 350M, 16381 tokens, float32, gate per token 70
+// -> 66); in a smaller one they would miss what that cache holds (350M, 8192 tokens 24.8 ->
+// 30.3).  Forward loads never gained (1B 280 -> 288).  Stores: kStreamStores in the forward, always in the backward.
 constexpr int64_t kStreamLoads = int64_t(1) << 28;   // bytes
 
 template <class R, bool STREAM>
