@@ -8,7 +8,8 @@ kernels of ``libelas.so``; there is no fallback: if the library is not built,
 or a tensor is not on the GPU, the call raises.
 
 The operators around the FFN in a training step (norms, embedding, gradient
-clipping; ``include/elas_train.h``) are in ``train`` and exported here too.
+clipping; ``include/elas_train.h``) are in ``train``, its losses (``include/elas_loss.h``)
+in ``loss`` and its update (``include/elas_adamw.h``) in ``adamw``; all are exported here too.
 
 bf16 tensors use ``torch.bfloat16``; the compressed 2:4 metadata uses
 ``torch.uint8``; weight gradients are ``torch.float32``.
@@ -432,5 +433,9 @@ def elas_timing_collect() -> dict:
 
 from . import train  # noqa: E402  (needs the names above)
 from .train import *  # noqa: E402,F401,F403
+from . import loss  # noqa: E402  (needs train's)
+from .loss import *  # noqa: E402,F401,F403
+from . import adamw  # noqa: E402  (needs both)
+from .adamw import *  # noqa: E402,F401,F403
 
-__all__ += train.__all__
+__all__ += train.__all__ + loss.__all__ + adamw.__all__

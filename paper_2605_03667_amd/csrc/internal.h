@@ -129,6 +129,65 @@ size_t grad_workspace_bytes(int64_t n);
 hipError_t run_grad_norm(const void* const* grads, void* const* out, const int64_t* numel, const int32_t* dtype, int64_t n,
                          bool clip, float max_norm, float* stats, void* ws, hipStream_t stream);
 
+// Arguments of the calls on logits (include/elas_loss.h).
+struct LogitsArgs {
+  enum Kind { LOGP, TOKEN, POLICY };
+  Kind kind;
+  int64_t T, V, ld, ld_out;
+  const void *logits, *ids;
+  bool f32, ids_i64;
+  float scale, reduce;
+  const float *weight, *advantage, *old_logp, *ref_logp;
+  float z_coef, low, high, kl_coef;   // low, high: the clamp's bounds
+  float *logp, *lse, *stats;
+  void* dlogits;
+  const float *dlogp, *dlse, *lse_in;   // backward
+  void* ws;
+};
+
+// token_loss.hip
+size_t token_loss_workspace_bytes(int64_t T, int64_t V, bool f32);
+hipError_t run_token_loss(const LogitsArgs& a, hipStream_t stream);
+hipError_t run_token_logp_bwd(const LogitsArgs& a, hipStream_t stream);
+
+// Arguments of the preference loss.
+struct PreferenceArgs {
+  int64_t N, pairs;
+  const float *logp, *ref;
+  const void* offsets;
+  bool i64;
+  float beta, smoothing;
+  float *margin, *dlogp, *stats;
+  void* ws;
+};
+
+// preference.hip
+size_t preference_workspace_bytes(int64_t pairs);
+hipError_t run_preference(const PreferenceArgs& a, hipStream_t stream);
+
+// Arguments of a step of AdamW (include/elas_adamw.h); host arrays of n.
+struct AdamwArgs {
+  void* const* params;
+  const void* const* grads;
+  uint16_t* const* copies;
+  const int64_t* numel;
+  const int32_t *param_dtype, *grad_dtype;
+  const float* decay;
+  int64_t n;
+  bool eight;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  int64_t* step;
+  double rate, beta1, beta2, eps, max_norm;
+  const float *rate_factor, *norm;
+  void* ws;
+};
+
+// adamw.hip
+size_t adamw_workspace_bytes();
+hipError_t run_adamw(const AdamwArgs& a, hipStream_t stream);
+hipError_t run_adam8_values(const uint8_t* codes, const float* scale, int64_t blocks, bool second, bool f32, void* out, hipStream_t stream);
+
 // ffn.hip
 size_t spmm_workspace_bytes(int64_t K, int64_t N, int b_layout);
 size_t fwd_workspace_bytes(int64_t T, int64_t d, int64_t F, int64_t r, bool dense, bool ab, bool lean = false);

@@ -1,12 +1,14 @@
 // C-ABI layer of the operators around the FFN (include/elas_train.h): argument
 // checks on the host, before anything is enqueued.
-#include <math.h>
-
 #include "../../include/elas_train.h"
-#include "internal.h"
+#include "checks.h"
 
 using elas::begin_call;
+using elas::check_absent;
+using elas::check_elem_ptr;
 using elas::check_ptr;
+using elas::check_scale;
+using elas::check_workspace;
 using elas::device_status;
 using elas::fail;
 
@@ -21,28 +23,6 @@ int check_rows(int64_t T, int64_t d) {
   if (d <= 0 || d % 8 || d > kMaxWidth)
     return fail(ELAS_ERR_SHAPE, "d=%lld must be a positive multiple of 8, at most 65536", (long long)d);
   return ELAS_OK;
-}
-
-int check_scale(float v, const char* name) {
-  if (!isfinite(v)) return fail(ELAS_ERR_SHAPE, "%s must be finite", name);
-  return ELAS_OK;
-}
-
-// Alignment of a pointer that only needs its element's; NULL is an error.
-int check_elem_ptr(const void* p, size_t size, const char* name) {
-  if (p == nullptr) return fail(ELAS_ERR_NULL, "%s is NULL", name);
-  if ((uintptr_t)p % size) return fail(ELAS_ERR_ALIGN, "%s is not %zu-byte aligned", name, size);
-  return ELAS_OK;
-}
-
-int check_absent(const void* p, const char* name, const char* needs) {
-  if (p != nullptr) return fail(ELAS_ERR_FLAGS, "%s is given without %s", name, needs);
-  return ELAS_OK;
-}
-
-int check_workspace(const void* ws, size_t have, size_t need) {
-  if (have < need) return fail(ELAS_ERR_WORKSPACE, "workspace %zu bytes, %zu needed", have, need);
-  return need ? check_ptr(ws, "workspace") : ELAS_OK;
 }
 
 // Sizes, flags and which operands belong together, for both directions.
