@@ -2,6 +2,8 @@
 // their elements: N consecutive values, 16 bytes of float32 or bf16 (or 8 of bf16).
 #pragma once
 
+#include <math.h>
+
 #include "rows.h"
 
 namespace elas {
@@ -63,11 +65,18 @@ struct Span;
 template <>
 struct Span<float> : Four<float> {
   static constexpr int N = 4;
+  __device__ __forceinline__ void set(int i, float v) { q[i] = v; }
+  __device__ __forceinline__ void keep_packed() {}
+  // -inf everywhere
+  __device__ __forceinline__ void clear() { q = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY}; }
 };
 template <>
 struct Span<uint16_t> {
   static constexpr int N = 8;
   u32x4 q;
+  __device__ __forceinline__ void clear() { q = u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}; }
+  // Keeps the compiler from holding the values as 8 floats instead of 4 words from here on.
+  __device__ __forceinline__ void keep_packed() { asm volatile("" : "+v"(q)); }
   template <bool STREAM>
   __device__ __forceinline__ void load(const uint16_t* p) {
     q = STREAM ? __builtin_nontemporal_load((const u32x4_span*)p) : *(const u32x4_span*)p;

@@ -18,7 +18,7 @@ namespace elas {
 
 namespace {
 
-constexpr int kGroups = 2048;            // most workgroups that take rows
+constexpr int kGroups = 8192;            // most workgroups that take rows
 constexpr int kSums = 3;                 // statistics of a workgroup
 constexpr float kLowest = -0x1.fffffep127f;
 constexpr float kLog2E = 0x1.715476p0f;
@@ -121,121 +121,283 @@ __device__ __forceinline__ Terms row_terms(const Rows& a, int64_t t, float w, fl
   return r;
 }
 
-template <int KIND, class E, int WAVES, bool GRAD>
-__global__ __launch_bounds__(WAVES * 64) void rows_kernel(const Rows a) {
-  using S = Span<E>;
-  constexpr int N = S::N, TH = WAVES * 64;
-  __shared__ float red[2][2 * WAVES + 1];
+// How a row is cut: pieces of 16 bytes from `lead` on, the first that is aligned in the matrix
+// that is written (or, without one, read), `full` of them; and the values in front of and behind them,
+// one to a thread.
+template <class E>
+struct Cut {
+  static constexpr int N = Span<E>::N;
+  int lead, full, edges;
+  __device__ __forceinline__ Cut(const E* row, int V) {
+    lead = (int)(-(uintptr_t)row % 16 / sizeof(E));
+    if (lead > V) lead = V;
+    full = (V - lead) / N;
+    edges = V - full * N;
+  }
+  // place of a thread's value outside the pieces; only the first `edges` threads have one
+  __device__ __forceinline__ int edge(int tid) const { return tid < lead ? tid : full * N + tid; }
+};
+
+// A thread's place `i` values behind a row's uniform one: a 32-bit offset, so that the address stays in scalar registers.
+template <class E>
+__device__ __forceinline__ E* at_value(E* uniform, int i) {
+  return (E*)((char*)uniform + (uint32_t)i * (uint32_t)sizeof(E));
+}
+template <class E>
+__device__ __forceinline__ const E* at_value(const E* uniform, int i) {
+  return (const E*)((const char*)uniform + (uint32_t)i * (uint32_t)sizeof(E));
+}
+
+// Maximum and sum of a thread's pieces i, i + stride .. of a row and of an edge, 4 pieces at a time.
+template <class E, bool STREAM>
+__device__ __forceinline__ void add_pieces(MaxSum& r, float c, const E* pieces, int i, int full, int stride) {
+  constexpr int N = Span<E>::N, AT_ONCE = 4;
+  for (; i < full; i += AT_ONCE * stride) {
+    Span<E> p[AT_ONCE];
+#pragma unroll
+    for (int q = 0; q < AT_ONCE; ++q) {
+      p[q].clear();
+      if (i + q * stride < full) p[q].template load<STREAM>(at_value(pieces, (i + q * stride) * N));
+    }
+    float m = r.m;
+#pragma unroll
+    for (int q = 0; q < AT_ONCE; ++q)
+#pragma unroll
+      for (int k = 0; k < N; ++k) m = fmaxf(m, p[q].get(k));
+    r.rescale(m, c);
+#pragma unroll
+    for (int q = 0; q < AT_ONCE; ++q)
+#pragma unroll
+      for (int k = 0; k < N; ++k) r.s += __builtin_amdgcn_exp2f((p[q].get(k) - m) * c);
+  }
+}
+__device__ __forceinline__ void add_value(MaxSum& r, float c, float v) {
+  r.rescale(fmaxf(r.m, v), c);
+  r.s += __builtin_amdgcn_exp2f((v - r.m) * c);
+}
+__device__ __forceinline__ void add(MaxSum& r, float c, const MaxSum& o) {
+  const float m = fmaxf(r.m, o.m);
+  r.rescale(m, c);
+  r.s += o.s * __builtin_amdgcn_exp2f((o.m - m) * c);
+}
+
+// The threads' maxima and sums to the row's, in every thread; returns the label's logit.  `lds` holds
+// 2 WAVES + 1 floats; used in turn, two of them need no other barrier.
+template <int WAVES, class E>
+__device__ __forceinline__ float whole_row(MaxSum& r, float c, const E* label, float* lds) {
   const int tid = threadIdx.x;
+  r.rescale(wave_max(r.m), c);
+  r.s = wave_sum(r.s);
+  if constexpr (WAVES == 1) return span_value(*label);
+  if ((tid & 63) == 0) lds[tid >> 6] = r.m, lds[WAVES + (tid >> 6)] = r.s;
+  if (tid == 0) lds[2 * WAVES] = span_value(*label);   // before any wave writes the row in place
+  __syncthreads();
+  float m = lds[0], s = 0.f;
+#pragma unroll
+  for (int k = 1; k < WAVES; ++k) m = fmaxf(m, lds[k]);
+#pragma unroll
+  for (int k = 0; k < WAVES; ++k) s += lds[WAVES + k] * __builtin_amdgcn_exp2f((lds[k] - m) * c);
+  r.m = m, r.s = s;
+  return lds[2 * WAVES];
+}
+
+// Waves to a row; a workgroup of rows of one wave takes kRowsOfOne of them.
+constexpr int kRowsOfOne = 4;
+template <int WAVES>
+struct Team {
+  static constexpr int THREADS = WAVES * 64, ROWS = WAVES == 1 ? kRowsOfOne : 1;
+};
+
+// Which of its workgroup's rows a wave's team takes, in a scalar register.
+template <int WAVES>
+__device__ __forceinline__ int wave_row() {
+  return WAVES == 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0;
+}
+
+// A team's statistics, in shared memory: its first thread adds to them, and the workgroup's
+// first threads add up the teams'.
+template <int WAVES>
+struct Sums {
+  double (*all)[kSums];
+  __device__ __forceinline__ explicit Sums(double (*lds)[kSums]) : all(lds + wave_row<WAVES>()) {
+    if (threadIdx.x % Team<WAVES>::THREADS == 0)
+#pragma unroll
+      for (int k = 0; k < kSums; ++k) (*all)[k] = 0.0;
+  }
+  __device__ __forceinline__ void add(const double (&v)[kSums]) {
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) (*all)[k] += v[k];
+  }
+  static __device__ __forceinline__ void write(const double (*lds)[kSums], double* part) {
+    __syncthreads();
+    if (threadIdx.x < kSums) {
+      double v = lds[0][threadIdx.x];
+#pragma unroll
+      for (int w = 1; w < Team<WAVES>::ROWS; ++w) v += lds[w][threadIdx.x];
+      part[(int64_t)blockIdx.x * kSums + threadIdx.x] = v;
+    }
+  }
+};
+
+__device__ __forceinline__ void write_row(const Rows& a, int64_t t, float logp, float lse) {
+  if (a.logp) a.logp[t] = logp;
+  if (a.lse) a.lse[t] = lse;
+}
+
+// Without a gradient: a row once through its team.
+template <int KIND, class E, int WAVES>
+__global__ __launch_bounds__(Team<WAVES>::THREADS * Team<WAVES>::ROWS) void rows_kernel(const Rows a) {
+  constexpr int TH = Team<WAVES>::THREADS, ROWS = Team<WAVES>::ROWS;
+  __shared__ float red[2][2 * WAVES + 1];
+  const int tid = threadIdx.x % TH;
   const float c = a.scale * kLog2E;
-  const int full = a.V / N, rest = a.V - full * N;       // whole pieces, and values behind them
-  double sum[kSums] = {0.0, 0.0, 0.0};
+  __shared__ double sums[ROWS][kSums];
+  Sums<WAVES> sum(sums);
   int turn = 0;
-  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+  for (int64_t t = (int64_t)blockIdx.x * ROWS + wave_row<WAVES>(); t < a.T; t += (int64_t)gridDim.x * ROWS) {
     const int64_t id = id_of(a.ids, a.ids_i64, t);
     const float w = KIND != LogitsArgs::LOGP && a.weight ? a.weight[t] : 1.f;
-    const E* x = (const E*)a.logits + t * a.ld;
-    E* d = GRAD ? (E*)a.dlogits + t * a.ld_out : nullptr;
     if (id < 0 || id >= a.V || w == 0.f) {
-      if (GRAD) {
-        const float zero[N] = {};
-        for (int i = tid; i < full; i += TH) S::template store<false>(d + i * N, zero);
-        if (tid < rest) set_span_value(d + full * N + tid, 0.f);
-      }
-      if (tid == 0) {
-        if (a.logp) a.logp[t] = 0.f;
-        if (a.lse) a.lse[t] = 0.f;
-      }
+      if (tid == 0) write_row(a, t, 0.f, 0.f);
       continue;
     }
+    const E* x = (const E*)a.logits + t * a.ld;
+    const Cut<E> cut(x, a.V);
     MaxSum r;
-    for (int i = tid; i < full; i += TH) {
-      S p;
-      p.template load<false>(x + i * N);
-      float m = r.m;
-#pragma unroll
-      for (int k = 0; k < N; ++k) m = fmaxf(m, p.get(k));
-      r.rescale(m, c);
-#pragma unroll
-      for (int k = 0; k < N; ++k) r.s += __builtin_amdgcn_exp2f((p.get(k) - m) * c);
-    }
-    if (tid < rest) {
-      const float v = span_value(x[full * N + tid]);
-      r.rescale(fmaxf(r.m, v), c);
-      r.s += __builtin_amdgcn_exp2f((v - r.m) * c);
-    }
-    r.rescale(wave_max(r.m), c);
-    r.s = wave_sum(r.s);
-    float label;
-    if (WAVES > 1) {
-      // (two buffers in turn: one barrier a row)
-      float* lds = red[turn];
-      turn ^= 1;
-      if ((tid & 63) == 0) lds[tid >> 6] = r.m, lds[WAVES + (tid >> 6)] = r.s;
-      if (tid == 0) lds[2 * WAVES] = span_value(x[id]);   // before any wave writes the row in place
-      __syncthreads();
-      label = lds[2 * WAVES];
-      float m = lds[0];
-#pragma unroll
-      for (int k = 1; k < WAVES; ++k) m = fmaxf(m, lds[k]);
-      float s = 0.f;
-#pragma unroll
-      for (int k = 0; k < WAVES; ++k) s += lds[WAVES + k] * __builtin_amdgcn_exp2f((lds[k] - m) * c);
-      r.m = m, r.s = s;
-    } else {
-      label = span_value(x[id]);
-    }
+    add_pieces<E, false>(r, c, x + cut.lead, tid, cut.full, TH);
+    if (tid < cut.edges) add_value(r, c, span_value(x[cut.edge(tid)]));
+    const float label = whole_row<WAVES>(r, c, x + id, red[turn]);
+    turn ^= 1;
     float logp, lse;
     const Terms o = row_terms<KIND>(a, t, w, label, r, &logp, &lse);
     if (tid == 0) {
-      if (a.logp) a.logp[t] = logp;
-      if (a.lse) a.lse[t] = lse;
-#pragma unroll
-      for (int k = 0; k < kSums; ++k) sum[k] += o.sum[k];
-    }
-    if (!GRAD) continue;
-    const int at = (int)id;
-    for (int i = tid; i < full; i += TH) {
-      S p;
-      p.template load<false>(x + i * N);
-      float v[N];
-#pragma unroll
-      for (int k = 0; k < N; ++k) v[k] = __builtin_amdgcn_exp2f((p.get(k) - r.m) * c) * o.all;
-      if ((unsigned)(at - i * N) < (unsigned)N) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += at - i * N == k ? o.label : 0.f;
-      }
-      S::template store<false>(d + i * N, v);
-    }
-    if (tid < rest) {
-      const int i = full * N + tid;
-      const float v = __builtin_amdgcn_exp2f((span_value(x[i]) - r.m) * c) * o.all;
-      set_span_value(d + i, at == i ? v + o.label : v);
+      write_row(a, t, logp, lse);
+      if (KIND != LogitsArgs::LOGP) sum.add(o.sum);
     }
   }
-  if (KIND != LogitsArgs::LOGP && tid == 0) {
-#pragma unroll
-    for (int k = 0; k < kSums; ++k) a.part[(int64_t)blockIdx.x * kSums + k] = sum[k];
-  }
+  if (KIND != LogitsArgs::LOGP) sum.write(sums, a.part);
 }
 
-__global__ __launch_bounds__(256) void loss_sum_kernel(const double* part, int groups, int count, float* stats) {
-  __shared__ double red[4];
+// A loss with its gradient, the row in the registers of its team: PARTS pieces to a thread, what lies
+// behind the row -inf.  BEYOND: a longer row, whose pieces behind those are read twice.
+template <int KIND, class E, int WAVES, int PARTS, bool BEYOND>
+__global__ __launch_bounds__(Team<WAVES>::THREADS * Team<WAVES>::ROWS) void held_kernel(const Rows a) {
+  using S = Span<E>;
+  constexpr int N = S::N, TH = Team<WAVES>::THREADS, ROWS = Team<WAVES>::ROWS;
+  constexpr bool KEEP = N == 4;      // float32: the exponentials take the logits' place
+  __shared__ float red[2][2 * WAVES + 1];
+  const int tid = threadIdx.x % TH;
+  const float c = a.scale * kLog2E;
+  __shared__ double sums[ROWS][kSums];
+  Sums<WAVES> sum(sums);
+  int turn = 0;
+  for (int64_t t = (int64_t)blockIdx.x * ROWS + wave_row<WAVES>(); t < a.T; t += (int64_t)gridDim.x * ROWS) {
+    const int64_t id = id_of(a.ids, a.ids_i64, t);
+    const float w = a.weight ? a.weight[t] : 1.f;
+    const E* x = (const E*)a.logits + t * a.ld;
+    E* d = (E*)a.dlogits + t * a.ld_out;
+    const Cut<E> cut(d, a.V);
+    const E* xp = x + cut.lead;
+    E* dp = d + cut.lead;
+    if (id < 0 || id >= a.V || w == 0.f) {
+      const float zero[N] = {};
+      for (int i = tid; i < cut.full; i += TH) S::template store<true>(dp + i * N, zero);
+      if (tid < cut.edges) set_span_value(d + cut.edge(tid), 0.f);
+      if (tid == 0) write_row(a, t, 0.f, 0.f);
+      continue;
+    }
+    S p[PARTS];
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q) {
+      p[q].clear();
+      if (tid + q * TH < cut.full) p[q].template load<true>(at_value(xp + q * TH * N, tid * N));
+    }
+    const float edge = tid < cut.edges ? span_value(x[cut.edge(tid)]) : -INFINITY;
+    MaxSum r;
+    r.m = fmaxf(r.m, edge);
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+      for (int k = 0; k < N; ++k) r.m = fmaxf(r.m, p[q].get(k));
+    const float own = r.m;
+    r.s = __builtin_amdgcn_exp2f((edge - own) * c);
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q) p[q].keep_packed();
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const float e = __builtin_amdgcn_exp2f((p[q].get(k) - own) * c);
+        if constexpr (KEEP) p[q].set(k, e);
+        r.s += e;
+      }
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q) p[q].keep_packed();
+    if constexpr (BEYOND) {
+      MaxSum more;
+      add_pieces<E, false>(more, c, xp, tid + PARTS * TH, cut.full, TH);
+      add(r, c, more);
+    }
+    const float label = whole_row<WAVES>(r, c, x + id, red[turn]);
+    turn ^= 1;
+    float logp, lse;
+    const Terms o = row_terms<KIND>(a, t, w, label, r, &logp, &lse);
+    if (tid == 0) {
+      write_row(a, t, logp, lse);
+      sum.add(o.sum);
+    }
+    const int at = (int)id - cut.lead;      // the label's place among the pieces
+    const auto put = [&](int first, float (&v)[N]) __attribute__((always_inline)) {     // piece first + tid
+      const int in = at - first * N - tid * N;
+      if ((unsigned)in < (unsigned)N) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += in == k ? o.label : 0.f;
+      }
+      if (first + tid < cut.full) S::template store<true>(at_value(dp + first * N, tid * N), v);
+    };
+    const float all = KEEP ? o.all * __builtin_amdgcn_exp2f((own - r.m) * c) : o.all;
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q) {
+      float v[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[k] = (KEEP ? p[q].get(k) : __builtin_amdgcn_exp2f((p[q].get(k) - r.m) * c)) * all;
+      put(q * TH, v);
+    }
+    if constexpr (BEYOND) {
+#pragma unroll 4
+      for (int first = PARTS * TH; first + tid < cut.full; first += TH) {
+        S more;
+        more.template load<true>(at_value(xp + first * N, tid * N));
+        float v[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = __builtin_amdgcn_exp2f((more.get(k) - r.m) * c) * o.all;
+        put(first, v);
+      }
+    }
+    if (tid < cut.edges) {
+      const float v = __builtin_amdgcn_exp2f((edge - r.m) * c) * o.all;
+      set_span_value(d + cut.edge(tid), cut.edge(tid) == (int)id ? v + o.label : v);
+    }
+  }
+  sum.write(sums, a.part);
+}
+
+__global__ __launch_bounds__(1024) void loss_sum_kernel(const double* part, int groups, int count, float* stats) {
+  __shared__ double red[16];
   double s[kSums] = {0.0, 0.0, 0.0};
-  for (int g = threadIdx.x; g < groups; g += 256) {
+  for (int g = threadIdx.x; g < groups; g += 1024) {
 #pragma unroll
     for (int k = 0; k < kSums; ++k) s[k] += part[(int64_t)g * kSums + k];
   }
 #pragma unroll
   for (int k = 0; k < kSums; ++k) {
-    const double v = block_sum<4>(s[k], red);
+    const double v = block_sum<16>(s[k], red);
     if (threadIdx.x == 0 && k < count) stats[k] = (float)v;
-    __syncthreads();
   }
 }
 
 // Gradient from those of logp and lse: every value by itself, kChunk pieces of a row to a thread at a time.
-constexpr int kChunk = 4;
+constexpr int kChunk = 2;
 
 struct BwdRows {
   const void *logits, *ids;
@@ -247,41 +409,42 @@ struct BwdRows {
   bool ids_i64;
 };
 
-template <class E>
-__global__ __launch_bounds__(256) void logp_bwd_kernel(const BwdRows a) {
+template <class E, int TH>
+__global__ __launch_bounds__(TH) void logp_bwd_kernel(const BwdRows a) {
   using S = Span<E>;
   constexpr int N = S::N;
   const int tid = threadIdx.x;
-  const int full = a.V / N, rest = a.V - full * N;
   const int64_t items = a.T * a.chunks;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int64_t t = item / a.chunks;
     const int chunk = (int)(item - t * a.chunks);
     const int64_t id = id_of(a.ids, a.ids_i64, t);
-    const bool keep = id >= 0 && id < a.V;
     const E* x = (const E*)a.logits + t * a.ld;
     E* d = (E*)a.dlogits + t * a.ld_out;
-    const int first = chunk * kChunk * 256 + tid;
-    const bool tail = chunk == a.chunks - 1 && tid < rest;
-    if (!keep) {
+    const Cut<E> cut(d, a.V);
+    const E* xp = x + cut.lead;
+    E* dp = d + cut.lead;
+    const int first = chunk * kChunk * TH + tid;
+    const bool edge = chunk == 0 && tid < cut.edges;
+    if (id < 0 || id >= a.V) {
       const float zero[N] = {};
 #pragma unroll
       for (int q = 0; q < kChunk; ++q)
-        if (first + q * 256 < full) S::template store<false>(d + (first + q * 256) * N, zero);
-      if (tail) set_span_value(d + full * N + tid, 0.f);
+        if (first + q * TH < cut.full) S::template store<true>(dp + (first + q * TH) * N, zero);
+      if (edge) set_span_value(d + cut.edge(tid), 0.f);
       continue;
     }
     const float g = a.dlogp[t], e = a.dlse ? a.dlse[t] : 0.f, lse = a.lse[t];
     const float at_label = a.scale * g, all = a.scale * (e - g);
-    const int at = (int)id;
+    const int at = (int)id - cut.lead;
     S p[kChunk];
 #pragma unroll
     for (int q = 0; q < kChunk; ++q)
-      if (first + q * 256 < full) p[q].template load<false>(x + (first + q * 256) * N);
+      if (first + q * TH < cut.full) p[q].template load<true>(at_value(xp, (first + q * TH) * N));
 #pragma unroll
     for (int q = 0; q < kChunk; ++q) {
-      const int i = first + q * 256;
-      if (i >= full) break;
+      const int i = first + q * TH;
+      if (i >= cut.full) break;
       float v[N];
 #pragma unroll
       for (int k = 0; k < N; ++k) v[k] = __builtin_amdgcn_exp2f((p[q].get(k) * a.scale - lse) * kLog2E) * all;
@@ -289,12 +452,12 @@ __global__ __launch_bounds__(256) void logp_bwd_kernel(const BwdRows a) {
 #pragma unroll
         for (int k = 0; k < N; ++k) v[k] += at - i * N == k ? at_label : 0.f;
       }
-      S::template store<false>(d + i * N, v);
+      S::template store<true>(at_value(dp, i * N), v);
     }
-    if (tail) {
-      const int i = full * N + tid;
+    if (edge) {
+      const int i = cut.edge(tid);
       const float v = __builtin_amdgcn_exp2f((span_value(x[i]) * a.scale - lse) * kLog2E) * all;
-      set_span_value(d + i, at == i ? v + at_label : v);
+      set_span_value(d + i, i == (int)id ? v + at_label : v);
     }
   }
 }
@@ -303,25 +466,55 @@ __global__ __launch_bounds__(256) void logp_bwd_kernel(const BwdRows a) {
 
 int groups_of(int64_t T) { return (int)std::min<int64_t>(T, kGroups); }
 
+template <int WAVES>
+dim3 grid_of(int64_t T) {
+  return dim3((unsigned)std::min<int64_t>((T + Team<WAVES>::ROWS - 1) / Team<WAVES>::ROWS, kGroups));
+}
+template <int KIND, class E, int WAVES, int PARTS, bool BEYOND = false>
+unsigned launch_held(const Rows& r, hipStream_t stream) {
+  const dim3 grid = grid_of<WAVES>(r.T);
+  hipLaunchKernelGGL((held_kernel<KIND, E, WAVES, PARTS, BEYOND>), grid, dim3(Team<WAVES>::THREADS * Team<WAVES>::ROWS), 0, stream, r);
+  return grid.x;
+}
 template <int KIND, class E, int WAVES>
-void launch_rows(const Rows& r, hipStream_t stream) {
-  const dim3 grid((unsigned)groups_of(r.T)), block(WAVES * 64);
-  if (r.dlogits)
-    hipLaunchKernelGGL((rows_kernel<KIND, E, WAVES, true>), grid, block, 0, stream, r);
-  else
-    hipLaunchKernelGGL((rows_kernel<KIND, E, WAVES, false>), grid, block, 0, stream, r);
+unsigned launch_rows(const Rows& r, hipStream_t stream) {
+  const dim3 grid = grid_of<WAVES>(r.T);
+  hipLaunchKernelGGL((rows_kernel<KIND, E, WAVES>), grid, dim3(Team<WAVES>::THREADS * Team<WAVES>::ROWS), 0, stream, r);
+  return grid.x;
+}
+
+// The smallest team that holds a row; returns the workgroups.
+template <int KIND, class E>
+unsigned launch_gradient(const Rows& r, hipStream_t stream) {
+  const int pieces = (r.V + Span<E>::N - 1) / Span<E>::N, whole = (pieces + 63) / 64;      // pieces to a lane of one wave
+  if (whole <= 2) return launch_held<KIND, E, 1, 2>(r, stream);
+  if (whole <= 4) return launch_held<KIND, E, 1, 4>(r, stream);
+  if (whole <= 8) return launch_held<KIND, E, 4, 2>(r, stream);
+  if (whole <= 12) return launch_held<KIND, E, 4, 3>(r, stream);
+  if (whole <= 16) return launch_held<KIND, E, 4, 4>(r, stream);
+  if (whole <= 24) return launch_held<KIND, E, 8, 3>(r, stream);
+  if (whole <= 32) return launch_held<KIND, E, 8, 4>(r, stream);
+  if (whole <= 48) return launch_held<KIND, E, 8, 6>(r, stream);
+  if (whole <= 64) return launch_held<KIND, E, 8, 8>(r, stream);
+  if (whole <= 96) return launch_held<KIND, E, 16, 6>(r, stream);
+  if (whole <= 128) return launch_held<KIND, E, 16, 8>(r, stream);
+  if (whole <= 192) return launch_held<KIND, E, 16, 12>(r, stream);
+  if (whole <= 256) return launch_held<KIND, E, 16, 16>(r, stream);
+  return launch_held<KIND, E, 16, sizeof(E) == 2 ? 12 : 16, true>(r, stream);
 }
 template <int KIND, class E>
-void launch_rows(const Rows& r, hipStream_t stream) {
-  if (r.V <= 2048 / (int)sizeof(E))
-    launch_rows<KIND, E, 1>(r, stream);
-  else
-    launch_rows<KIND, E, 4>(r, stream);
+unsigned launch_rows(const Rows& r, hipStream_t stream) {
+  if constexpr (KIND != LogitsArgs::LOGP)
+    if (r.dlogits) return launch_gradient<KIND, E>(r, stream);
+  const int64_t bytes = (int64_t)r.V * sizeof(E);
+  if (bytes <= 4096) return launch_rows<KIND, E, 1>(r, stream);
+  if (bytes > 32768 && r.T <= 512) return launch_rows<KIND, E, 16>(r, stream);
+  return launch_rows<KIND, E, 4>(r, stream);
 }
 template <int KIND>
-hipError_t launch_rows(const Rows& r, bool f32, const char* tag, hipStream_t stream) {
+hipError_t launch_rows(const Rows& r, bool f32, const char* tag, unsigned* groups, hipStream_t stream) {
   TimedLaunch tl(tag, stream);
-  f32 ? launch_rows<KIND, float>(r, stream) : launch_rows<KIND, uint16_t>(r, stream);
+  *groups = f32 ? launch_rows<KIND, float>(r, stream) : launch_rows<KIND, uint16_t>(r, stream);
   return hipGetLastError();
 }
 
@@ -338,14 +531,15 @@ hipError_t run_token_loss(const LogitsArgs& a, hipStream_t stream) {
   r.ref_logp = a.ref_logp; r.logp = a.logp; r.lse = a.lse; r.part = (double*)a.ws; r.T = a.T; r.ld = a.ld; r.ld_out = a.ld_out;
   r.V = (int32_t)a.V; r.scale = a.scale; r.reduce = a.reduce; r.z_coef = a.z_coef; r.low = a.low; r.high = a.high; r.kl_coef = a.kl_coef;
   r.ids_i64 = a.ids_i64;
+  unsigned groups = 0;
   if (a.T > 0) {
-    const hipError_t e = a.kind == LogitsArgs::LOGP    ? launch_rows<LogitsArgs::LOGP>(r, a.f32, "token_logp", stream)
-                         : a.kind == LogitsArgs::TOKEN ? launch_rows<LogitsArgs::TOKEN>(r, a.f32, "token_loss", stream)
-                                                       : launch_rows<LogitsArgs::POLICY>(r, a.f32, "policy_loss", stream);
+    const hipError_t e = a.kind == LogitsArgs::LOGP    ? launch_rows<LogitsArgs::LOGP>(r, a.f32, "token_logp", &groups, stream)
+                         : a.kind == LogitsArgs::TOKEN ? launch_rows<LogitsArgs::TOKEN>(r, a.f32, "token_loss", &groups, stream)
+                                                       : launch_rows<LogitsArgs::POLICY>(r, a.f32, "policy_loss", &groups, stream);
     if (e != hipSuccess || a.kind == LogitsArgs::LOGP) return e;
   }
   TimedLaunch tl("loss_sum", stream);
-  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(256), 0, stream, (const double*)a.ws, groups_of(a.T), a.kind == LogitsArgs::TOKEN ? 2 : 3,
+  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, stream, (const double*)a.ws, (int)groups, a.kind == LogitsArgs::TOKEN ? 2 : 3,
                      a.stats);
   return hipGetLastError();
 }
@@ -354,14 +548,18 @@ hipError_t run_token_logp_bwd(const LogitsArgs& a, hipStream_t stream) {
   BwdRows r{};
   r.logits = a.logits; r.ids = a.ids; r.dlogits = a.dlogits; r.dlogp = a.dlogp; r.dlse = a.dlse; r.lse = a.lse_in; r.T = a.T; r.ld = a.ld;
   r.ld_out = a.ld_out; r.V = (int32_t)a.V; r.scale = a.scale; r.ids_i64 = a.ids_i64;
-  const int64_t per = (int64_t)kChunk * 256 * (a.f32 ? 4 : 8);
-  r.chunks = (int32_t)((a.V + per - 1) / per);
-  const unsigned grid = (unsigned)std::min<int64_t>(a.T * r.chunks, 1 << 16);
+  // (a wave where it takes a row at once, so that no lanes idle)
+  const int64_t pieces = (a.V + (a.f32 ? 3 : 7)) / (a.f32 ? 4 : 8);
+  const int threads = pieces <= kChunk * 64 ? 64 : 256;
+  r.chunks = (int32_t)((pieces + kChunk * threads - 1) / (kChunk * threads));
   TimedLaunch tl("token_logp_bwd", stream);
-  if (a.f32)
-    hipLaunchKernelGGL(logp_bwd_kernel<float>, dim3(grid), dim3(256), 0, stream, r);
+  const auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(a.T * r.chunks, 1 << 20)), dim3((unsigned)threads), 0, stream, r);
+  };
+  if (threads == 64)
+    a.f32 ? launch(logp_bwd_kernel<float, 64>) : launch(logp_bwd_kernel<uint16_t, 64>);
   else
-    hipLaunchKernelGGL(logp_bwd_kernel<uint16_t>, dim3(grid), dim3(256), 0, stream, r);
+    a.f32 ? launch(logp_bwd_kernel<float, 256>) : launch(logp_bwd_kernel<uint16_t, 256>);
   return hipGetLastError();
 }
 
