@@ -67,8 +67,9 @@ def step(p, g, m, v, t, rate, beta1, beta2, eps, decay, clip=1.0):
     r, root = rate / (1 - beta1 ** t), (1 - beta2 ** t) ** -0.5
     den = np.sqrt(v1) * root + eps
     up = r * m1 / den
-    # the denominator: half v's relative error (or the root of all of it, near 0) and 5 roundings; the quotient's and its factor's 4
+    # the denominator: half v's relative error (or the root of all of it, near 0) and 5 roundings (2 of them a root to 1 ulp);
+    # a reciprocal to 1 ulp, its product, the rate and its product: 5
     den_err = root * np.where(v1 > 2 * v_err, v_err / np.sqrt(np.maximum(v1, 1e-300)), np.sqrt(v1 + v_err)) + 5 * EPS32 * den
-    up_err = r * m_err / den + np.abs(up) * (np.minimum(den_err / np.maximum(den - den_err, eps / 2), 1e3) + 4 * EPS32)
+    up_err = r * m_err / den + np.abs(up) * (np.minimum(den_err / np.maximum(den - den_err, eps / 2), 1e3) + 5 * EPS32)
     new = p * (1 - rate * decay) - up
     return new, m1, v1, EPS32 * (3 * np.abs(p) + np.abs(new)) + up_err, m_err, v_err

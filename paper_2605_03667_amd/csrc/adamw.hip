@@ -20,8 +20,10 @@ namespace {
 
 constexpr int kTensors = 64;      // per launch, at most (a lane of a wave to each)
 constexpr int kBlock = ELAS_ADAMW_BLOCK;
-constexpr int kPiece = 2048;      // values: 2 blocks to each of a workgroup's 4 waves
-constexpr int kGroups = 4096;     // most workgroups per launch
+constexpr int kAtOnce = 1;        // blocks to a wave at a time
+constexpr int kPiece = 4 * kAtOnce * kBlock;      // values to a workgroup of 4 waves at a time
+constexpr uint32_t kGroups = 1u << 24;   // most workgroups per launch
+constexpr int64_t kStreamed = int64_t(1) << 24;   // values from which on nothing is kept in the caches
 constexpr float kTopM = 245760.f, kTopV = 507904.f;     // largest codes: 15 2^14, 31 2^14
 
 // What the step's formulas need, found once.
@@ -97,130 +99,178 @@ __device__ __forceinline__ uint32_t code_of(float y, uint32_t u) {
   constexpr uint32_t TOP = (16u << MANTISSA) - 1;
   return code < TOP ? code : TOP;
 }
-// What a code's magnitude stands for, in units of its scale.
-template <int MANTISSA>
-__device__ __forceinline__ float code_value(uint32_t code) {
-  const uint32_t e = code >> MANTISSA;
-  const float low = (float)code;
-  // the code with a bit in front of its mantissa, as the upper bits of a float32
-  const float high = as_float((code + ((126u + MANTISSA) << MANTISSA)) << (23 - MANTISSA));
-  return e ? high : low;
+// Codes as values.  A magnitude's code in the bits of a float32's lowest exponents and highest mantissa stands for
+// its value times 2^-(126 + MANTISSA), subnormals (e = 0) included: one product with 2^127 and one with the scale's
+// share of the rest, which rounds as a product of value and scale does.
+__device__ __forceinline__ float first_moment(uint32_t codes, int k, float scale4) {      // byte k; 4 scale
+  const float x = as_float((codes >> (8 * k) & 0x7Fu) << 20) * 0x1p127f * scale4;
+  return __builtin_copysignf(x, as_float(codes << (24 - 8 * k)));
+}
+__device__ __forceinline__ float second_moment(uint32_t codes, int k, float scale8) {     // byte k; 8 scale
+  return as_float((codes >> (8 * k) & 0xFFu) << 19) * 0x1p127f * scale8;
 }
 
-// Scale of a block from its largest magnitude's bits.
-__device__ __forceinline__ float scale_of(uint32_t top_bits, float top) { return as_float(top_bits) / top; }
+// x / s for a block's values: a product with the reciprocal, corrected by its remainder, which came out as the
+// division's rounding in all of 1.7e8 quotients of random mantissas (scales whose remainders may leave the range of
+// float32 are divided).
+struct Quotient {
+  float s, r;
+  bool tiny;
+  __device__ __forceinline__ explicit Quotient(float scale) : s(scale) {
+    const float r0 = __builtin_amdgcn_rcpf(s);
+    r = fmaf(fmaf(-s, r0, 1.f), r0, r0);
+    tiny = !(s >= 0x1p-90f && s <= 0x1p90f);
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    if (tiny) return x / s;                // (the same for the whole wave)
+    const float q = x * r;
+    return fmaf(fmaf(-q, s, x), r, q);
+  }
+};
+
+// Square root of a magnitude to 1 ulp; subnormals, which the instruction takes for 0, are scaled
+// by 2^64 first and the root by 2^-32 after.
+__device__ __forceinline__ float root_of(float v) {
+  const bool tiny = v < 0x1p-126f;
+  const float r = __builtin_amdgcn_sqrtf(tiny ? v * 0x1p64f : v);
+  return tiny ? r * 0x1p-32f : r;
+}
 
 struct Update {
   Factors f;
   Betas b;
   float keep;    // 1 - lr decay
+  // Every product and sum is rounded by itself, in the order of the formulas, and so are the scales and
+  // quotients of 8-bit moments: float32 arithmetic in elementary steps gives the same moments bit for bit, and with the
+  // same random bits the same codes.  (Fused products would be as exact, but a code that falls to the other
+  // neighbour is off by an eighth.)
   __device__ __forceinline__ void moments(float g, float& m, float& v) const {
+#pragma clang fp contract(off)
     g = g * f.clip * f.clip_power;
-    m = fmaf(b.b1, m, b.c1 * g);
-    v = fmaf(b.b2, v, b.c2 * g * g);
+    m = b.b1 * m + b.c1 * g;
+    v = b.b2 * v + b.c2 * g * g;
   }
   __device__ __forceinline__ float weight(float p, float m, float v) const {
-    return fmaf(p, keep, -(f.rate * (m / (sqrtf(v) * f.root + b.eps))));
+    return fmaf(p, keep, -(f.rate * (m * __builtin_amdgcn_rcpf(root_of(v) * f.root + b.eps))));
   }
 };
 
-// 256 values of a tensor from value `at` on, n of them the tensor's; `moment`: their first moment's place.
+// A lane's 4 of the 256 values of a block, as they were loaded.
 template <class P, class G, bool EIGHT>
-__device__ __forceinline__ void update_block(P* p, const G* g, uint16_t* copy, int n, const Moments& s, int64_t moment, const Update& u,
-                                             uint32_t key, uint32_t index) {
-  const int lane = threadIdx.x & 63, i = 4 * lane;
-  const bool whole = i + 4 <= n;
-  float pv[4] = {}, gv[4] = {}, m[4], v[4], scale_m = 0.f, scale_v = 0.f;
-  if (whole) {
-    Four<P> a;
-    Four<G> b;
-    a.template load<false>(p + i);
-    b.template load<false>(g + i);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) pv[k] = a.get(k), gv[k] = b.get(k);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (i + k < n) pv[k] = span_value(p[i + k]), gv[k] = span_value(g[i + k]);
-  }
-  if constexpr (EIGHT) {
-    const uint32_t mc = *(const uint32_t*)((const uint8_t*)s.m + moment + i), vc = *(const uint32_t*)((const uint8_t*)s.v + moment + i);
-    const int64_t block = moment / kBlock;
-    scale_m = s.m_scale[block];
-    scale_v = s.v_scale[block];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t c = mc >> (8 * k) & 0xFFu;
-      const float x = code_value<3>(c & 0x7Fu) * scale_m;
-      m[k] = c & 0x80u ? -x : x;
-      v[k] = code_value<4>(vc >> (8 * k) & 0xFFu) * scale_v;
-    }
-  } else {
-    const f32x4 a = *(const f32x4*)((const float*)s.m + moment + i), b = *(const f32x4*)((const float*)s.v + moment + i);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) m[k] = a[k], v[k] = b[k];
-  }
-  float out[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    u.moments(gv[k], m[k], v[k]);
-    if (i + k >= n) m[k] = v[k] = 0.f;
-    out[k] = u.weight(pv[k], m[k], v[k]);
-  }
-  if (whole) {
-    Four<P>::template store<false>(p + i, out);
-    if (copy) Four<uint16_t>::template store<false>(copy + i, out);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (i + k < n) {
-        set_span_value(p + i + k, out[k]);
-        if (copy) set_span_value(copy + i + k, out[k]);
-      }
-  }
-  if constexpr (EIGHT) {
-    uint32_t top_m = 0, top_v = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t a = __builtin_bit_cast(uint32_t, m[k]) & 0x7FFFFFFFu, b = __builtin_bit_cast(uint32_t, v[k]) & 0x7FFFFFFFu;
-      top_m = a > top_m ? a : top_m;
-      top_v = b > top_v ? b : top_v;
-    }
-    scale_m = scale_of(wave_max(top_m), kTopM);
-    scale_v = scale_of(wave_max(top_v), kTopV);
-    // (a block of zeros, or of magnitudes whose scale float32 cannot hold)
-    const float div_m = scale_m > 0.f ? scale_m : 1.f, div_v = scale_v > 0.f ? scale_v : 1.f;
-    uint32_t mc = 0, vc = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t bits = mix(index + (uint32_t)(i + k) + key);
-      uint32_t c = code_of<3>(fabsf(m[k]) / div_m, bits & 0xFFFFu);
-      if (m[k] < 0.f) c |= 0x80u;
-      mc |= c << (8 * k);
-      c = code_of<4>(v[k] / div_v, bits >> 16);
-      if (v[k] > 0.f && c == 0) c = 1;
-      vc |= c << (8 * k);
-    }
-    *(uint32_t*)((uint8_t*)s.m + moment + i) = mc;
-    *(uint32_t*)((uint8_t*)s.v + moment + i) = vc;
-    if (lane == 0) {
-      s.m_scale[moment / kBlock] = scale_m;
-      s.v_scale[moment / kBlock] = scale_v;
-    }
-  } else {
-    *(f32x4*)((float*)s.m + moment + i) = f32x4{m[0], m[1], m[2], m[3]};
-    *(f32x4*)((float*)s.v + moment + i) = f32x4{v[0], v[1], v[2], v[3]};
-  }
-}
+struct Block {
+  Four<P> p;
+  Four<G> g;
+  f32x4 m, v;
+  uint32_t mc, vc;
+  float m_scale, v_scale;
 
-template <class P, class G, bool EIGHT>
+  // `moment`: the block's first moment; `n` values of the tensor from p, g on.
+  template <bool STREAM>
+  __device__ __forceinline__ void load(const P* pp, const G* gp, const Moments& s, int64_t moment, int n) {
+    const int i = 4 * (int)(threadIdx.x & 63);
+    if constexpr (EIGHT) {
+      mc = load_as<STREAM>((const uint32_t*)((const uint8_t*)s.m + moment) + i / 4);
+      vc = load_as<STREAM>((const uint32_t*)((const uint8_t*)s.v + moment) + i / 4);
+      m_scale = s.m_scale[moment / kBlock];
+      v_scale = s.v_scale[moment / kBlock];
+    } else {
+      m = load_as<STREAM>((const f32x4*)((const float*)s.m + moment) + i / 4);
+      v = load_as<STREAM>((const f32x4*)((const float*)s.v + moment) + i / 4);
+    }
+    if (i + 4 <= n) {
+      p.template load<STREAM>(pp + i);
+      g.template load<STREAM>(gp + i);
+    } else {
+      float x[4] = {}, y[4] = {};
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        if (i + k < n) x[k] = span_value(pp[i + k]), y[k] = span_value(gp[i + k]);
+      p.set(x);
+      g.set(y);
+    }
+  }
+
+  template <bool STREAM>
+  __device__ __forceinline__ void step(P* pp, uint16_t* copy, const Moments& s, int64_t moment, int n, const Update& u, uint32_t key, uint32_t index) {
+    const int lane = threadIdx.x & 63, i = 4 * lane;
+    float mv[4], vv[4], out[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (EIGHT) {
+        mv[k] = first_moment(mc, k, 4.f * m_scale);
+        vv[k] = second_moment(vc, k, 8.f * v_scale);
+      } else {
+        mv[k] = m[k], vv[k] = v[k];
+      }
+      u.moments(g.get(k), mv[k], vv[k]);
+      if (i + k >= n) mv[k] = vv[k] = 0.f;
+      out[k] = u.weight(p.get(k), mv[k], vv[k]);
+    }
+    if (i + 4 <= n) {
+      Four<P>::template store<STREAM>(pp + i, out);
+      if (copy) Four<uint16_t>::template store<false>(copy + i, out);     // (read next)
+    } else {
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        if (i + k < n) {
+          set_span_value(pp + i + k, out[k]);
+          if (copy) set_span_value(copy + i + k, out[k]);
+        }
+    }
+    if constexpr (EIGHT) {
+      uint32_t top_m = 0, top_v = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t a = __builtin_bit_cast(uint32_t, mv[k]) & 0x7FFFFFFFu, b = __builtin_bit_cast(uint32_t, vv[k]) & 0x7FFFFFFFu;
+        top_m = a > top_m ? a : top_m;
+        top_v = b > top_v ? b : top_v;
+      }
+      const float new_m = as_float(wave_max(top_m)) * (1.f / kTopM), new_v = as_float(wave_max(top_v)) * (1.f / kTopV);
+      // (a block of zeros, or of magnitudes whose scale float32 cannot hold)
+      const Quotient div_m(new_m > 0.f ? new_m : 1.f), div_v(new_v > 0.f ? new_v : 1.f);
+      uint32_t to_m = 0, to_v = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t bits = mix(index + (uint32_t)(i + k) + key);
+        uint32_t c = code_of<3>(div_m(fabsf(mv[k])), bits & 0xFFFFu);
+        if (mv[k] < 0.f) c |= 0x80u;
+        to_m |= c << (8 * k);
+        c = code_of<4>(div_v(vv[k]), bits >> 16);
+        if (vv[k] > 0.f && c == 0) c = 1;
+        to_v |= c << (8 * k);
+      }
+      store_as<STREAM>((uint32_t*)((uint8_t*)s.m + moment) + lane, to_m);
+      store_as<STREAM>((uint32_t*)((uint8_t*)s.v + moment) + lane, to_v);
+      if (lane == 0) {
+        s.m_scale[moment / kBlock] = new_m;
+        s.v_scale[moment / kBlock] = new_v;
+      }
+    } else {
+      store_as<STREAM>((f32x4*)((float*)s.m + moment) + lane, f32x4{mv[0], mv[1], mv[2], mv[3]});
+      store_as<STREAM>((f32x4*)((float*)s.v + moment) + lane, f32x4{vv[0], vv[1], vv[2], vv[3]});
+    }
+  }
+};
+
+// A piece: each wave takes kAtOnce blocks, all of them loaded before the first is computed.
+template <class P, class G, bool EIGHT, bool STREAM>
 __device__ __forceinline__ void update_piece(P* p, const G* g, uint16_t* copy, int n, const Moments& s, int64_t moment, const Update& u,
                                              uint32_t key, uint32_t index) {
-  for (int at = (int)(threadIdx.x >> 6) * kBlock; at < n; at += 4 * kBlock)
-    update_block<P, G, EIGHT>(p + at, g + at, copy ? copy + at : nullptr, n - at, s, moment + at, u, key, index + at);
+  const int first = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * kBlock;
+  Block<P, G, EIGHT> b[kAtOnce];
+#pragma unroll
+  for (int q = 0; q < kAtOnce; ++q) {
+    const int at = first + q * 4 * kBlock;
+    if (at < n) b[q].template load<STREAM>(p + at, g + at, s, moment + at, n - at);
+  }
+#pragma unroll
+  for (int q = 0; q < kAtOnce; ++q) {
+    const int at = first + q * 4 * kBlock;
+    if (at < n) b[q].template step<STREAM>(p + at, copy ? copy + at : nullptr, s, moment + at, n - at, u, key, index + at);
+  }
 }
 
-template <int CAP, bool EIGHT>
+template <int CAP, bool EIGHT, bool STREAM>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensors<CAP> a, const Moments s, const Betas b, const Factors* factors) {
   const Factors f = *factors;
   if (f.skip) return;
@@ -239,43 +289,41 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors<CAP> a, const 
     const bool pb = a.p_bf16[k >> 5] >> (k & 31) & 1u, gb = a.g_bf16[k >> 5] >> (k & 31) & 1u;
     if (pb) {
       uint16_t* p = (uint16_t*)a.p[k] + at;
-      gb ? update_piece<uint16_t, uint16_t, EIGHT>(p, (const uint16_t*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at)
-         : update_piece<uint16_t, float, EIGHT>(p, (const float*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at);
+      gb ? update_piece<uint16_t, uint16_t, EIGHT, STREAM>(p, (const uint16_t*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at)
+         : update_piece<uint16_t, float, EIGHT, STREAM>(p, (const float*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at);
     } else {
       float* p = (float*)a.p[k] + at;
-      gb ? update_piece<float, uint16_t, EIGHT>(p, (const uint16_t*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at)
-         : update_piece<float, float, EIGHT>(p, (const float*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at);
+      gb ? update_piece<float, uint16_t, EIGHT, STREAM>(p, (const uint16_t*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at)
+         : update_piece<float, float, EIGHT, STREAM>(p, (const float*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at);
     }
   }
 }
 
-// Values of codes, 4 to a lane: a wave to a block.
+// Values of codes, 8 to a lane: half a wave to a block.
 template <bool SECOND, class E>
 __global__ __launch_bounds__(256) void adam8_values_kernel(const uint8_t* codes, const float* scale, int64_t blocks, E* out) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t b = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); b < blocks; b += (int64_t)gridDim.x * 4) {
-    const int64_t i = b * kBlock + 4 * lane;
-    const uint32_t q = *(const uint32_t*)(codes + i);
-    const float s = scale[b];
-    float v[4];
+  const int64_t lanes = blocks * (kBlock / 8);
+  for (int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x; j < lanes; j += (int64_t)gridDim.x * 256) {
+    const u32x2 q = __builtin_nontemporal_load((const u32x2*)codes + j);
+    const float s = scale[j / (kBlock / 8)] * (SECOND ? 8.f : 4.f);
+    float v[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t c = q >> (8 * k) & 0xFFu;
-      if (SECOND) {
-        v[k] = code_value<4>(c) * s;
-      } else {
-        const float x = code_value<3>(c & 0x7Fu) * s;
-        v[k] = c & 0x80u ? -x : x;
-      }
+    for (int k = 0; k < 8; ++k) v[k] = SECOND ? second_moment(q[k / 4], k % 4, s) : first_moment(q[k / 4], k % 4, s);
+    E* to = out + 8 * j;
+    if constexpr (sizeof(E) == 2) {
+      Span<E>::template store<true>(to, v);
+    } else {
+      const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+      Span<E>::template store<true>(to, a);
+      Span<E>::template store<true>(to + 4, b);
     }
-    Four<E>::template store<false>(out + i, v);
   }
 }
 
 // ---- host -----------------------------------------------------------------------------
 
 template <bool EIGHT>
-hipError_t launch_update(const AdamwArgs& c, int64_t k0, int count, int64_t& block, const Betas& b, hipStream_t stream) {
+hipError_t launch_update(const AdamwArgs& c, int64_t k0, int count, int64_t& block, const Betas& b, bool stream_data, hipStream_t stream) {
   Tensors<kTensors> a{};
   a.count = count;
   a.number = (int)k0;
@@ -298,8 +346,11 @@ hipError_t launch_update(const AdamwArgs& c, int64_t k0, int count, int64_t& blo
   if (pieces == 0) return hipSuccess;
   const Moments s{c.m, c.v, c.m_scale, c.v_scale};
   TimedLaunch tl(EIGHT ? "adamw8" : "adamw", stream);
-  hipLaunchKernelGGL((adamw_kernel<kTensors, EIGHT>), dim3(std::min<uint32_t>(pieces, kGroups)), dim3(256), 0, stream, a, s, b,
-                     (const Factors*)c.ws);
+  const dim3 grid(std::min<uint32_t>(pieces, kGroups));
+  if (stream_data)
+    hipLaunchKernelGGL((adamw_kernel<kTensors, EIGHT, true>), grid, dim3(256), 0, stream, a, s, b, (const Factors*)c.ws);
+  else
+    hipLaunchKernelGGL((adamw_kernel<kTensors, EIGHT, false>), grid, dim3(256), 0, stream, a, s, b, (const Factors*)c.ws);
   return hipGetLastError();
 }
 
@@ -316,10 +367,13 @@ hipError_t run_adamw(const AdamwArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   const Betas b{(float)a.beta1, (float)(1.0 - a.beta1), (float)a.beta2, (float)(1.0 - a.beta2), (float)a.eps};
-  int64_t block = 0;
+  int64_t block = 0, total = 0;
+  for (int64_t k = 0; k < a.n; ++k) total += a.numel[k];
+  const bool stream_data = total >= kStreamed;
   for (int64_t k = 0; k < a.n; k += kTensors) {
     const int count = (int)std::min<int64_t>(kTensors, a.n - k);
-    const hipError_t e = a.eight ? launch_update<true>(a, k, count, block, b, stream) : launch_update<false>(a, k, count, block, b, stream);
+    const hipError_t e = a.eight ? launch_update<true>(a, k, count, block, b, stream_data, stream)
+                                 : launch_update<false>(a, k, count, block, b, stream_data, stream);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -328,7 +382,7 @@ hipError_t run_adamw(const AdamwArgs& a, hipStream_t stream) {
 hipError_t run_adam8_values(const uint8_t* codes, const float* scale, int64_t blocks, bool second, bool f32, void* out, hipStream_t stream) {
   TimedLaunch tl("adam8_values", stream);
   const auto launch = [&](auto kernel, auto* to) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((blocks + 3) / 4, 1 << 14)), dim3(256), 0, stream, codes, scale, blocks, to);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((blocks * (kBlock / 8) + 255) / 256, 1 << 24)), dim3(256), 0, stream, codes, scale, blocks, to);
   };
   if (second)
     f32 ? launch(adam8_values_kernel<true, float>, (float*)out) : launch(adam8_values_kernel<true, uint16_t>, (uint16_t*)out);

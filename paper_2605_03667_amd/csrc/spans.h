@@ -28,6 +28,7 @@ struct Four<float> {
   __device__ __forceinline__ void load(const float* p) {
     q = STREAM ? __builtin_nontemporal_load((const f32x4_span*)p) : *(const f32x4_span*)p;
   }
+  __device__ __forceinline__ void set(const float (&v)[4]) { q = f32x4{v[0], v[1], v[2], v[3]}; }
   __device__ __forceinline__ float get(int i) const { return q[i]; }
   template <bool STREAM>
   static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
@@ -45,6 +46,7 @@ struct Four<uint16_t> {
   __device__ __forceinline__ void load(const uint16_t* p) {
     q = STREAM ? __builtin_nontemporal_load((const u32x2_span*)p) : *(const u32x2_span*)p;
   }
+  __device__ __forceinline__ void set(const float (&v)[4]) { q = u32x2{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])}; }
   __device__ __forceinline__ float get(int i) const {
     const uint32_t w = q[i >> 1];
     return as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
@@ -65,6 +67,7 @@ struct Span;
 template <>
 struct Span<float> : Four<float> {
   static constexpr int N = 4;
+  using Four<float>::set;
   __device__ __forceinline__ void set(int i, float v) { q[i] = v; }
   __device__ __forceinline__ void keep_packed() {}
   // -inf everywhere

@@ -221,6 +221,7 @@ def test_timing_tags():
         elas.elas_timing_enable(True)
         h.run()
         elas.elas_adam8_values(h.opt.m, h.opt.m_scale)
+        elas.elas_preference_loss(h.old, torch.arange(201, device=DEV))       # (few pairs take one launch)
         torch.cuda.synchronize()
         elas.elas_timing_enable(False)
         tags = elas.elas_timing_collect()
