@@ -2,8 +2,8 @@
 //
 // A first launch of one thread finds the step's factors in 64 bits and counts the step; then
 // one launch for up to kTensors tensors does everything to every value: read p, g and the
-// moments, write p, the moments and the copy.  Tensors are cut into pieces of kPiece
-// values, numbered through and dealt out to the workgroups in turn.  A wave takes 256 values
+// moments, write p, the moments and the copy.  Tensors are cut into pieces, numbered through, one
+// to a workgroup (dealt out to 4096 workgroups in turn 1B in 8 bits took 960 us for 822).  A wave takes 256 values
 // at a time, 4 to a lane: a block of moments in 8 bits is one wave's, its largest magnitude
 // a maximum over the wave.
 #include <math.h>
@@ -20,8 +20,9 @@ namespace {
 
 constexpr int kTensors = 64;      // per launch, at most (a lane of a wave to each)
 constexpr int kBlock = ELAS_ADAMW_BLOCK;
-constexpr int kAtOnce = 1;        // blocks to a wave at a time
-constexpr int kPiece = 4 * kAtOnce * kBlock;      // values to a workgroup of 4 waves at a time
+// Values of a piece: AT_ONCE blocks to each of a workgroup's 4 waves.  One, but two where moments in 8 bits and
+// weights in bf16 leave a block little to load (1B: 581 us with one, 523 with two; float32 weights 744 and 798).
+constexpr int piece_of(int at_once) { return 4 * at_once * kBlock; }
 constexpr uint32_t kGroups = 1u << 24;   // most workgroups per launch
 constexpr int64_t kStreamed = int64_t(1) << 24;   // values from which on nothing is kept in the caches
 constexpr float kTopM = 245760.f, kTopV = 507904.f;     // largest codes: 15 2^14, 31 2^14
@@ -76,7 +77,7 @@ struct Tensors {
   uint16_t last[CAP];        // values of its last piece
   uint32_t p_bf16[CAP / 32], g_bf16[CAP / 32];
   int count, number;         // tensors here; number of the first of them in the call
-  __device__ __forceinline__ int values(uint32_t c, int k) const { return c + 1 < first[k + 1] ? kPiece : (int)last[k]; }
+  __device__ __forceinline__ int values(uint32_t c, int k, int piece) const { return c + 1 < first[k + 1] ? piece : (int)last[k]; }
 };
 
 struct Moments {
@@ -87,53 +88,87 @@ struct Betas {
   float b1, c1, b2, c2, eps;   // c = 1 - b
 };
 
-// A magnitude's code: y in units of the scale, u 16 random bits.  From 2^MANTISSA on codes are the
-// upper bits of a float32, below that whole numbers; adding u below the lowest bit kept and
-// cutting off rounds up with the probability of the distance to the lower neighbour.
+// Codes are the upper bits of a float32: a code in the bits of a float32's lowest exponents and highest mantissa
+// stands for its value times 2^-(126 + MANTISSA), subnormals (e = 0) included.
 template <int MANTISSA>
-__device__ __forceinline__ uint32_t code_of(float y, uint32_t u) {
-  constexpr int SHIFT = 23 - MANTISSA;
-  const uint32_t high = ((__builtin_bit_cast(uint32_t, y) + (u << (SHIFT - 16))) >> SHIFT) - ((126u + MANTISSA) << MANTISSA);
-  const uint32_t low = (uint32_t)(fminf(y, 64.f) + (float)u * 0x1p-16f);   // (held to the range of the conversion)
-  const uint32_t code = y >= (float)(1 << MANTISSA) ? high : low;
-  constexpr uint32_t TOP = (16u << MANTISSA) - 1;
-  return code < TOP ? code : TOP;
-}
-// Codes as values.  A magnitude's code in the bits of a float32's lowest exponents and highest mantissa stands for
-// its value times 2^-(126 + MANTISSA), subnormals (e = 0) included: one product with 2^127 and one with the scale's
-// share of the rest, which rounds as a product of value and scale does.
-__device__ __forceinline__ float first_moment(uint32_t codes, int k, float scale4) {      // byte k; 4 scale
-  const float x = as_float((codes >> (8 * k) & 0x7Fu) << 20) * 0x1p127f * scale4;
-  return __builtin_copysignf(x, as_float(codes << (24 - 8 * k)));
-}
-__device__ __forceinline__ float second_moment(uint32_t codes, int k, float scale8) {     // byte k; 8 scale
-  return as_float((codes >> (8 * k) & 0xFFu) << 19) * 0x1p127f * scale8;
+constexpr float kUnit = MANTISSA == 3 ? 0x1p-129f : 0x1p-130f;
+template <int MANTISSA>
+constexpr int kShift = 23 - MANTISSA;
+
+// A magnitude's code: y in units of the scale, u 16 random bits.  Adding u below the lowest bit kept and cutting off
+// rounds up with the probability of the distance to the lower neighbour.  (y below 2^MANTISSA is a subnormal here, to
+// 2^-20 or 2^-19.)
+template <int MANTISSA>
+__device__ __forceinline__ uint32_t code_of(float y, uint32_t u, uint32_t least) {
+  const uint32_t code = (__builtin_bit_cast(uint32_t, y * kUnit<MANTISSA>) + (u << (kShift<MANTISSA> - 16))) >> kShift<MANTISSA>;
+  const uint32_t top = (16u << MANTISSA) - 1;
+  return __builtin_elementwise_min(__builtin_elementwise_max(code, least), top);
 }
 
-// x / s for a block's values: a product with the reciprocal, corrected by its remainder, which came out as the
-// division's rounding in all of 1.7e8 quotients of random mantissas (scales whose remainders may leave the range of
-// float32 are divided).
-struct Quotient {
-  float s, r;
-  bool tiny;
-  __device__ __forceinline__ explicit Quotient(float scale) : s(scale) {
-    const float r0 = __builtin_amdgcn_rcpf(s);
-    r = fmaf(fmaf(-s, r0, 1.f), r0, r0);
-    tiny = !(s >= 0x1p-90f && s <= 0x1p90f);
+// Values of the 4 codes of a word.  One product with the scale over the unit rounds as a product of value and scale does;
+// a scale for which that leaves float32's range takes two.
+template <int MANTISSA>
+struct Decoder {
+  float a, b;
+  bool two;
+  __device__ __forceinline__ explicit Decoder(float scale) {
+    two = !(scale < 0x1p-4f);
+    a = 0x1p127f;
+    b = scale * (1.f / (kUnit<MANTISSA> * 0x1p127f));      // 4 scale, 8 scale
   }
-  __device__ __forceinline__ float operator()(float x) const {
-    if (tiny) return x / s;                // (the same for the whole wave)
-    const float q = x * r;
-    return fmaf(fmaf(-q, s, x), r, q);
+  template <bool ANY = false>     // (ANY: two products, where lanes hold different scales)
+  __device__ __forceinline__ void get(uint32_t codes, float (&v)[4]) const {
+    constexpr uint32_t MASK = (16u << MANTISSA) - 1;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = as_float((codes >> (8 * k) & MASK) << kShift<MANTISSA>);
+    if (ANY || two) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = v[k] * a * b;
+    } else {
+      const float c = a * b;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] *= c;
+    }
+    if constexpr (MANTISSA == 3) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = __builtin_copysignf(v[k], as_float(codes << (24 - 8 * k)));
+    }
   }
 };
 
-// Square root of a magnitude to 1 ulp; subnormals, which the instruction takes for 0, are scaled
-// by 2^64 first and the root by 2^-32 after.
-__device__ __forceinline__ float root_of(float v) {
-  const bool tiny = v < 0x1p-126f;
-  const float r = __builtin_amdgcn_sqrtf(tiny ? v * 0x1p64f : v);
-  return tiny ? r * 0x1p-32f : r;
+// Largest of two magnitudes each over a wave, as bits (NaN above all): the first in lane 0 .. 31, the second in
+// 32 .. 63, read into scalar registers.
+__device__ __forceinline__ void wave_max2(uint32_t& a, uint32_t& b) {
+  const auto s32 = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  uint32_t v = __builtin_elementwise_max(s32[0], s32[1]);
+  const auto s16 = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = __builtin_elementwise_max(s16[0], s16[1]);
+  const auto step = [&](uint32_t o) { v = __builtin_elementwise_max(v, o); };
+  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));
+  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));
+  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));
+  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true));
+  a = (uint32_t)__builtin_amdgcn_readlane((int)v, 0);
+  b = (uint32_t)__builtin_amdgcn_readlane((int)v, 32);
+}
+
+// A block's magnitudes in units of its scale s: products with the reciprocal, corrected by their remainders, which came out
+// as the division's rounding in all of 1.7e8 quotients of random mantissas (scales whose remainders may leave the range of
+// float32 are divided).
+__device__ __forceinline__ void in_units(float scale, const float (&x)[4], float (&y)[4]) {
+  // (a block of zeros, or of magnitudes whose scale float32 cannot hold: unit 1)
+  const float s = scale > 0.f ? scale : 1.f;
+  if (s >= 0x1p-90f && s <= 0x1p90f) {
+    const float r0 = __builtin_amdgcn_rcpf(s), r = fmaf(fmaf(-s, r0, 1.f), r0, r0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float v = fabsf(x[k]), q = v * r;
+      y[k] = fmaf(fmaf(-q, s, v), r, q);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = fabsf(x[k]) / s;
+  }
 }
 
 struct Update {
@@ -144,14 +179,36 @@ struct Update {
   // quotients of 8-bit moments: float32 arithmetic in elementary steps gives the same moments bit for bit, and with the
   // same random bits the same codes.  (Fused products would be as exact, but a code that falls to the other
   // neighbour is off by an eighth.)
-  __device__ __forceinline__ void moments(float g, float& m, float& v) const {
+  __device__ __forceinline__ void moments(float (&g)[4], float (&m)[4], float (&v)[4]) const {
 #pragma clang fp contract(off)
-    g = g * f.clip * f.clip_power;
-    m = b.b1 * m + b.c1 * g;
-    v = b.b2 * v + b.c2 * g * g;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) g[k] = g[k] * f.clip;
+    if (f.clip_power != 1.f) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) g[k] = g[k] * f.clip_power;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      m[k] = b.b1 * m[k] + b.c1 * g[k];
+      v[k] = b.b2 * v[k] + b.c2 * g[k] * g[k];
+    }
   }
-  __device__ __forceinline__ float weight(float p, float m, float v) const {
-    return fmaf(p, keep, -(f.rate * (m * __builtin_amdgcn_rcpf(root_of(v) * f.root + b.eps))));
+  // Roots of subnormals, which the instruction takes for 0, matter beside an eps under 1e-10 alone.
+  __device__ __forceinline__ void weights(float (&p)[4], const float (&m)[4], const float (&v)[4]) const {
+    float r[4];
+    if (b.eps < 1e-10f) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const bool tiny = v[k] < 0x1p-126f;
+        r[k] = __builtin_amdgcn_sqrtf(tiny ? v[k] * 0x1p64f : v[k]);
+        r[k] = tiny ? r[k] * 0x1p-32f : r[k];
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) r[k] = __builtin_amdgcn_sqrtf(v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) p[k] = fmaf(p[k], keep, -(f.rate * (m[k] * __builtin_amdgcn_rcpf(r[k] * f.root + b.eps))));
   }
 };
 
@@ -194,17 +251,22 @@ struct Block {
   __device__ __forceinline__ void step(P* pp, uint16_t* copy, const Moments& s, int64_t moment, int n, const Update& u, uint32_t key, uint32_t index) {
     const int lane = threadIdx.x & 63, i = 4 * lane;
     float mv[4], vv[4], out[4];
+    if constexpr (EIGHT) {
+      Decoder<3>(m_scale).get(mc, mv);
+      Decoder<4>(v_scale).get(vc, vv);
+    } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if constexpr (EIGHT) {
-        mv[k] = first_moment(mc, k, 4.f * m_scale);
-        vv[k] = second_moment(vc, k, 8.f * v_scale);
-      } else {
-        mv[k] = m[k], vv[k] = v[k];
-      }
-      u.moments(g.get(k), mv[k], vv[k]);
-      if (i + k >= n) mv[k] = vv[k] = 0.f;
-      out[k] = u.weight(p.get(k), mv[k], vv[k]);
+      for (int k = 0; k < 4; ++k) mv[k] = m[k], vv[k] = v[k];
+    }
+    float gv[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) gv[k] = g.get(k), out[k] = p.get(k);
+    u.moments(gv, mv, vv);
+    u.weights(out, mv, vv);
+    if (n < kBlock) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i + k >= n) mv[k] = vv[k] = 0.f;
     }
     if (i + 4 <= n) {
       Four<P>::template store<STREAM>(pp + i, out);
@@ -225,19 +287,18 @@ struct Block {
         top_m = a > top_m ? a : top_m;
         top_v = b > top_v ? b : top_v;
       }
-      const float new_m = as_float(wave_max(top_m)) * (1.f / kTopM), new_v = as_float(wave_max(top_v)) * (1.f / kTopV);
-      // (a block of zeros, or of magnitudes whose scale float32 cannot hold)
-      const Quotient div_m(new_m > 0.f ? new_m : 1.f), div_v(new_v > 0.f ? new_v : 1.f);
+      wave_max2(top_m, top_v);
+      const float new_m = as_float(top_m) * (1.f / kTopM), new_v = as_float(top_v) * (1.f / kTopV);
+      float ym[4], yv[4];
+      in_units(new_m, mv, ym);
+      in_units(new_v, vv, yv);
       uint32_t to_m = 0, to_v = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint32_t bits = mix(index + (uint32_t)(i + k) + key);
-        uint32_t c = code_of<3>(div_m(fabsf(mv[k])), bits & 0xFFFFu);
-        if (mv[k] < 0.f) c |= 0x80u;
-        to_m |= c << (8 * k);
-        c = code_of<4>(div_v(vv[k]), bits >> 16);
-        if (vv[k] > 0.f && c == 0) c = 1;
-        to_v |= c << (8 * k);
+        const uint32_t bits = mix(index + (uint32_t)(i + k) + key), sign = __builtin_bit_cast(uint32_t, mv[k]) >> 31;
+        to_m |= (code_of<3>(ym[k], bits & 0xFFFFu, 0u) | sign << 7) << (8 * k);
+        const uint32_t least = __builtin_elementwise_min(__builtin_bit_cast(uint32_t, vv[k]), 1u);      // (v is not negative)
+        to_v |= code_of<4>(yv[k], bits >> 16, least) << (8 * k);
       }
       store_as<STREAM>((uint32_t*)((uint8_t*)s.m + moment) + lane, to_m);
       store_as<STREAM>((uint32_t*)((uint8_t*)s.v + moment) + lane, to_v);
@@ -252,25 +313,25 @@ struct Block {
   }
 };
 
-// A piece: each wave takes kAtOnce blocks, all of them loaded before the first is computed.
-template <class P, class G, bool EIGHT, bool STREAM>
+// A piece: each wave takes AT_ONCE blocks, all of them loaded before the first is computed.
+template <class P, class G, bool EIGHT, bool STREAM, int AT_ONCE>
 __device__ __forceinline__ void update_piece(P* p, const G* g, uint16_t* copy, int n, const Moments& s, int64_t moment, const Update& u,
                                              uint32_t key, uint32_t index) {
   const int first = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * kBlock;
-  Block<P, G, EIGHT> b[kAtOnce];
+  Block<P, G, EIGHT> b[AT_ONCE];
 #pragma unroll
-  for (int q = 0; q < kAtOnce; ++q) {
+  for (int q = 0; q < AT_ONCE; ++q) {
     const int at = first + q * 4 * kBlock;
     if (at < n) b[q].template load<STREAM>(p + at, g + at, s, moment + at, n - at);
   }
 #pragma unroll
-  for (int q = 0; q < kAtOnce; ++q) {
+  for (int q = 0; q < AT_ONCE; ++q) {
     const int at = first + q * 4 * kBlock;
     if (at < n) b[q].template step<STREAM>(p + at, copy ? copy + at : nullptr, s, moment + at, n - at, u, key, index + at);
   }
 }
 
-template <int CAP, bool EIGHT, bool STREAM>
+template <int CAP, bool EIGHT, bool STREAM, int AT_ONCE>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensors<CAP> a, const Moments s, const Betas b, const Factors* factors) {
   const Factors f = *factors;
   if (f.skip) return;
@@ -280,8 +341,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors<CAP> a, const 
   for (uint32_t c = blockIdx.x; c < pieces; c += gridDim.x) {
     // the last tensor whose first piece is not behind it
     const int k = __popcll(__ballot(firsts <= c)) - 1;
-    const int64_t at = (int64_t)(c - a.first[k]) * kPiece;
-    const int n = a.values(c, k);
+    const int64_t at = (int64_t)(c - a.first[k]) * piece_of(AT_ONCE);
+    const int n = a.values(c, k, piece_of(AT_ONCE));
     const Update u{f, b, 1.f - f.lr * a.decay[k]};
     const uint32_t key = mix(mix(f.key + (uint32_t)(a.number + k)));
     const int64_t moment = a.block[k] * kBlock + at;
@@ -289,12 +350,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors<CAP> a, const 
     const bool pb = a.p_bf16[k >> 5] >> (k & 31) & 1u, gb = a.g_bf16[k >> 5] >> (k & 31) & 1u;
     if (pb) {
       uint16_t* p = (uint16_t*)a.p[k] + at;
-      gb ? update_piece<uint16_t, uint16_t, EIGHT, STREAM>(p, (const uint16_t*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at)
-         : update_piece<uint16_t, float, EIGHT, STREAM>(p, (const float*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at);
+      gb ? update_piece<uint16_t, uint16_t, EIGHT, STREAM, AT_ONCE>(p, (const uint16_t*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at)
+         : update_piece<uint16_t, float, EIGHT, STREAM, AT_ONCE>(p, (const float*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at);
     } else {
       float* p = (float*)a.p[k] + at;
-      gb ? update_piece<float, uint16_t, EIGHT, STREAM>(p, (const uint16_t*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at)
-         : update_piece<float, float, EIGHT, STREAM>(p, (const float*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at);
+      gb ? update_piece<float, uint16_t, EIGHT, STREAM, AT_ONCE>(p, (const uint16_t*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at)
+         : update_piece<float, float, EIGHT, STREAM, AT_ONCE>(p, (const float*)a.g[k] + at, copy, n, s, moment, u, key, (uint32_t)at);
     }
   }
 }
@@ -305,15 +366,15 @@ __global__ __launch_bounds__(256) void adam8_values_kernel(const uint8_t* codes,
   const int64_t lanes = blocks * (kBlock / 8);
   for (int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x; j < lanes; j += (int64_t)gridDim.x * 256) {
     const u32x2 q = __builtin_nontemporal_load((const u32x2*)codes + j);
-    const float s = scale[j / (kBlock / 8)] * (SECOND ? 8.f : 4.f);
-    float v[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = SECOND ? second_moment(q[k / 4], k % 4, s) : first_moment(q[k / 4], k % 4, s);
+    const Decoder<SECOND ? 4 : 3> values(scale[j / (kBlock / 8)]);
+    float a[4], b[4];
+    values.template get<true>(q[0], a);
+    values.template get<true>(q[1], b);
     E* to = out + 8 * j;
     if constexpr (sizeof(E) == 2) {
+      const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
       Span<E>::template store<true>(to, v);
     } else {
-      const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
       Span<E>::template store<true>(to, a);
       Span<E>::template store<true>(to + 4, b);
     }
@@ -327,16 +388,19 @@ hipError_t launch_update(const AdamwArgs& c, int64_t k0, int count, int64_t& blo
   Tensors<kTensors> a{};
   a.count = count;
   a.number = (int)k0;
+  bool small = EIGHT;
+  for (int k = 0; k < count; ++k) small = small && c.param_dtype[k0 + k] == ELAS_GRAD_BF16;
+  const int64_t piece = piece_of(small ? 2 : 1);
   uint32_t pieces = 0;
   for (int k = 0; k < count; ++k) {
-    const int64_t n = c.numel[k0 + k], of = (n + kPiece - 1) / kPiece;
+    const int64_t n = c.numel[k0 + k], of = (n + piece - 1) / piece;
     a.p[k] = c.params[k0 + k];
     a.g[k] = c.grads[k0 + k];
     a.copy[k] = c.copies ? c.copies[k0 + k] : nullptr;
     a.block[k] = block;
     a.first[k] = pieces;
     a.decay[k] = c.decay[k0 + k];
-    a.last[k] = (uint16_t)(n - (of - 1) * kPiece);
+    a.last[k] = (uint16_t)(n - (of - 1) * piece);
     pieces += (uint32_t)of;
     block += (n + kBlock - 1) / kBlock;
     if (c.param_dtype[k0 + k] == ELAS_GRAD_BF16) a.p_bf16[k >> 5] |= 1u << (k & 31);
@@ -347,10 +411,14 @@ hipError_t launch_update(const AdamwArgs& c, int64_t k0, int count, int64_t& blo
   const Moments s{c.m, c.v, c.m_scale, c.v_scale};
   TimedLaunch tl(EIGHT ? "adamw8" : "adamw", stream);
   const dim3 grid(std::min<uint32_t>(pieces, kGroups));
-  if (stream_data)
-    hipLaunchKernelGGL((adamw_kernel<kTensors, EIGHT, true>), grid, dim3(256), 0, stream, a, s, b, (const Factors*)c.ws);
-  else
-    hipLaunchKernelGGL((adamw_kernel<kTensors, EIGHT, false>), grid, dim3(256), 0, stream, a, s, b, (const Factors*)c.ws);
+  const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, s, b, (const Factors*)c.ws); };
+  if constexpr (EIGHT) {
+    if (small) {
+      stream_data ? launch(adamw_kernel<kTensors, true, true, 2>) : launch(adamw_kernel<kTensors, true, false, 2>);
+      return hipGetLastError();
+    }
+  }
+  stream_data ? launch(adamw_kernel<kTensors, EIGHT, true, 1>) : launch(adamw_kernel<kTensors, EIGHT, false, 1>);
   return hipGetLastError();
 }
 

@@ -65,8 +65,9 @@ def _check_codes(code, scale, x, err, mantissa, bits, name):
     # the scale: the largest magnitude's error, and two roundings (a reciprocal and its product)
     assert np.all(np.abs(scale - top / oa.TOP[mantissa]) <= err.max(axis=1) / oa.TOP[mantissa] + 2 * EPS32 * scale + 2.0 ** -149), name
     s = np.where(scale > 0, scale, 1.0)[:, None]
-    # (2 roundings: the quotient's, and of the sum with the random bits)
-    lo, hi = np.maximum(x - err, 0) / s * (1 - 3 * EPS32), (x + err) / s * (1 + 3 * EPS32)
+    # (2 roundings: the quotient's, and, below 2^mantissa, of it to a multiple of 2^-(23 - mantissa))
+    low = 2.0 ** -(24 - mantissa)
+    lo, hi = np.maximum(np.maximum(x - err, 0) / s * (1 - 3 * EPS32) - low, 0), (x + err) / s * (1 + 3 * EPS32) + low
     a, b = oa.codes(lo, bits, mantissa), oa.codes(hi, bits, mantissa)
     code = code.reshape(-1, 256)
     if mantissa == 4:
