@@ -2,14 +2,15 @@
 training step uses them together:
 
     ids -> embedding -> [norm -> low-rank 2:4 FFN -> norm, gate, residual sum] x L
-        -> norm -> loss -> the same backward -> clipping -> update
+        -> norm -> logits -> token loss -> the same backward -> gradient norm -> AdamW
 
-    python examples/train_stack.py [--steps N] [--tokens T] [--layers L]
+    python examples/train_stack.py [--steps N] [--tokens T] [--layers L] [--bits 8]
 
-Each token learns to predict a fixed vector of the token that follows it (a
-permutation of the vocabulary), so no sequence mixing is needed.  torch provides
-the memory, the squared-error loss and the update of the float32 master weights;
-everything between is libelas.
+Each token learns to predict the token that follows it (a permutation of the
+vocabulary), so no sequence mixing is needed.  torch provides the memory and the
+dense products of the logits' layer; everything else is libelas: the loss writes its
+gradient over the logits, and the update of the float32 master weights clips the
+gradients and writes the bf16 copies.
 """
 from __future__ import annotations
 
@@ -26,9 +27,10 @@ BF = torch.bfloat16
 
 
 class Stack:
-    """Weights of the stack: float32 masters, their bf16 copies and gradients."""
+    """Weights of the stack: float32 masters, their bf16 copies and gradients, and AdamW's state.  The logits' layer is
+    apart from the rest: ``forward`` and ``backward`` go to and from the final norm's output."""
 
-    def __init__(self, vocab: int, d: int, d_ff: int, r: int, layers: int, seed: int = 0, mode: int = elas.ELAS_MODE_SPARSE24):
+    def __init__(self, vocab: int, d: int, d_ff: int, r: int, layers: int, seed: int = 0, mode: int = elas.ELAS_MODE_SPARSE24, bits: int = 32):
         gen = torch.Generator(device="cuda")
         gen.manual_seed(seed)
         self.vocab, self.d, self.layers, self.mode = vocab, d, layers, mode
@@ -49,7 +51,12 @@ class Stack:
             self.master[f"{k}.w_pre"] = torch.ones(d, device="cuda")
         self.w = {k: v.to(BF) for k, v in self.master.items()}
         self.grad = {k: torch.empty_like(v) for k, v in self.master.items()}
-        self.grads = elas.ElasTensors(self.grad.values())
+        self.head_master = normal(vocab, d, sigma=d ** -0.5)
+        self.head = self.head_master.to(BF)
+        self.head_grad = torch.empty_like(self.head_master)
+        self.grads = elas.ElasTensors([*self.grad.values(), self.head_grad])
+        masters = [*self.master.values(), self.head_master]
+        self.opt = elas.ElasAdamW(masters, copies=[*self.w.values(), self.head], decay=[0.1 * (m.dim() > 1) for m in masters], bits=bits)
 
     def factors(self, k: int):
         return [self.w[f"{k}.{n}"] for n in ("U_up", "V_up", "U_down", "V_down")]
@@ -89,36 +96,40 @@ class Stack:
         elas.elas_norm_join_bwd(dh, dn, h0, w_pre=self.w["0.w_pre"], grads=g)
         elas.elas_embed_bwd(ids, dh, self.vocab, self.d ** 0.5, dtable=self.grad["table"])
 
+    def loss(self, n: torch.Tensor, targets: torch.Tensor):
+        """The mean cross-entropy of the targets ([1], with its z term beside it: stats [2]), the gradient of n;
+        fills ``head_grad``."""
+        logits = n @ self.head.t()
+        out = {"stats": torch.empty(2, device="cuda"), "dlogits": logits}      # (the gradient over the logits)
+        elas.elas_token_loss(logits, targets, reduce=1 / targets.numel(), z_coef=1e-4, out=out)
+        self.head_grad.copy_(logits.t() @ n)
+        return out["stats"], logits @ self.head
+
     def update(self, rate: float, max_norm: float) -> torch.Tensor:
-        """Clips the gradients in place and takes a step; returns (norm, factor).
-        Where the norm is not finite the factor is 0 and the step is skipped."""
-        stats = elas.elas_grad_clip(self.grads, max_norm)
-        step = torch.where(stats[1] > 0, -rate, 0.0)
-        for k, m in self.master.items():
-            m.add_(torch.nan_to_num(self.grad[k]) * step)
-            self.w[k].copy_(m)
-        return stats
+        """A step of AdamW with the gradients clipped to max_norm; returns their norm.  Where it is not
+        finite the step is skipped."""
+        norm = elas.elas_grad_norm(self.grads)
+        elas.elas_adamw_step(self.opt, self.grads, rate, beta2=0.95, norm=norm, max_norm=max_norm)
+        return norm
 
 
-def train(steps: int, tokens: int, layers: int, vocab: int = 1000, d: int = 256, d_ff: int = 688, r: int = 64, rate: float = 1.0,
-          max_norm: float = 1.0, seed: int = 0, log=None) -> list:
+def train(steps: int, tokens: int, layers: int, vocab: int = 1000, d: int = 256, d_ff: int = 688, r: int = 64, rate: float = 1e-2,
+          max_norm: float = 1.0, seed: int = 0, bits: int = 32, log=None) -> list:
     """Losses of the steps."""
-    model = Stack(vocab, d, d_ff, r, layers, seed)
+    model = Stack(vocab, d, d_ff, r, layers, seed, bits=bits)
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed + 1)
     follows = torch.randperm(vocab, generator=gen, device="cuda")
-    targets = torch.randn(vocab, d, generator=gen, device="cuda")
     losses = []
     for step in range(steps):
         ids = torch.randint(0, vocab, (tokens,), generator=gen, device="cuda")
         n, saved = model.forward(ids)
-        diff = n.float() - targets[follows[ids]]
-        model.backward((diff / tokens).to(BF), saved)
-        stats = model.update(rate, max_norm)
-        losses.append(diff.square().mean())
+        stats, dn = model.loss(n, follows[ids])
+        model.backward(dn, saved)
+        norm = model.update(rate, max_norm)
+        losses.append(stats[0])
         if log and step % log == 0:
-            print(f"step {step:4d}  loss {float(losses[-1]):.4f}  gradient norm {float(stats[0]):.3f}  factor {float(stats[1]):.3f}",
-                  flush=True)
+            print(f"step {step:4d}  loss {float(stats[0]):.4f}  gradient norm {float(norm):.3f}", flush=True)
     return [float(v) for v in losses]
 
 
@@ -127,5 +138,6 @@ if __name__ == "__main__":
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--tokens", type=int, default=4096)
     ap.add_argument("--layers", type=int, default=3)
+    ap.add_argument("--bits", type=int, choices=(8, 32), default=32, help="of AdamW's moments")
     a = ap.parse_args()
-    train(a.steps, a.tokens, a.layers, log=20)
+    train(a.steps, a.tokens, a.layers, bits=a.bits, log=20)

@@ -45,7 +45,7 @@ extern "C" {
  *          sign.  The scale is the block's largest magnitude / 245760 (v: 507904).  A magnitude
  *          is rounded to one of its two neighbours by chance, so that its expectation is
  *          its value and averages that move by less than a step move all the same; the
- *          random bits are a hash of t, k and the value's index, so a step can be repeated.
+ *          random bits are a hash of t, k and the value's index (32 bits of it), so a step can be repeated.
  *          A v above 0 is never rounded to 0.  A block that a value which is not finite gets
  *          into has a scale that is not finite either.
  * step           device int64 [1], 8-byte aligned: steps taken; raised by 1 in the call.

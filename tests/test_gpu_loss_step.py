@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2605_03667_amd as elas
+from examples.train_stack import Stack
 
 pytestmark = pytest.mark.gpu
 
@@ -241,3 +242,51 @@ def test_debug_sync_same_results():
     finally:
         elas.elas_debug_sync(prev)
     assert all(torch.equal(x, y) for x, y in zip(a.state(), b.state()))
+
+
+def test_example_gradients():
+    """The example's gradients of its loss, against float32 autograd of the same stack at its bf16 weights (dense
+    activations).  Between the two lie the bf16 roundings of the block's intermediate values, of the logits and of their
+    gradient, about a dozen a block of relative size 2^-9 each: a percent; 3 % is allowed."""
+    model = Stack(300, 256, 344, 64, 2, seed=3, mode=elas.ELAS_MODE_DENSE)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    ids, targets = (torch.randint(0, 300, (777,), generator=g, device=DEV) for _ in range(2))
+    n, saved = model.forward(ids)
+    stats, dn = model.loss(n, targets)
+    model.backward(dn, saved)
+
+    w = {k: v.float().requires_grad_() for k, v in [*model.w.items(), ("head", model.head)]}
+
+    def norm(v, gain):
+        return v * torch.rsqrt(v.square().mean(-1, keepdim=True) + 1e-6) * gain
+
+    h = w["table"][ids] * model.d ** 0.5
+    for k in range(model.layers):
+        s = torch.relu(norm(h, w[f"{k}.w_pre"]) @ w[f"{k}.U_up"] @ w[f"{k}.V_up"]).square()
+        h = h + model.block_scale * w[f"{k}.gate"] * norm(s @ w[f"{k}.U_down"] @ w[f"{k}.V_down"], w[f"{k}.w_post"])
+    z = norm(h, w[f"{model.layers}.w_pre"]) @ w["head"].t()
+    lse = torch.logsumexp(z, 1)
+    loss = (lse - z[torch.arange(777), targets] + 1e-4 * lse ** 2).mean()
+    loss.backward()
+    assert abs(float(stats[0]) - loss.item()) < 0.01 * loss.item()
+    for k, grad in [*model.grad.items(), ("head", model.head_grad)]:
+        assert torch.linalg.norm(grad - w[k].grad) < 0.03 * torch.linalg.norm(w[k].grad), k
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_example_step(bits):
+    """A step of the example changes every weight by at most about the rate (AdamW's first step moves a value by
+    the rate where its gradient is above eps, and by the decay), and writes the copies of the new weights."""
+    model = Stack(200, 128, 344, 64, 2, seed=1, bits=bits)
+    before = {k: v.clone() for k, v in model.master.items()}
+    ids = torch.randint(0, 200, (512,), device=DEV)
+    n, saved = model.forward(ids)
+    _, dn = model.loss(n, ids.flip(0))
+    model.backward(dn, saved)
+    norm = model.update(1e-2, 1.0)
+    assert torch.isfinite(norm).all() and int(model.opt.step) == 1
+    for k, v in model.master.items():
+        moved = (v - before[k]).abs()
+        assert moved.max() > 0 and (moved <= 1e-2 * (1.001 + 0.1 * before[k].abs()) + 2.0 ** -23 * before[k].abs()).all(), k
+        assert torch.equal(model.w[k], v.to(BF)), k
