@@ -14,7 +14,7 @@
  * ids      [T] int32 (ELAS_IDS_I64: int64).  A token whose id is outside 0 .. V-1
  *          (padding, a prompt) takes no part: its logits are not read, its results
  *          are 0, and its row of the gradient is zeros.
- * scale    z = scale logits (the inverse temperature), finite and > 0.
+ * scale    z = scale logits (the inverse temperature), 0 < scale <= 2^100.
  * With lse_t = log sum_j exp z_tj, logp_t = z_t,id - lse_t and p = exp(z - lse).
  * dlogits  T rows of V values of the logits' type, row t at dlogits + t ld_out, ld_out >= V;
  *          what lies behind the V values of a row is not touched.  It may be
@@ -55,7 +55,8 @@ int elas_token_logp_fwd(const void* logits, int64_t ld, const void* ids, int64_t
  *
  *     dlogits_tj = scale (dlogp_t (1[j = id_t] - p_tj) + dlse_t p_tj)
  *
- * lse is the forward's; dlse NULL: zero.
+ * lse is the forward's on these logits (p = exp(z - lse) has a relative error of 2^-24 (|z| + 3 |z - lse| + 6);
+ * where |lse| is above 4096 or not finite the row's sum is taken anew); dlse NULL: zero.
  */
 int elas_token_logp_bwd(const float* dlogp, const float* dlse, const void* logits, int64_t ld, const void* ids,
                         const float* lse, int64_t T, int64_t V, float scale, uint32_t flags, void* dlogits,

@@ -40,7 +40,7 @@ int elas_adamw_step(void* const* params, const void* const* grads, uint16_t* con
   begin_call();
   if (n < 0 || n > kMaxTensors) return fail(ELAS_ERR_SHAPE, "n=%lld out of range", (long long)n);
   if (bits != 8 && bits != 32) return fail(ELAS_ERR_SHAPE, "bits=%d must be 8 or 32", bits);
-  ELAS_CHECK(check_scale(rate, "rate"));
+  ELAS_CHECK(check_scale((float)rate, "rate (as float32)"));
   ELAS_CHECK(check_beta(beta1, "beta1"));
   ELAS_CHECK(check_beta(beta2, "beta2"));
   if (!((float)eps > 0.f) || !isfinite((float)eps)) return fail(ELAS_ERR_SHAPE, "eps must be positive and finite in float32");

@@ -24,8 +24,7 @@ int check_logits(LogitsArgs& a, const void* logits, int64_t ld, const void* ids,
   if (flags & ~(ELAS_LOGITS_F32 | ELAS_IDS_I64)) return fail(ELAS_ERR_FLAGS, "flags: only ELAS_LOGITS_F32 and ELAS_IDS_I64 are allowed");
   if (T < 0 || T > kMaxTokens) return fail(ELAS_ERR_SHAPE, "T=%lld out of range", (long long)T);
   if (V <= 0 || V > kMaxVocab) return fail(ELAS_ERR_SHAPE, "V=%lld out of range", (long long)V);
-  ELAS_CHECK(check_scale(scale, "scale"));
-  if (!(scale > 0.f)) return fail(ELAS_ERR_SHAPE, "scale must be positive");
+  if (!(scale > 0.f && scale <= 0x1p100f)) return fail(ELAS_ERR_SHAPE, "scale must be positive and at most 2^100");
   if (ld < V || ld > kMaxPitch) return fail(ELAS_ERR_SHAPE, "ld=%lld must be at least V=%lld and at most 2^31", (long long)ld, (long long)V);
   if (dlogits && (ld_out < V || ld_out > kMaxPitch))
     return fail(ELAS_ERR_SHAPE, "ld_out=%lld must be at least V=%lld and at most 2^31", (long long)ld_out, (long long)V);

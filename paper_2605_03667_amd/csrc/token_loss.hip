@@ -382,6 +382,124 @@ __global__ __launch_bounds__(Team<WAVES>::THREADS * Team<WAVES>::ROWS) void held
   sum.write(sums, a.part);
 }
 
+// Few rows: each is split over workgroups, in two launches.  The first leaves every part's maximum and sum, and the
+// label's logit (a gradient may take the logits' place); the second joins them, every workgroup for itself, and
+// writes its part of the gradient, and one more workgroup, a row to a thread, the rows' results and the statistics.
+struct Split {
+  float2* part;       // [T][parts]: maximum, sum
+  float* label;       // [T]
+  float* stats;
+  int parts, per;     // parts of a row (kParts at most), pieces of one
+};
+
+// Whether a row takes part.
+__device__ __forceinline__ bool row_of(const Rows& a, int64_t t, int64_t& id, float& w) {
+  id = id_of(a.ids, a.ids_i64, t);
+  w = a.weight ? a.weight[t] : 1.f;
+  return id >= 0 && id < a.V && w != 0.f;
+}
+
+template <class E>
+__global__ __launch_bounds__(256) void split_kernel(const Rows a, const Split sp) {
+  __shared__ float red[2 * 4 + 1];
+  const int tid = threadIdx.x, part = blockIdx.x;
+  const int64_t t = blockIdx.y;
+  int64_t id;
+  float w;
+  if (!row_of(a, t, id, w)) return;
+  const float c = a.scale * kLog2E;
+  const E* x = (const E*)a.logits + t * a.ld;
+  const Cut<E> cut(a.dlogits ? (const E*)a.dlogits + t * a.ld_out : x, a.V);
+  MaxSum r;
+  const int first = part * sp.per, end = first + sp.per;
+  add_pieces<E, false>(r, c, x + cut.lead, first + tid, end < cut.full ? end : cut.full, 256);
+  if (part == 0 && tid < cut.edges) add_value(r, c, span_value(x[cut.edge(tid)]));
+  const float label = whole_row<4>(r, c, x + id, red);
+  if (tid == 0) {
+    sp.part[t * sp.parts + part] = make_float2(r.m, r.s);
+    if (part == 0) sp.label[t] = label;
+  }
+}
+
+template <int KIND, class E>
+__global__ __launch_bounds__(256) void join_kernel(const Rows a, const Split sp) {
+  using S = Span<E>;
+  constexpr int N = S::N;
+  __shared__ double red[4];
+  const int tid = threadIdx.x, lane = tid & 63, part = blockIdx.x;
+  const float c = a.scale * kLog2E;
+  if (blockIdx.y == gridDim.y - 1) {
+    if (part > 0) return;
+    double sum[kSums] = {0.0, 0.0, 0.0};
+    for (int64_t t = tid; t < a.T; t += 256) {
+      int64_t id;
+      float w, logp = 0.f, lse = 0.f;
+      if (row_of(a, t, id, w)) {
+        MaxSum r;
+        for (int k = 0; k < sp.parts; ++k) {
+          const float2 v = sp.part[t * sp.parts + k];
+          add(r, c, MaxSum{v.x, v.y});
+        }
+        const Terms o = row_terms<KIND>(a, t, w, sp.label[t], r, &logp, &lse);
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) sum[k] += o.sum[k];
+      }
+      write_row(a, t, logp, lse);
+    }
+#pragma unroll
+    for (int k = 0; k < (KIND == LogitsArgs::LOGP ? 0 : KIND == LogitsArgs::TOKEN ? 2 : 3); ++k) {
+      const double v = block_sum<4>(sum[k], red);
+      if (tid == 0) sp.stats[k] = (float)v;
+    }
+    return;
+  }
+  const int64_t t = blockIdx.y;
+  int64_t id;
+  float w;
+  const bool on = row_of(a, t, id, w);
+  const E* x = (const E*)a.logits + t * a.ld;
+  E* d = (E*)a.dlogits + t * a.ld_out;
+  const Cut<E> cut(d, a.V);
+  const int first = part * sp.per + tid, end = (part + 1) * sp.per < cut.full ? (part + 1) * sp.per : cut.full;
+  const bool edge = part == 0 && tid < cut.edges;
+  MaxSum r;
+  Terms o{};
+  if (on) {
+    if (lane < sp.parts) {
+      const float2 v = sp.part[t * sp.parts + lane];
+      r.m = v.x, r.s = v.y;
+    }
+    r.rescale(wave_max(r.m), c);
+    r.s = wave_sum(r.s);
+    float logp, lse;
+    o = row_terms<KIND>(a, t, w, sp.label[t], r, &logp, &lse);
+  }
+  const int at = on ? (int)id - cut.lead : -1;
+  for (int i = first; i < end; i += 256) {
+    float v[N] = {};
+    if (on) {
+      S p;
+      p.template load<false>(at_value(x + cut.lead, i * N));
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[k] = __builtin_amdgcn_exp2f((p.get(k) - r.m) * c) * o.all;
+      if ((unsigned)(at - i * N) < (unsigned)N) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += at - i * N == k ? o.label : 0.f;
+      }
+    }
+    S::template store<false>(at_value(d + cut.lead, i * N), v);
+  }
+  if (edge) {
+    const int i = cut.edge(tid);
+    float v = 0.f;
+    if (on) {
+      v = __builtin_amdgcn_exp2f((span_value(x[i]) - r.m) * c) * o.all;
+      if (i == (int)id) v += o.label;
+    }
+    set_span_value(d + i, v);
+  }
+}
+
 __global__ __launch_bounds__(1024) void loss_sum_kernel(const double* part, int groups, int count, float* stats) {
   __shared__ double red[16];
   double s[kSums] = {0.0, 0.0, 0.0};
@@ -396,7 +514,10 @@ __global__ __launch_bounds__(1024) void loss_sum_kernel(const double* part, int 
   }
 }
 
-// Gradient from those of logp and lse: every value by itself, kChunk pieces of a row to a thread at a time.
+// Gradient from those of logp and lse: every value by itself, kChunk pieces of a row to a thread at a time.  (A
+// lse beyond kLargeLse leaves exp(z - lse) an error of 2^-24 of that, and among logits of a type's lowest value it holds
+// nothing of the sum at all.)
+constexpr float kLargeLse = 4096.f;
 constexpr int kChunk = 2;
 
 struct BwdRows {
@@ -413,6 +534,7 @@ template <class E, int TH>
 __global__ __launch_bounds__(TH) void logp_bwd_kernel(const BwdRows a) {
   using S = Span<E>;
   constexpr int N = S::N;
+  __shared__ float red[2 * (TH / 64) + 1];
   const int tid = threadIdx.x;
   const int64_t items = a.T * a.chunks;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
@@ -437,6 +559,30 @@ __global__ __launch_bounds__(TH) void logp_bwd_kernel(const BwdRows a) {
     const float g = a.dlogp[t], e = a.dlse ? a.dlse[t] : 0.f, lse = a.lse[t];
     const float at_label = a.scale * g, all = a.scale * (e - g);
     const int at = (int)id - cut.lead;
+    if (!(fabsf(lse) <= kLargeLse)) {
+      // the whole row by its first workgroup, which finds its maximum and sum anew
+      if (chunk > 0) continue;
+      const float c = a.scale * kLog2E;
+      MaxSum r;
+      add_pieces<E, false>(r, c, xp, tid, cut.full, TH);
+      if (edge) add_value(r, c, span_value(x[cut.edge(tid)]));
+      __syncthreads();      // (`red` may still be read from another such row)
+      whole_row<TH / 64>(r, c, x + id, red);
+      const float share = all / r.s;
+      for (int i = tid; i < cut.full; i += TH) {
+        S q;
+        q.template load<false>(at_value(xp, i * N));
+        float v[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = __builtin_amdgcn_exp2f((q.get(k) - r.m) * c) * share + (at - i * N == k ? at_label : 0.f);
+        S::template store<false>(at_value(dp, i * N), v);
+      }
+      if (edge) {
+        const int i = cut.edge(tid);
+        set_span_value(d + i, __builtin_amdgcn_exp2f((span_value(x[i]) - r.m) * c) * share + (i == (int)id ? at_label : 0.f));
+      }
+      continue;
+    }
     S p[kChunk];
 #pragma unroll
     for (int q = 0; q < kChunk; ++q)
@@ -465,6 +611,42 @@ __global__ __launch_bounds__(TH) void logp_bwd_kernel(const BwdRows a) {
 // ---- host -----------------------------------------------------------------------------
 
 int groups_of(int64_t T) { return (int)std::min<int64_t>(T, kGroups); }
+
+// Whether rows are split, and how: few rows of 16 KB and more, whose logits stay in the caches between the launches.
+constexpr int64_t kSplitRows = 256, kSplitRow = 16384, kSplitBytes = 8 << 20;
+constexpr int kParts = 16;
+struct SplitPlan {
+  bool split;
+  int parts, per;
+  SplitPlan(int64_t T, int64_t V, bool f32) {
+    const int64_t n = f32 ? 4 : 8, pieces = (V + n - 1) / n, bytes = pieces * 16;
+    split = T > 0 && T <= kSplitRows && bytes >= kSplitRow && T * bytes <= kSplitBytes;
+    const int64_t at_least = (pieces + kParts * 256 - 1) / (kParts * 256);
+    per = (int)(256 * std::max<int64_t>(at_least, 2));
+    parts = (int)((pieces + per - 1) / per);
+  }
+  size_t bytes(int64_t T) const { return (size_t)T * ((size_t)parts * sizeof(float2) + sizeof(float)); }
+};
+
+template <int KIND, class E>
+hipError_t launch_split(const Rows& r, const SplitPlan& plan, void* ws, float* stats, const char* tag, hipStream_t stream) {
+  Split sp{};
+  sp.part = (float2*)ws;
+  sp.label = (float*)(sp.part + r.T * plan.parts);
+  sp.stats = stats;
+  sp.parts = plan.parts;
+  sp.per = plan.per;
+  {
+    TimedLaunch tl("loss_split", stream);
+    hipLaunchKernelGGL(split_kernel<E>, dim3((unsigned)plan.parts, (unsigned)r.T), dim3(256), 0, stream, r, sp);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const dim3 grid = r.dlogits ? dim3((unsigned)plan.parts, (unsigned)r.T + 1) : dim3(1, 1);
+  TimedLaunch tl(tag, stream);
+  hipLaunchKernelGGL((join_kernel<KIND, E>), grid, dim3(256), 0, stream, r, sp);
+  return hipGetLastError();
+}
 
 template <int WAVES>
 dim3 grid_of(int64_t T) {
@@ -521,8 +703,8 @@ hipError_t launch_rows(const Rows& r, bool f32, const char* tag, unsigned* group
 }  // namespace
 
 size_t token_loss_workspace_bytes(int64_t T, int64_t V, bool f32) {
-  (void)V, (void)f32;
-  return (size_t)groups_of(T) * kSums * sizeof(double);
+  const SplitPlan plan(T, V, f32);
+  return plan.split ? plan.bytes(T) : (size_t)groups_of(T) * kSums * sizeof(double);
 }
 
 hipError_t run_token_loss(const LogitsArgs& a, hipStream_t stream) {
@@ -531,6 +713,12 @@ hipError_t run_token_loss(const LogitsArgs& a, hipStream_t stream) {
   r.ref_logp = a.ref_logp; r.logp = a.logp; r.lse = a.lse; r.part = (double*)a.ws; r.T = a.T; r.ld = a.ld; r.ld_out = a.ld_out;
   r.V = (int32_t)a.V; r.scale = a.scale; r.reduce = a.reduce; r.z_coef = a.z_coef; r.low = a.low; r.high = a.high; r.kl_coef = a.kl_coef;
   r.ids_i64 = a.ids_i64;
+  const SplitPlan plan(a.T, a.V, a.f32);
+  if (plan.split && a.kind != LogitsArgs::LOGP) {
+    const auto launch = [&](auto f32, auto bf16, const char* tag) { return (a.f32 ? f32 : bf16)(r, plan, a.ws, a.stats, tag, stream); };
+    return a.kind == LogitsArgs::TOKEN ? launch(launch_split<LogitsArgs::TOKEN, float>, launch_split<LogitsArgs::TOKEN, uint16_t>, "token_loss")
+                                       : launch(launch_split<LogitsArgs::POLICY, float>, launch_split<LogitsArgs::POLICY, uint16_t>, "policy_loss");
+  }
   unsigned groups = 0;
   if (a.T > 0) {
     const hipError_t e = a.kind == LogitsArgs::LOGP    ? launch_rows<LogitsArgs::LOGP>(r, a.f32, "token_logp", &groups, stream)

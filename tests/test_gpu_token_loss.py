@@ -113,6 +113,41 @@ def test_widths(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V, pitch", [(v, p) for v in WIDTHS if v >= 2047 for p in (0, 3)])
+def test_widths_of_many_tokens(V, pitch, dtype):
+    """(Few rows are split over workgroups, many are not.)  300 tokens, 6 of which take part, so that the oracle has few rows
+    to compute; all others have results and gradients of 0."""
+    T, on = 300, [0, 1, 128, 255, 256, 299]
+    x, ids, g = _inputs(T, V, dtype, V, pitch)
+    keep = ids.clone()
+    ids.fill_(-1)
+    ids[on] = keep[on]
+    n, i = _f64(x[on]), keep[on].cpu().numpy()
+    w = torch.rand(T, generator=g, device=DEV)
+    flat, d = _gradient_like(x, pitch)
+    out = {"stats": torch.empty(2, device=DEV), "logp": torch.empty(T, device=DEV), "lse": torch.empty(T, device=DEV), "dlogits": d}
+    adv = torch.randn(T, generator=g, device=DEV)
+    for name, got, want in (("token", elas.elas_token_loss(x, ids, weight=w, scale=1.25, reduce=0.5, z_coef=0.125, out=out),
+                             ol.token_loss(n, i, _f64(w[on]), 1.25, 0.5, 0.125)),
+                            ("policy", None, ol.policy_loss(n, i, _f64(adv[on]), None, None, _f64(w[on]), 1.25, 0.5, 0.25, 0.25, 0.0)[0])):
+        if got is None:
+            d.fill_(55.0)
+            out = {"stats": torch.empty(3, device=DEV), "logp": torch.empty(T, device=DEV), "dlogits": d}
+            got = elas.elas_policy_loss(x, ids, adv, weight=w, scale=1.25, reduce=0.5, clip_low=0.25, clip_high=0.25, out=out)
+        for k in want:
+            _near(got[k] if k == "stats" else got[k][on], *want[k], dtype if k == "dlogits" else F32, (name, k))
+        off = torch.ones(T, dtype=torch.bool, device=DEV)
+        off[on] = False
+        assert not d[off].any() and not got["logp"][off].any()
+        _check_frame(flat, d)
+    # in place
+    elas.elas_policy_loss(x, ids, adv, weight=w, scale=1.25, reduce=0.5, clip_low=0.25, clip_high=0.25,
+                          out={"stats": torch.empty(3, device=DEV), "dlogits": x})
+    _near(x[on], *want["dlogits"], dtype, "in place")
+    assert not x[off].any()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("T", [1, 2, 255, 2048, 2049, 5000])
 def test_token_counts(T, dtype):
     x, ids, g = _inputs(T, 301, dtype, T, padding=0.3, i64=False)
@@ -153,6 +188,37 @@ def test_the_types_lowest_value(V, dtype):
         _near(r["dlogits"][0], want, np.abs(want) * 2.0 ** -24 * (V / 64 + 70), dtype)
         assert float(r["logp"][1]) == 0 and float(r["lse"][1]) == scale
         assert not r["dlogits"][1].any()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [5, 300, 1100, 20001, 70000])
+def test_gradient_where_lse_holds_too_little(V, dtype):
+    """Logits far from 0, and rows of nothing but the type's lowest value: the gradient of log-probabilities is
+    the loss's, and within its bounds (no lse of float32 could give it)."""
+    x, ids, g = _inputs(7, V, dtype, V, pitch=3)
+    x[1] += 30000.0
+    x[2] -= 70000.0
+    x[3] = torch.finfo(dtype).min
+    x[4] = torch.finfo(dtype).min
+    x[4, V // 2] = 0.5
+    x[5] += 4000.0
+    ids[6] = -1
+    w = torch.rand(7, generator=g, device=DEV)
+    n, i, wn = _f64(x), ids.cpu().numpy(), _f64(w)
+    for scale in (1.0, 0.25, 2.0):
+        lse = elas.elas_token_logp_fwd(x, ids, scale=scale)["lse"]
+        want = ol.token_loss(n, i, wn, scale, 1.0, 0.0)["dlogits"]
+        d = elas.elas_token_logp_bwd(-w, x, ids, lse, scale=scale)
+        # rows of a smaller lse: the bound at a given one, and p's change by lse's own error
+        lse_err = ol.logp(n, i, scale)[3]
+        p = np.exp(scale * (n - n.max(axis=1, keepdims=True)))
+        p /= p.sum(axis=1, keepdims=True)
+        given = ol.logp_grad(-wn, np.zeros(7), n, i, _f64(lse), scale)[1] + 1.01 * scale * (wn * lse_err)[:, None] * p
+        bound = np.where(np.abs(_f64(lse))[:, None] <= 4096, given, want[1])
+        _near(d, want[0], bound, dtype, scale)
+        y = _gradient_like(x, 3)[1].copy_(x)
+        elas.elas_token_logp_bwd(-w, y, ids, lse, scale=scale, dlogits=y)
+        _near(y, want[0], bound, dtype, "in place")
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -222,9 +288,10 @@ def test_in_place(V, dtype):
     assert torch.equal(one["stats"], two["stats"]) and torch.equal(one["dlogits"], two["dlogits"])
 
 
-def test_outputs_that_are_not_wanted():
+@pytest.mark.parametrize("V", [900, 20000])
+def test_outputs_that_are_not_wanted(V):
     """A loss without its gradient adds a row's values up in another order: within the same bounds."""
-    x, ids, g = _inputs(50, 900, BF, 1)
+    x, ids, g = _inputs(50, V, BF, 1)
     a = torch.rand(50, generator=g, device=DEV)
     n, i = _f64(x), ids.cpu().numpy()
     alone = elas.elas_token_loss(x, ids, z_coef=0.1, out={"stats": torch.empty(2, device=DEV)})

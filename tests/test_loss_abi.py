@@ -71,7 +71,7 @@ def test_refusals_on_logits(call):
         assert call(V=V) == SHAPE
     for ld in (9, 0, -16, (1 << 31) + 1):
         assert call(ld=ld) == SHAPE
-    for scale in (0.0, -1.0, INF, NAN):
+    for scale in (0.0, -1.0, INF, NAN, 2.0 ** 101):
         assert call(scale=scale) == SHAPE
     assert call(x=None) == NULL and call(x=A + 1) == ALIGN and call(x=A + 2, flags=elas.ELAS_LOGITS_F32) == ALIGN
     assert call(ids=None) == NULL and call(ids=A + 2) == ALIGN and call(ids=A + 4, flags=elas.ELAS_IDS_I64) == ALIGN
@@ -153,7 +153,7 @@ def test_adamw_refusals():
         assert call(b1=bad) == SHAPE and call(b2=bad) == SHAPE
     for bad in (0.0, -1.0, NAN, INF, 1e-60, 1e60):
         assert call(eps=bad) == SHAPE
-    assert call(rate=NAN) == SHAPE and call(max=-1.0) == SHAPE and call(max=NAN) == SHAPE
+    assert call(rate=NAN) == SHAPE and call(rate=1e300) == SHAPE and call(max=-1.0) == SHAPE and call(max=NAN) == SHAPE
     assert call(step=None) == NULL and call(step=A + 4) == ALIGN and call(norm=A + 2) == ALIGN and call(factor=A + 1) == ALIGN
     assert call(ws=None) == NULL and call(ws=A + 8) == ALIGN and call(wsb=elas.elas_adamw_workspace_bytes() - 1) == WORKSPACE
 
