@@ -26,7 +26,7 @@
  * A logit may be -inf (its p is 0).  Where a row holds nothing but -inf, a NaN or +inf,
  * its results follow the formulas (NaN, lse -inf), and so do the statistics; other rows do not change.
  * Requires 0 <= T < 2^31, 0 < V <= 2^30.  With T == 0 statistics are zeros and nothing else is
- * written.  workspace >= elas_token_loss_workspace_bytes(T, V, flags) bytes, 16-byte aligned.
+ * written.
  */
 #ifndef ELAS_LOSS_H
 #define ELAS_LOSS_H
@@ -41,14 +41,11 @@ extern "C" {
 /* logits and dlogits are float32 instead of bf16. */
 #define ELAS_LOGITS_F32     1u
 
-/* Workspace of the calls below on T rows of V logits (0 for sizes that no call takes). */
-size_t elas_token_loss_workspace_bytes(int64_t T, int64_t V, uint32_t flags);
-
 /*
  * elas_token_logp_fwd -- logp and lse of every token.  lse may be NULL.
  */
 int elas_token_logp_fwd(const void* logits, int64_t ld, const void* ids, int64_t T, int64_t V, float scale,
-                        uint32_t flags, float* logp, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+                        uint32_t flags, float* logp, float* lse, void* stream);
 
 /*
  * elas_token_logp_bwd -- gradient of the logits from those of logp and lse:
@@ -72,7 +69,10 @@ int elas_token_logp_bwd(const float* dlogp, const float* dlse, const void* logit
  *
  * weight NULL: 1; a token of weight 0 takes no part.  logp, lse, dlogits may be
  * NULL: not wanted.  stats: device float32 [2].
+ * workspace (of this call and the next): 16-byte aligned, at least
+ * elas_token_loss_workspace_bytes(T, V, flags) bytes, which is 0 for sizes that no call takes.
  */
+size_t elas_token_loss_workspace_bytes(int64_t T, int64_t V, uint32_t flags);
 int elas_token_loss(const void* logits, int64_t ld, const void* ids, const float* weight, int64_t T, int64_t V,
                     float scale, float reduce, float z_coef, uint32_t flags, float* logp, float* lse, void* dlogits,
                     int64_t ld_out, float* stats, void* workspace, size_t workspace_bytes, void* stream);
@@ -114,9 +114,10 @@ int elas_policy_loss(const void* logits, int64_t ld, const void* ids, const floa
  * first sequence and behind the last one.  A sequence may be empty (its sum is 0).
  * stats: device float32 [3], zeros where there are no pairs.  Sums are 64-bit, in a fixed order.
  * Requires 0 <= pairs < 2^30, 0 <= N < 2^40, 0 <= smoothing <= 1, finite beta.
- * workspace >= elas_preference_loss_workspace_bytes(pairs) bytes.
+ * workspace >= elas_preference_loss_workspace_bytes(N, pairs) bytes (0 for few short answers, and for
+ * sizes that no call takes).
  */
-size_t elas_preference_loss_workspace_bytes(int64_t pairs);
+size_t elas_preference_loss_workspace_bytes(int64_t N, int64_t pairs);
 int elas_preference_loss(const float* logp, const float* ref_logp, const void* offsets, int64_t N, int64_t pairs, float beta,
                          float smoothing, uint32_t flags, float* margin, float* dlogp, float* stats, void* workspace,
                          size_t workspace_bytes, void* stream);

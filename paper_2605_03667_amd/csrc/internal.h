@@ -162,7 +162,7 @@ struct PreferenceArgs {
 };
 
 // preference.hip
-size_t preference_workspace_bytes(int64_t pairs);
+size_t preference_workspace_bytes(int64_t N, int64_t pairs);
 hipError_t run_preference(const PreferenceArgs& a, hipStream_t stream);
 
 // Arguments of a step of AdamW (include/elas_adamw.h); host arrays of n.

@@ -16,6 +16,7 @@ namespace {
 
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1;
 constexpr int64_t kMaxVocab = int64_t(1) << 30;
+constexpr int64_t kMaxValues = int64_t(1) << 40;
 constexpr int64_t kMaxPitch = int64_t(1) << 31;
 
 // What the calls on logits share; nothing is inspected behind the sizes where there are no tokens.
@@ -53,7 +54,7 @@ size_t elas_token_loss_workspace_bytes(int64_t T, int64_t V, uint32_t flags) {
 }
 
 int elas_token_logp_fwd(const void* logits, int64_t ld, const void* ids, int64_t T, int64_t V, float scale, uint32_t flags, float* logp,
-                        float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+                        float* lse, void* stream) {
   begin_call();
   LogitsArgs a{};
   a.kind = LogitsArgs::LOGP;
@@ -61,8 +62,7 @@ int elas_token_logp_fwd(const void* logits, int64_t ld, const void* ids, int64_t
   if (T == 0) return ELAS_OK;
   ELAS_CHECK(check_elem_ptr(logp, 4, "logp"));
   ELAS_CHECK(check_optional_ptr(lse, 4, "lse"));
-  ELAS_CHECK(check_workspace(workspace, workspace_bytes, workspace_of(a)));
-  a.logp = logp; a.lse = lse; a.ws = workspace;
+  a.logp = logp; a.lse = lse;
   return device_status(elas::run_token_loss(a, (hipStream_t)stream), "log-probability launch");
 }
 
@@ -127,8 +127,8 @@ int elas_policy_loss(const void* logits, int64_t ld, const void* ids, const floa
   return device_status(elas::run_token_loss(a, (hipStream_t)stream), "policy loss launch");
 }
 
-size_t elas_preference_loss_workspace_bytes(int64_t pairs) {
-  return pairs < 0 || pairs >= kMaxVocab ? 0 : elas::preference_workspace_bytes(pairs);
+size_t elas_preference_loss_workspace_bytes(int64_t N, int64_t pairs) {
+  return pairs < 0 || pairs >= kMaxVocab || N < 0 || N >= kMaxValues ? 0 : elas::preference_workspace_bytes(N, pairs);
 }
 
 int elas_preference_loss(const float* logp, const float* ref_logp, const void* offsets, int64_t N, int64_t pairs, float beta, float smoothing,
@@ -136,7 +136,7 @@ int elas_preference_loss(const float* logp, const float* ref_logp, const void* o
   begin_call();
   if (flags & ~ELAS_IDS_I64) return fail(ELAS_ERR_FLAGS, "flags: only ELAS_IDS_I64 is allowed");
   if (pairs < 0 || pairs >= kMaxVocab) return fail(ELAS_ERR_SHAPE, "pairs=%lld out of range", (long long)pairs);
-  if (N < 0 || N >= int64_t(1) << 40) return fail(ELAS_ERR_SHAPE, "N=%lld out of range", (long long)N);
+  if (N < 0 || N >= kMaxValues) return fail(ELAS_ERR_SHAPE, "N=%lld out of range", (long long)N);
   ELAS_CHECK(check_scale(beta, "beta"));
   if (!(smoothing >= 0.f && smoothing <= 1.f)) return fail(ELAS_ERR_SHAPE, "smoothing must be between 0 and 1");
   elas::PreferenceArgs a{};
@@ -151,7 +151,7 @@ int elas_preference_loss(const float* logp, const float* ref_logp, const void* o
   }
   if (N > 0) ELAS_CHECK(check_optional_ptr(dlogp, 4, "dlogp"));
   ELAS_CHECK(check_elem_ptr(stats, 4, "stats"));
-  ELAS_CHECK(check_workspace(workspace, workspace_bytes, elas::preference_workspace_bytes(pairs)));
+  ELAS_CHECK(check_workspace(workspace, workspace_bytes, elas::preference_workspace_bytes(N, pairs)));
   a.N = N; a.pairs = pairs; a.logp = logp; a.ref = ref_logp; a.offsets = offsets; a.beta = beta; a.smoothing = smoothing;
   a.margin = margin; a.dlogp = N > 0 ? dlogp : nullptr; a.stats = stats; a.ws = workspace;
   return device_status(elas::run_preference(a, (hipStream_t)stream), "preference loss launch");

@@ -166,23 +166,22 @@ __global__ __launch_bounds__(WAVES * TEAMS * 64) void preference_kernel(const Pr
 }
 
 __global__ __launch_bounds__(1024) void preference_sum_kernel(const double* part, int groups, double pairs, float* stats) {
-  __shared__ double red[16];
+  __shared__ double red[16][kSums];
   double s[kSums] = {0.0, 0.0, 0.0};
   for (int g = threadIdx.x; g < groups; g += 1024) {
 #pragma unroll
     for (int k = 0; k < kSums; ++k) s[k] += part[(int64_t)g * kSums + k];
   }
-#pragma unroll
-  for (int k = 0; k < kSums; ++k) {
-    const double v = block_sum<16>(s[k], red);
-    if (threadIdx.x == 0) stats[k] = pairs > 0.0 ? (float)(v / pairs) : 0.f;
-  }
+  const double v = block_sums<16>(s, red);
+  if (threadIdx.x < kSums) stats[threadIdx.x] = pairs > 0.0 ? (float)(v / pairs) : 0.f;
 }
+
+bool few(int64_t N, int64_t pairs) { return pairs <= kFewPairs && N <= kFewValues; }
 
 }  // namespace
 
-size_t preference_workspace_bytes(int64_t pairs) {
-  return (size_t)std::max<int64_t>(1, std::min<int64_t>(pairs, kGroups)) * kSums * sizeof(double);
+size_t preference_workspace_bytes(int64_t N, int64_t pairs) {
+  return few(N, pairs) ? 0 : (size_t)std::max<int64_t>(1, std::min<int64_t>(pairs, kGroups)) * kSums * sizeof(double);
 }
 
 hipError_t run_preference(const PreferenceArgs& a, hipStream_t stream) {
@@ -194,7 +193,7 @@ hipError_t run_preference(const PreferenceArgs& a, hipStream_t stream) {
     return hipGetLastError();
   };
   // few short pairs: one workgroup, and no second launch
-  if (a.pairs <= kFewPairs && a.N <= kFewValues)
+  if (few(a.N, a.pairs))
     return launch(preference_kernel<1, 16, true, true>, preference_kernel<1, 16, true, false>, 1024, kFewPairs, 16);
   const int64_t length = a.pairs ? a.N / a.pairs : 0;       // both answers
   const hipError_t e =

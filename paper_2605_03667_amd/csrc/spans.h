@@ -111,6 +111,22 @@ __device__ __forceinline__ float wave_max(float v) {
   const auto s32 = __builtin_amdgcn_permlane32_swap(x, x, false, false);
   return fmaxf(as_float(s32[0]), as_float(s32[1]));
 }
+// K sums over a workgroup of WAVES waves at once, with one barrier; thread k gets the k-th.  `lds` holds WAVES rows.
+template <int WAVES, int K>
+__device__ __forceinline__ double block_sums(const double (&s)[K], double (*lds)[K]) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const double v = wave_sum(s[k]);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][k] = v;
+  }
+  __syncthreads();
+  double v = 0.0;
+  if (threadIdx.x < K)
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v += lds[w][threadIdx.x];
+  return v;
+}
+
 // Of bit patterns: for magnitudes in the order of their values, NaN above them all.
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   const auto step = [&](uint32_t o) { v = v > o ? v : o; };

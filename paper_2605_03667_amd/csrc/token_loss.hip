@@ -425,7 +425,7 @@ template <int KIND, class E>
 __global__ __launch_bounds__(256) void join_kernel(const Rows a, const Split sp) {
   using S = Span<E>;
   constexpr int N = S::N;
-  __shared__ double red[4];
+  __shared__ double red[4][kSums];
   const int tid = threadIdx.x, lane = tid & 63, part = blockIdx.x;
   const float c = a.scale * kLog2E;
   if (blockIdx.y == gridDim.y - 1) {
@@ -446,11 +446,8 @@ __global__ __launch_bounds__(256) void join_kernel(const Rows a, const Split sp)
       }
       write_row(a, t, logp, lse);
     }
-#pragma unroll
-    for (int k = 0; k < (KIND == LogitsArgs::LOGP ? 0 : KIND == LogitsArgs::TOKEN ? 2 : 3); ++k) {
-      const double v = block_sum<4>(sum[k], red);
-      if (tid == 0) sp.stats[k] = (float)v;
-    }
+    const double v = block_sums<4>(sum, red);
+    if (tid < (KIND == LogitsArgs::TOKEN ? 2 : 3)) sp.stats[tid] = (float)v;
     return;
   }
   const int64_t t = blockIdx.y;
@@ -501,17 +498,14 @@ __global__ __launch_bounds__(256) void join_kernel(const Rows a, const Split sp)
 }
 
 __global__ __launch_bounds__(1024) void loss_sum_kernel(const double* part, int groups, int count, float* stats) {
-  __shared__ double red[16];
+  __shared__ double red[16][kSums];
   double s[kSums] = {0.0, 0.0, 0.0};
   for (int g = threadIdx.x; g < groups; g += 1024) {
 #pragma unroll
     for (int k = 0; k < kSums; ++k) s[k] += part[(int64_t)g * kSums + k];
   }
-#pragma unroll
-  for (int k = 0; k < kSums; ++k) {
-    const double v = block_sum<16>(s[k], red);
-    if (threadIdx.x == 0 && k < count) stats[k] = (float)v;
-  }
+  const double v = block_sums<16>(s, red);
+  if ((int)threadIdx.x < count) stats[threadIdx.x] = (float)v;
 }
 
 // Gradient from those of logp and lse: every value by itself, kChunk pieces of a row to a thread at a time.  (A

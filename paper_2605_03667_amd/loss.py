@@ -25,11 +25,11 @@ ELAS_LOGITS_F32 = 1
 
 _SIGNATURES.update({
     "elas_token_loss_workspace_bytes": ([_i64, _i64, _u32], _sz),
-    "elas_token_logp_fwd": ([_p, _i64, _p, _i64, _i64, _f32, _u32, _p, _p, _p, _sz, _p], ctypes.c_int),
+    "elas_token_logp_fwd": ([_p, _i64, _p, _i64, _i64, _f32, _u32, _p, _p, _p], ctypes.c_int),
     "elas_token_logp_bwd": ([_p, _p, _p, _i64, _p, _p, _i64, _i64, _f32, _u32, _p, _i64, _p], ctypes.c_int),
     "elas_token_loss": ([_p, _i64, _p, _p, _i64, _i64, _f32, _f32, _f32, _u32, _p, _p, _p, _i64, _p, _p, _sz, _p], ctypes.c_int),
     "elas_policy_loss": ([_p, _i64, _p, _p, _p, _p, _p, _i64, _i64] + [_f32] * 5 + [_u32, _p, _p, _i64, _p, _p, _sz, _p], ctypes.c_int),
-    "elas_preference_loss_workspace_bytes": ([_i64], _sz),
+    "elas_preference_loss_workspace_bytes": ([_i64, _i64], _sz),
     "elas_preference_loss": ([_p, _p, _p, _i64, _i64, _f32, _f32, _u32, _p, _p, _p, _p, _sz, _p], ctypes.c_int),
 })
 
@@ -101,18 +101,28 @@ def _gradient(dlogits, logits, dev):
     return p, pitch
 
 
+def _space(workspace, need: int, device: torch.device):
+    """The caller's workspace or a new one, its address and size."""
+    if workspace is None:
+        if need == 0:
+            return None, None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        return workspace, workspace.data_ptr(), need
+    return _scratch(workspace, need, device)
+
+
 def _rows(T, device):
     return torch.empty(T, dtype=_F32, device=device)
 
 
 @functools.lru_cache(maxsize=1024)   # (of the sizes alone)
 def elas_token_loss_workspace_bytes(T: int, V: int, flags: int = 0) -> int:
-    """Workspace of elas_token_logp_fwd, elas_token_loss and elas_policy_loss on logits [T, V]
-    (``flags``: ELAS_LOGITS_F32 for float32 logits)."""
+    """Workspace of elas_token_loss and elas_policy_loss on logits [T, V] (``flags``:
+    ELAS_LOGITS_F32 for float32 logits)."""
     return lib().elas_token_loss_workspace_bytes(T, V, flags)
 
 
-def elas_token_logp_fwd(logits, ids, scale: float = 1.0, out: dict | None = None, workspace: torch.Tensor | None = None) -> dict:
+def elas_token_logp_fwd(logits, ids, scale: float = 1.0, out: dict | None = None) -> dict:
     """Log-probabilities of tokens: with z = scale * logits, lse = log sum exp z over
     the vocabulary and logp = z[id] - lse.  logits is [T, V], bf16 or float32, its rows
     contiguous (any pitch and alignment); ids [T] int32 or int64.  A token whose id is
@@ -123,8 +133,7 @@ def elas_token_logp_fwd(logits, ids, scale: float = 1.0, out: dict | None = None
         out = {"logp": _rows(T, logits.device), "lse": _rows(T, logits.device)}
     logp_p = _arg(_required(out.get("logp"), "out['logp']"), (T,), _F32, dev, "out['logp']")
     lse_p = _opt(out.get("lse"), (T,), _F32, dev, "out['lse']")
-    workspace, ws_p, ws_n = _scratch(workspace, elas_token_loss_workspace_bytes(T, V, flags & ELAS_LOGITS_F32), logits.device)
-    _on(dev, lib().elas_token_logp_fwd, x, ld, ids_p, T, V, scale, flags, logp_p, lse_p, ws_p, ws_n)
+    _on(dev, lib().elas_token_logp_fwd, x, ld, ids_p, T, V, scale, flags, logp_p, lse_p)
     return out
 
 
@@ -158,7 +167,7 @@ def elas_token_loss(logits, ids, weight: torch.Tensor | None = None, scale: floa
                "dlogits": torch.empty((T, V), dtype=logits.dtype, device=logits.device)}
     stats_p = _arg(_required(out.get("stats"), "out['stats']"), (2,), _F32, dev, "out['stats']")
     d_p, ld_out = _gradient(out.get("dlogits"), logits, dev)
-    workspace, ws_p, ws_n = _scratch(workspace, elas_token_loss_workspace_bytes(T, V, flags & ELAS_LOGITS_F32), logits.device)
+    workspace, ws_p, ws_n = _space(workspace, elas_token_loss_workspace_bytes(T, V, flags & ELAS_LOGITS_F32), logits.device)
     _on(dev, lib().elas_token_loss, x, ld, ids_p, _opt(weight, (T,), _F32, dev, "weight"), T, V, scale, reduce, z_coef, flags,
         _opt(out.get("logp"), (T,), _F32, dev, "out['logp']"), _opt(out.get("lse"), (T,), _F32, dev, "out['lse']"), d_p, ld_out, stats_p,
         ws_p, ws_n)
@@ -186,7 +195,7 @@ def elas_policy_loss(logits, ids, advantage, old_logp: torch.Tensor | None = Non
     stats_p = _arg(_required(out.get("stats"), "out['stats']"), (3,), _F32, dev, "out['stats']")
     d_p, ld_out = _gradient(out.get("dlogits"), logits, dev)
     row = (T,)
-    workspace, ws_p, ws_n = _scratch(workspace, elas_token_loss_workspace_bytes(T, V, flags & ELAS_LOGITS_F32), logits.device)
+    workspace, ws_p, ws_n = _space(workspace, elas_token_loss_workspace_bytes(T, V, flags & ELAS_LOGITS_F32), logits.device)
     _on(dev, lib().elas_policy_loss, x, ld, ids_p, _arg(advantage, row, _F32, dev, "advantage"), _opt(old_logp, row, _F32, dev, "old_logp"),
         _opt(ref_logp, row, _F32, dev, "ref_logp"), _opt(weight, row, _F32, dev, "weight"), T, V, scale, reduce, clip_low, clip_high, kl_coef,
         flags, _opt(out.get("logp"), row, _F32, dev, "out['logp']"), d_p, ld_out, stats_p, ws_p, ws_n)
@@ -194,8 +203,8 @@ def elas_policy_loss(logits, ids, advantage, old_logp: torch.Tensor | None = Non
 
 
 @functools.lru_cache(maxsize=1024)   # (of the sizes alone)
-def elas_preference_loss_workspace_bytes(pairs: int) -> int:
-    return lib().elas_preference_loss_workspace_bytes(pairs)
+def elas_preference_loss_workspace_bytes(N: int, pairs: int) -> int:
+    return lib().elas_preference_loss_workspace_bytes(N, pairs)
 
 
 def elas_preference_loss(logp, offsets, ref_logp: torch.Tensor | None = None, beta: float = 0.1, smoothing: float = 0.0,
@@ -222,8 +231,12 @@ def elas_preference_loss(logp, offsets, ref_logp: torch.Tensor | None = None, be
     if out is None:
         out = {"stats": _rows(3, logp.device), "margin": _rows(pairs, logp.device), "dlogp": torch.empty_like(logp)}
     stats_p = _arg(_required(out.get("stats"), "out['stats']"), (3,), _F32, dev, "out['stats']")
-    workspace, ws_p, ws_n = _scratch(workspace, elas_preference_loss_workspace_bytes(pairs), logp.device)
+    dlogp_p = _opt(out.get("dlogp"), (N,), _F32, dev, "out['dlogp']")
+    for t, name in ((logp_p, "logp"), (None if ref_logp is None else ref_logp.data_ptr(), "ref_logp")):
+        if dlogp_p and t and abs(dlogp_p - t) < 4 * N and not (dlogp_p == t and name == "logp"):
+            raise ValueError(f"dlogp must be logp itself or overlap nothing of {name}")
+    workspace, ws_p, ws_n = _space(workspace, elas_preference_loss_workspace_bytes(N, pairs), logp.device)
     _on(dev, lib().elas_preference_loss, logp_p, _opt(ref_logp, (N,), _F32, dev, "ref_logp"), offsets_p, N, pairs, beta, smoothing, flags,
-        _opt(out.get("margin"), (pairs,), _F32, dev, "out['margin']"), _opt(out.get("dlogp"), (N,), _F32, dev, "out['dlogp']"), stats_p,
+        _opt(out.get("margin"), (pairs,), _F32, dev, "out['margin']"), dlogp_p, stats_p,
         ws_p, ws_n)
     return out

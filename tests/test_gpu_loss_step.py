@@ -38,7 +38,7 @@ class _Head:
                     "pairs": {"stats": torch.empty(3, device=DEV), "margin": torch.empty(3, device=DEV), "dlogp": torch.empty(T, device=DEV)}}
         self.norm = torch.empty(1, device=DEV)
         self.ws = {"loss": torch.empty(elas.elas_token_loss_workspace_bytes(T, V, elas.ELAS_LOGITS_F32), dtype=torch.uint8, device=DEV),
-                   "pairs": torch.empty(elas.elas_preference_loss_workspace_bytes(3), dtype=torch.uint8, device=DEV),
+                   "pairs": torch.empty(elas.elas_preference_loss_workspace_bytes(T, 3), dtype=torch.uint8, device=DEV),
                    "grad": torch.empty(elas.elas_grad_workspace_bytes(2), dtype=torch.uint8, device=DEV)}
 
     def forward(self):
@@ -62,7 +62,7 @@ class _Head:
                               out={**self.out["policy"], "dlogits": self.logits}, workspace=self.ws["loss"])
 
     def pairs(self):
-        elas.elas_token_logp_fwd(self.logits, self.ids, out=self.out["logp"], workspace=self.ws["loss"])
+        elas.elas_token_logp_fwd(self.logits, self.ids, out=self.out["logp"])
         elas.elas_preference_loss(self.out["logp"]["logp"], self.offsets, ref_logp=self.ref, beta=0.3, smoothing=0.1, out=self.out["pairs"],
                                   workspace=self.ws["pairs"])
         elas.elas_token_logp_bwd(self.out["pairs"]["dlogp"], self.logits, self.ids, self.out["logp"]["lse"], dlogits=self.logits)

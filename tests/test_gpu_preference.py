@@ -110,7 +110,7 @@ def test_gradient_against_differences():
 
 
 def test_refusals_on_the_gpu():
-    x, off = torch.zeros(10, device=DEV), torch.tensor([0, 5, 10], device=DEV)
+    x, y, off = torch.zeros(10, device=DEV), torch.zeros(10, device=DEV), torch.tensor([0, 5, 10], device=DEV)
 
     def raises(match, *a, **k):
         with pytest.raises(ValueError, match=match):
@@ -121,6 +121,8 @@ def test_refusals_on_the_gpu():
     raises("offsets must be a GPU", x, off.cpu())
     raises("margin", x, off, out={"stats": x[:3], "margin": x[:2]})
     raises("stats", x, off, out={"margin": x[:1]})
+    raises("overlap", x[:8], off.clamp_max(8), out={"stats": x[:3].clone(), "dlogp": x[1:9]})
+    raises("overlap", x, off, y, out={"stats": x[:3].clone(), "dlogp": y})
     raises("contiguous", torch.zeros((10, 2), device=DEV)[:, 0], off)
     with pytest.raises(elas.ElasError, match="smoothing"):
         elas.elas_preference_loss(x, off, smoothing=1.5)

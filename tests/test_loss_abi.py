@@ -45,7 +45,7 @@ LOGITS = dict(x=A, ld=16, ids=A, T=4, V=10, scale=1.0, flags=0)
 
 
 def _fwd(**kw):
-    return _status("elas_token_logp_fwd", {**LOGITS, "logp": A, "lse": A, **WS}, **kw)
+    return _status("elas_token_logp_fwd", {**LOGITS, "logp": A, "lse": A}, **kw)
 
 
 def _bwd(**kw):
@@ -85,7 +85,7 @@ def test_refusals_of_gradients(call):
     assert call(d=A + 2, flags=elas.ELAS_LOGITS_F32) == ALIGN
 
 
-@pytest.mark.parametrize("call", [_fwd, _loss, _policy])
+@pytest.mark.parametrize("call", [_loss, _policy])
 def test_refusals_of_workspaces(call):
     assert call(wsb=elas.elas_token_loss_workspace_bytes(4, 10) - 1) == WORKSPACE
     assert call(ws=None) == NULL and call(ws=A + 8) == ALIGN
@@ -107,13 +107,13 @@ def test_other_refusals_on_logits():
         assert _policy(high=bad) == SHAPE
     # without tokens nothing is inspected or launched where there are no statistics
     empty = dict(T=0, x=None, ids=None)
-    assert _fwd(**empty, logp=None, lse=None, ws=None, wsb=0) == 0
+    assert _fwd(**empty, logp=None, lse=None) == 0
     assert _bwd(**empty, dlogp=None, dlse=None, lse=None, d=None, ldo=0) == 0
 
 
 def test_preference_refusals():
     def call(**kw):
-        return _status("elas_preference_loss", dict(logp=A, ref=A, off=A, N=50, pairs=3, beta=0.1, smoothing=0.0, flags=0, margin=A, d=A, stats=A, **WS), **kw)
+        return _status("elas_preference_loss", dict(logp=A, ref=A, off=A, N=5000, pairs=300, beta=0.1, smoothing=0.0, flags=0, margin=A, d=A, stats=A, **WS), **kw)
 
     assert call(flags=1) == FLAGS
     for bad in (-1, 1 << 30):
@@ -125,7 +125,7 @@ def test_preference_refusals():
         assert call(smoothing=bad) == SHAPE
     assert call(off=None) == NULL and call(off=A + 2) == ALIGN and call(off=A + 4, flags=elas.ELAS_IDS_I64) == ALIGN
     assert call(logp=None) == NULL and call(ref=A + 1) == ALIGN and call(margin=A + 2) == ALIGN and call(d=A + 2) == ALIGN
-    assert call(stats=None) == NULL and call(wsb=elas.elas_preference_loss_workspace_bytes(3) - 1) == WORKSPACE and call(ws=None) == NULL
+    assert call(stats=None) == NULL and call(wsb=elas.elas_preference_loss_workspace_bytes(5000, 300) - 1) == WORKSPACE and call(ws=None) == NULL
 
 
 def test_adamw_refusals():
@@ -172,11 +172,12 @@ def test_workspace_of_sizes_out_of_range():
     big = 2 ** 63 - 1
     for T, V in ((big, 10), (1 << 31, 10), (-1, 10), (4, 0), (4, big), (4, (1 << 30) + 1)):
         assert elas.elas_token_loss_workspace_bytes(T, V) == 0
-    for pairs in (-1, 1 << 30, big):
-        assert elas.elas_preference_loss_workspace_bytes(pairs) == 0
+    for N, pairs in ((100, -1), (100, 1 << 30), (100, big), (-1, 100), (1 << 40, 100)):
+        assert elas.elas_preference_loss_workspace_bytes(N, pairs) == 0
+    assert elas.elas_preference_loss_workspace_bytes(1000, 8) == 0 and elas.elas_preference_loss_workspace_bytes(1 << 20, 8) > 0
     # the largest that are taken: sums of workgroups, which do not grow with the tokens
     assert 0 < elas.elas_token_loss_workspace_bytes((1 << 31) - 1, 1 << 30) < 1 << 24
-    assert 0 < elas.elas_preference_loss_workspace_bytes((1 << 30) - 1) < 1 << 24
+    assert 0 < elas.elas_preference_loss_workspace_bytes((1 << 40) - 1, (1 << 30) - 1) < 1 << 24
 
 
 def test_binding_refusals():
