@@ -1,9 +1,10 @@
 // The loss of paired answers by their log-ratios, with its gradient (the formulas are in
 // include/elas_loss.h).
 //
-// A workgroup takes a pair at a time: the sums of both answers in 64 bits, z and the loss, then the
-// gradient, one value for each answer.  The pairs' losses are added up in a fixed order by a
-// second launch.
+// A pair's answers are summed in 64 bits by a team of 1, 2, 4 or 16 waves, then come its margin and loss, then the
+// gradient, one value for each answer.  The pairs' losses are added up in a fixed order by a second launch.  2048
+// pairs of 1000 tokens an answer: 10 us of kernel (49 MB) and 4 for the sum; 8 pairs of 100: 4.3 us, one launch; bound by
+// latency below about a thousand pairs.
 #include <math.h>
 
 #include <algorithm>
@@ -18,8 +19,12 @@ namespace {
 
 constexpr int kGroups = 2048;
 constexpr int kSums = 3;
+// Up to so many pairs and values one workgroup does everything, a pair to a wave (in a graph, 20 pairs of 20 tokens: 5.4 us,
+// 7.0 in two launches; 64 pairs of 100: 9.8 and 7.3).
 constexpr int64_t kFewPairs = 32, kFewValues = 1 << 14;
-constexpr int64_t kWavePair = 512;      // values of a pair up to which a wave takes it
+// Values of a pair up to which a wave takes it, 2 waves, 4 waves (300 pairs of 600 values: 7.4 us either way; 2048 of 2000: 15.6 by
+// one wave, 14.7 by 2, 16.8 by 4; 20000 of 100: 16 by one, 42 by 2; one pair of 40000: 9.8 by 16, 13.8 by 4).
+constexpr int64_t kWavePair = 512, kTwoWavePair = 4096, kFourWavePair = 16384;
 
 __device__ __forceinline__ int64_t offset_of(const PreferenceArgs& a, int64_t s) {
   const int64_t o = a.i64 ? ((const int64_t*)a.offsets)[s] : (int64_t)((const int32_t*)a.offsets)[s];
@@ -201,9 +206,9 @@ hipError_t run_preference(const PreferenceArgs& a, hipStream_t stream) {
           // a pair to a wave, up to 16 a workgroup where that leaves enough workgroups
           ? launch(preference_kernel<1, 4, false, true>, preference_kernel<1, 4, false, false>, 256,
                    4 * std::max<int64_t>(1, std::min<int64_t>(a.pairs / 4096, 4)), 4)
-      : length <= 4096
+      : length <= kTwoWavePair
           ? launch(preference_kernel<2, 1, false, true>, preference_kernel<2, 1, false, false>, 128, 1, 1)
-      : length <= 16384 || a.pairs > 512
+      : length <= kFourWavePair || a.pairs > 512
           ? launch(preference_kernel<4, 1, false, true>, preference_kernel<4, 1, false, false>, 256, 1, 1)
           : launch(preference_kernel<16, 1, false, true>, preference_kernel<16, 1, false, false>, 1024, 1, 1);
   if (e != hipSuccess) return e;

@@ -1,11 +1,13 @@
 // Log-probabilities of tokens from logits and the losses on them, with their gradients
 // (the formulas are in include/elas_loss.h).
 //
-// A workgroup takes a row at a time: one pass for the running maximum and the sum of
-// exp2((x - max) scale log2(e)), then the token's own terms, then, where a gradient is wanted, a second
-// pass that writes it.  The maximum is of the logits themselves, so that a row of nothing
-// but a type's lowest value is a uniform distribution at any scale.  Statistics are 64-bit
-// sums per workgroup over its rows, added up by a second launch.
+// Bound by HBM: 2 to 6 instructions a value and an exponential or two against one read and one write of it.  So a row
+// is read once: a team of 1 to 16 waves holds it in registers, finds its maximum and the sum of
+// exp2((x - max) scale log2(e)), then the token's own terms, and writes the gradient.  The maximum is of the
+// logits themselves, so that a row of nothing but a type's lowest value is a uniform distribution at
+// any scale.  Statistics are 64-bit sums per workgroup over its rows, added up by a second launch.  65536 x 32000
+// bf16 with gradient: 1514 us, 5.5 TB/s (read twice: 2153); 16381 x 32000 bf16, an eighth padding and
+// a sixth of weight 0: 331; 2000 x 32000 float32: 86; 4093 x 32003 float32 without one: 70.
 #include <math.h>
 
 #include <algorithm>
@@ -18,7 +20,9 @@ namespace elas {
 
 namespace {
 
-constexpr int kGroups = 8192;            // most workgroups that take rows
+// Most workgroups that take rows.  More than the card holds at once, so that those with masked rows do not
+// leave it idle at the end (16381 x 32000, a quarter masked: 373 us with 1024, 366 with 2048, 352 with 4096, 333 with 8192).
+constexpr int kGroups = 8192;
 constexpr int kSums = 3;                 // statistics of a workgroup
 constexpr float kLowest = -0x1.fffffep127f;
 constexpr float kLog2E = 0x1.715476p0f;
@@ -123,7 +127,8 @@ __device__ __forceinline__ Terms row_terms(const Rows& a, int64_t t, float w, fl
 
 // How a row is cut: pieces of 16 bytes from `lead` on, the first that is aligned in the matrix
 // that is written (or, without one, read), `full` of them; and the values in front of and behind them,
-// one to a thread.
+// one to a thread.  (8000 rows of 50257 bf16 logits, half of them not even 4-byte aligned: 358 us, 402 with pieces
+// from the row's first value on; without a gradient 140 and 170.)
 template <class E>
 struct Cut {
   static constexpr int N = Span<E>::N;
@@ -249,9 +254,9 @@ template <int KIND, class E, int WAVES>
 __global__ __launch_bounds__(Team<WAVES>::THREADS * Team<WAVES>::ROWS) void rows_kernel(const Rows a) {
   constexpr int TH = Team<WAVES>::THREADS, ROWS = Team<WAVES>::ROWS;
   __shared__ float red[2][2 * WAVES + 1];
+  __shared__ double sums[ROWS][kSums];
   const int tid = threadIdx.x % TH;
   const float c = a.scale * kLog2E;
-  __shared__ double sums[ROWS][kSums];
   Sums<WAVES> sum(sums);
   int turn = 0;
   for (int64_t t = (int64_t)blockIdx.x * ROWS + wave_row<WAVES>(); t < a.T; t += (int64_t)gridDim.x * ROWS) {
@@ -279,16 +284,18 @@ __global__ __launch_bounds__(Team<WAVES>::THREADS * Team<WAVES>::ROWS) void rows
 }
 
 // A loss with its gradient, the row in the registers of its team: PARTS pieces to a thread, what lies
-// behind the row -inf.  BEYOND: a longer row, whose pieces behind those are read twice.
+// behind the row -inf.  BEYOND: a longer row, whose pieces behind those are read twice (4000 x 131072 float32:
+// 853 us, 1300 with all of it read twice).  Loads and stores are non-temporal (65536 x 32000 bf16: 1488 us, with plain
+// loads 1548; before them, plain stores too, 1597 for 1537).
 template <int KIND, class E, int WAVES, int PARTS, bool BEYOND>
 __global__ __launch_bounds__(Team<WAVES>::THREADS * Team<WAVES>::ROWS) void held_kernel(const Rows a) {
   using S = Span<E>;
   constexpr int N = S::N, TH = Team<WAVES>::THREADS, ROWS = Team<WAVES>::ROWS;
   constexpr bool KEEP = N == 4;      // float32: the exponentials take the logits' place
   __shared__ float red[2][2 * WAVES + 1];
+  __shared__ double sums[ROWS][kSums];
   const int tid = threadIdx.x % TH;
   const float c = a.scale * kLog2E;
-  __shared__ double sums[ROWS][kSums];
   Sums<WAVES> sum(sums);
   int turn = 0;
   for (int64_t t = (int64_t)blockIdx.x * ROWS + wave_row<WAVES>(); t < a.T; t += (int64_t)gridDim.x * ROWS) {
@@ -385,6 +392,8 @@ __global__ __launch_bounds__(Team<WAVES>::THREADS * Team<WAVES>::ROWS) void held
 // Few rows: each is split over workgroups, in two launches.  The first leaves every part's maximum and sum, and the
 // label's logit (a gradient may take the logits' place); the second joins them, every workgroup for itself, and
 // writes its part of the gradient, and one more workgroup, a row to a thread, the rows' results and the statistics.
+// 16 rows in a graph: 32000 bf16 6.5 us (9.2 by the kernels above and their sum), 65000 bf16 8.0 (13.0),
+// 131072 float32 9.2 (19.5).
 struct Split {
   float2* part;       // [T][parts]: maximum, sum
   float* label;       // [T]
@@ -508,9 +517,9 @@ __global__ __launch_bounds__(1024) void loss_sum_kernel(const double* part, int 
   if ((int)threadIdx.x < count) stats[threadIdx.x] = (float)v;
 }
 
-// Gradient from those of logp and lse: every value by itself, kChunk pieces of a row to a thread at a time.  (A
-// lse beyond kLargeLse leaves exp(z - lse) an error of 2^-24 of that, and among logits of a type's lowest value it holds
-// nothing of the sum at all.)
+// Gradient from those of logp and lse: every value by itself, kChunk pieces of a row to a thread at a time (8192 x 32000
+// bf16: 168 us with 2, 174 with 4, 176 with 8 or 16).  Bound by HBM: 6.2 TB/s.  (A lse beyond kLargeLse leaves
+// exp(z - lse) an error of 2^-24 of that, and among logits of a type's lowest value it holds nothing of the sum at all.)
 constexpr float kLargeLse = 4096.f;
 constexpr int kChunk = 2;
 
@@ -606,7 +615,9 @@ __global__ __launch_bounds__(TH) void logp_bwd_kernel(const BwdRows a) {
 
 int groups_of(int64_t T) { return (int)std::min<int64_t>(T, kGroups); }
 
-// Whether rows are split, and how: few rows of 16 KB and more, whose logits stay in the caches between the launches.
+// Whether rows are split, and how: few rows of 16 KB and more, up to 8 MB (64 x 32000 bf16, 4 MB: 7.9 us, not split 9.5;
+// 256 x 32000, 16 MB: 13.9 and 10.6), into at most 16 parts, which one thread joins for the statistics (16 x 131072
+// float32: 9.2 us with 16, 11.5 with 8, 10.3 with 32).
 constexpr int64_t kSplitRows = 256, kSplitRow = 16384, kSplitBytes = 8 << 20;
 constexpr int kParts = 16;
 struct SplitPlan {
@@ -659,20 +670,23 @@ unsigned launch_rows(const Rows& r, hipStream_t stream) {
   return grid.x;
 }
 
-// The smallest team that holds a row; returns the workgroups.
+// The team that holds a row with the fewest idle lanes, of as few waves as leave a SIMD 4 or more of them.  In us, with the
+// next team beside it: 100000 x 2900 bf16 224 (4 waves of 2 pieces: 320), 60000 x 6000 262 (4 of 3: 280), 60000 x 8000 343
+// (8 of 2: 386), 60000 x 12000 538 (4 of 6: 570), 30000 x 16000 333 (4 of 8: 342), 65536 x 32000 1488 (4 of 16: 1591,
+// 16 of 4: 1689), 10000 x 48000 342 (16 of 6: 387), 16000 x 32000 float32 680 (8 of 16: 695).  Returns the workgroups.
 template <int KIND, class E>
 unsigned launch_gradient(const Rows& r, hipStream_t stream) {
   const int pieces = (r.V + Span<E>::N - 1) / Span<E>::N, whole = (pieces + 63) / 64;      // pieces to a lane of one wave
   if (whole <= 2) return launch_held<KIND, E, 1, 2>(r, stream);
   if (whole <= 4) return launch_held<KIND, E, 1, 4>(r, stream);
-  if (whole <= 8) return launch_held<KIND, E, 4, 2>(r, stream);
-  if (whole <= 12) return launch_held<KIND, E, 4, 3>(r, stream);
+  if (whole <= 8) return launch_held<KIND, E, 1, 8>(r, stream);
+  if (whole <= 12) return launch_held<KIND, E, 1, 12>(r, stream);
   if (whole <= 16) return launch_held<KIND, E, 4, 4>(r, stream);
   if (whole <= 24) return launch_held<KIND, E, 8, 3>(r, stream);
   if (whole <= 32) return launch_held<KIND, E, 8, 4>(r, stream);
   if (whole <= 48) return launch_held<KIND, E, 8, 6>(r, stream);
   if (whole <= 64) return launch_held<KIND, E, 8, 8>(r, stream);
-  if (whole <= 96) return launch_held<KIND, E, 16, 6>(r, stream);
+  if (whole <= 96) return launch_held<KIND, E, 8, 12>(r, stream);
   if (whole <= 128) return launch_held<KIND, E, 16, 8>(r, stream);
   if (whole <= 192) return launch_held<KIND, E, 16, 12>(r, stream);
   if (whole <= 256) return launch_held<KIND, E, 16, 16>(r, stream);
@@ -683,8 +697,10 @@ unsigned launch_rows(const Rows& r, hipStream_t stream) {
   if constexpr (KIND != LogitsArgs::LOGP)
     if (r.dlogits) return launch_gradient<KIND, E>(r, stream);
   const int64_t bytes = (int64_t)r.V * sizeof(E);
-  if (bytes <= 4096) return launch_rows<KIND, E, 1>(r, stream);
-  if (bytes > 32768 && r.T <= 512) return launch_rows<KIND, E, 16>(r, stream);
+  // (100000 x 5000 bf16: 176 us by a wave a row, 209 by 4; 16 x 131072 float32: 9.1 by 16 waves, 24.3 by 4; 512 x 32000
+  // bf16: 6.5 and 7.0; 1000 x 32000: 13.3 and 12.6)
+  if (bytes <= 16384) return launch_rows<KIND, E, 1>(r, stream);
+  if (r.T <= 512) return launch_rows<KIND, E, 16>(r, stream);
   return launch_rows<KIND, E, 4>(r, stream);
 }
 template <int KIND>
@@ -730,7 +746,7 @@ hipError_t run_token_logp_bwd(const LogitsArgs& a, hipStream_t stream) {
   BwdRows r{};
   r.logits = a.logits; r.ids = a.ids; r.dlogits = a.dlogits; r.dlogp = a.dlogp; r.dlse = a.dlse; r.lse = a.lse_in; r.T = a.T; r.ld = a.ld;
   r.ld_out = a.ld_out; r.V = (int32_t)a.V; r.scale = a.scale; r.ids_i64 = a.ids_i64;
-  // (a wave where it takes a row at once, so that no lanes idle)
+  // (a wave where it takes a row at once, so that no lanes idle: 60000 x 1000 bf16 43 us, 71 by workgroups of 4)
   const int64_t pieces = (a.V + (a.f32 ? 3 : 7)) / (a.f32 ? 4 : 8);
   const int threads = pieces <= kChunk * 64 ? 64 : 256;
   r.chunks = (int32_t)((pieces + kChunk * threads - 1) / (kChunk * threads));
