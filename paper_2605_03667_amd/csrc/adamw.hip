@@ -5,7 +5,7 @@
 // moments, write p, the moments and the copy.  Tensors are cut into pieces, numbered through, one
 // to a workgroup (dealt out to 4096 workgroups in turn 1B in 8 bits took 960 us for 822).  A wave takes 256 values
 // at a time, 4 to a lane: a block of moments in 8 bits is one wave's, its largest magnitude
-// a maximum over the wave.  Bound by HBM where weights are float32 (1B, 247 M values with copies: 1317 us in 32 bits,
+// a maximum over the wave.  Bound by HBM where weights are float32 (1B, 246 M values with copies: 1317 us in 32 bits,
 // 5.6 TB/s; 748 in 8 bits, 5.9 TB/s), by about 60 instructions a value in 8 bits with bf16 weights and gradients (524 us, 4.7
 // TB/s).  60M, 3.9 M values: 20.6 us of kernel and 29 a call, which is what reading three lists of 49 tensors costs the host.
 #include <math.h>
@@ -26,7 +26,7 @@ constexpr int kBlock = ELAS_ADAMW_BLOCK;
 // weights in bf16 leave a block little to load (1B: 581 us with one, 523 with two; float32 weights 744 and 798).
 constexpr int piece_of(int at_once) { return 4 * at_once * kBlock; }
 constexpr uint32_t kGroups = 1u << 24;   // most workgroups per launch
-// Values from which on nothing is kept in the caches (350M, 81 M values: 231 us, 245 kept; 130M in 8 bits, 17 M: 62 and 59).
+// Values from which on nothing is kept in the caches (350M, 46 M values: 231 us, 245 kept; 130M in 8 bits, 17 M: 62 and 59).
 constexpr int64_t kStreamed = int64_t(1) << 25;
 constexpr float kTopM = 245760.f, kTopV = 507904.f;     // largest codes: 15 2^14, 31 2^14
 
