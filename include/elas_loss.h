@@ -21,8 +21,9 @@
  *          logits itself with the same pitch (every row is read before it is
  *          written); otherwise outputs overlap nothing.
  * Per-token operands and results are float32 [T] and need 4-byte alignment.
- * Sums over the vocabulary are float32 sums of at most a few hundred values, added up
- * pairwise; per-token terms and sums over tokens are 64-bit, in a fixed order.
+ * Sums over the vocabulary are float32, in groups of at most 32 values, of which a thread adds up at most
+ * 16 + V / 8192; per-token terms and sums over tokens are 64-bit.  Their order is fixed by the sizes, the types and the
+ * alignment of the rows.
  * A logit may be -inf (its p is 0).  Where a row holds nothing but -inf, a NaN or +inf,
  * its results follow the formulas (NaN, lse -inf), and so do the statistics; other rows do not change.
  * Requires 0 <= T < 2^31, 0 < V <= 2^30.  With T == 0 statistics are zeros and nothing else is

@@ -170,10 +170,12 @@ __device__ __forceinline__ void add_pieces(MaxSum& r, float c, const E* pieces, 
 #pragma unroll
       for (int k = 0; k < N; ++k) m = fmaxf(m, p[q].get(k));
     r.rescale(m, c);
+    float s = 0.f;
 #pragma unroll
     for (int q = 0; q < AT_ONCE; ++q)
 #pragma unroll
-      for (int k = 0; k < N; ++k) r.s += __builtin_amdgcn_exp2f((p[q].get(k) - m) * c);
+      for (int k = 0; k < N; ++k) s += __builtin_amdgcn_exp2f((p[q].get(k) - m) * c);
+    r.s += s;
   }
 }
 __device__ __forceinline__ void add_value(MaxSum& r, float c, float v) {
@@ -284,7 +286,8 @@ __global__ __launch_bounds__(Team<WAVES>::THREADS * Team<WAVES>::ROWS) void rows
 }
 
 // A loss with its gradient, the row in the registers of its team: PARTS pieces to a thread, what lies
-// behind the row -inf.  BEYOND: a longer row, whose pieces behind those are read twice (4000 x 131072 float32:
+// behind the row -inf.  BEYOND: a longer row, whose pieces behind those are read twice (4000 x 160000 bf16: 599 us, with 12
+// held, which spill, 865; 4000 x 131072 float32:
 // 853 us, 1300 with all of it read twice).  Loads and stores are non-temporal (65536 x 32000 bf16: 1488 us, with plain
 // loads 1548; before them, plain stores too, 1597 for 1537).
 template <int KIND, class E, int WAVES, int PARTS, bool BEYOND>
@@ -331,13 +334,16 @@ __global__ __launch_bounds__(Team<WAVES>::THREADS * Team<WAVES>::ROWS) void held
 #pragma unroll
     for (int q = 0; q < PARTS; ++q) p[q].keep_packed();
 #pragma unroll
-    for (int q = 0; q < PARTS; ++q)
+    for (int q = 0; q < PARTS; ++q) {
+      float s = 0.f;
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         const float e = __builtin_amdgcn_exp2f((p[q].get(k) - own) * c);
         if constexpr (KEEP) p[q].set(k, e);
-        r.s += e;
+        s += e;
       }
+      r.s += s;
+    }
 #pragma unroll
     for (int q = 0; q < PARTS; ++q) p[q].keep_packed();
     if constexpr (BEYOND) {
@@ -690,7 +696,7 @@ unsigned launch_gradient(const Rows& r, hipStream_t stream) {
   if (whole <= 128) return launch_held<KIND, E, 16, 8>(r, stream);
   if (whole <= 192) return launch_held<KIND, E, 16, 12>(r, stream);
   if (whole <= 256) return launch_held<KIND, E, 16, 16>(r, stream);
-  return launch_held<KIND, E, 16, sizeof(E) == 2 ? 12 : 16, true>(r, stream);
+  return launch_held<KIND, E, 16, sizeof(E) == 2 ? 6 : 16, true>(r, stream);
 }
 template <int KIND, class E>
 unsigned launch_rows(const Rows& r, hipStream_t stream) {

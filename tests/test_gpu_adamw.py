@@ -156,6 +156,28 @@ def test_many_steps(bits):
     _verify([777, 3000], [F32], [F32], bits, copies=True, steps=12)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_bounds_of_max_norm(bits):
+    """No clipping, all of it, and factors below float32's normal range (whose values are scaled all the same)."""
+    lengths = [700, 5]
+    for size, max_norm in ((1.0, math.inf), (1.0, 0.0), (1e25, 1e-10), (1e30, 1e-12), (0.0, 1.0)):
+        params, _ = _views(lengths, [F32], 1, 0.5)
+        grads, _ = _views(lengths, [F32], 2, size)
+        opt = elas.ElasAdamW(params, bits=bits)
+        before = [_f64(t) for t in params]
+        norm = elas.elas_grad_norm(grads)
+        elas.elas_adamw_step(opt, grads, 1e-2, norm=norm, max_norm=max_norm, **HYPER)
+        factor = oa.factor(float(norm), max_norm)
+        for k, (m, v) in enumerate(_moments(opt, lengths)):
+            zero = np.zeros(lengths[k])
+            # (the norm is a float32: half a step more in the factor)
+            p, m1, v1, p_err, m_err, v_err = oa.step(before[k], _f64(grads[k]), zero, zero, 1, 1e-2, 0.9, 0.95, 1e-8, 0.0, factor)
+            _near(_f64(params[k]), p, p_err, F32, (size, max_norm))
+            if bits == 32:
+                _near(m, m1, m_err + 2.0 ** -149, F32, (size, max_norm))
+            assert int(opt.step) == 1
+
+
 def test_rate_factor():
     for f in (0.5, 0.0, 2.0):
         _verify([300, 5], [F32], [F32], 32, rate_factor=torch.tensor([f], device=DEV), steps=2)
