@@ -679,20 +679,25 @@ unsigned launch_rows(const Rows& r, hipStream_t stream) {
 // The team that holds a row with the fewest idle lanes, of as few waves as leave a SIMD 4 or more of them.  In us, with the
 // next team beside it: 100000 x 2900 bf16 224 (4 waves of 2 pieces: 320), 60000 x 6000 262 (4 of 3: 280), 60000 x 8000 343
 // (8 of 2: 386), 60000 x 12000 538 (4 of 6: 570), 30000 x 16000 333 (4 of 8: 342), 65536 x 32000 1488 (4 of 16: 1591,
-// 16 of 4: 1689), 10000 x 48000 342 (16 of 6: 387), 16000 x 32000 float32 680 (8 of 16: 695).  Returns the workgroups.
+// 16 of 4: 1689), 10000 x 48000 342 (16 of 6: 387), 8000 x 50257 292 (16 of 8: 358), 8000 x 61000
+// 370 (16 of 8: 408), 16000 x 32000 float32 680 (8 of 16: 695).  Returns the workgroups.
 template <int KIND, class E>
 unsigned launch_gradient(const Rows& r, hipStream_t stream) {
   const int pieces = (r.V + Span<E>::N - 1) / Span<E>::N, whole = (pieces + 63) / 64;      // pieces to a lane of one wave
   if (whole <= 2) return launch_held<KIND, E, 1, 2>(r, stream);
   if (whole <= 4) return launch_held<KIND, E, 1, 4>(r, stream);
+  if (whole <= 6) return launch_held<KIND, E, 1, 6>(r, stream);
   if (whole <= 8) return launch_held<KIND, E, 1, 8>(r, stream);
   if (whole <= 12) return launch_held<KIND, E, 1, 12>(r, stream);
   if (whole <= 16) return launch_held<KIND, E, 4, 4>(r, stream);
   if (whole <= 24) return launch_held<KIND, E, 8, 3>(r, stream);
   if (whole <= 32) return launch_held<KIND, E, 8, 4>(r, stream);
   if (whole <= 48) return launch_held<KIND, E, 8, 6>(r, stream);
+  if (whole <= 56) return launch_held<KIND, E, 8, 7>(r, stream);
   if (whole <= 64) return launch_held<KIND, E, 8, 8>(r, stream);
   if (whole <= 96) return launch_held<KIND, E, 8, 12>(r, stream);
+  if (whole <= 112) return launch_held<KIND, E, 8, 14>(r, stream);
+  if (whole <= 120) return launch_held<KIND, E, 8, 15>(r, stream);
   if (whole <= 128) return launch_held<KIND, E, 16, 8>(r, stream);
   if (whole <= 192) return launch_held<KIND, E, 16, 12>(r, stream);
   if (whole <= 256) return launch_held<KIND, E, 16, 16>(r, stream);

@@ -104,6 +104,10 @@ def _check_all(x, ids, g, scale, seed, pitch=0, shift=0):
 WIDTHS = [1, 2, 3, 7, 8, 9, 63, 255, 256, 257, 511, 513, 1000, 1023, 1025, 2047, 2049, 4096, 5003, 8191, 16385, 32000, 32003, 65537, 131072, 150001]
 
 
+# widths for the other teams that hold a row (with both types)
+TEAMS = [10007, 13001, 15000, 27001, 30001, 48001, 50257, 61003, 64007]
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("V", WIDTHS)
 def test_widths(V, dtype):
@@ -113,7 +117,7 @@ def test_widths(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("V, pitch", [(v, p) for v in WIDTHS if v >= 2047 for p in (0, 3)])
+@pytest.mark.parametrize("V, pitch", [(v, p) for v in WIDTHS if v >= 2047 for p in (0, 3)] + [(v, 1) for v in TEAMS])
 def test_widths_of_many_tokens(V, pitch, dtype):
     """(Few rows are split over workgroups, many are not.)  300 tokens, 6 of which take part, so that the oracle has few rows
     to compute; all others have results and gradients of 0."""
