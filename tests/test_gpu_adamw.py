@@ -270,6 +270,48 @@ def test_values_of_codes():
     assert elas.elas_adam8_values(codes[:0], scale[:0]).shape == (0,)
 
 
+def test_moments_are_those_of_elementary_operations():
+    """Each product, sum and quotient rounded by itself in float32, in the formulas' order: the same bits, and so the same
+    codes.  (Codes below 2^mantissa are of a quotient rounded to 2^-20: another code is then 2^-21 likely, and such codes are one
+    in thousands.)"""
+    n = 100 * 256
+    g = torch.Generator(device=DEV)
+    g.manual_seed(4)
+    size = torch.exp(2 * torch.randn((100, 1), generator=g, device=DEV))
+    params = [torch.randn(n, generator=g, device=DEV)]
+    wide, eight = elas.ElasAdamW([params[0].clone()]), elas.ElasAdamW([params[0].clone()], bits=8)
+    m, v = torch.zeros((100, 256), device=DEV), torch.zeros((100, 256), device=DEV)
+    m8, v8 = m.clone(), v.clone()
+
+    def moments(m, v, grad):
+        return 0.9 * m + (1.0 - 0.9) * grad, 0.95 * v + (1.0 - 0.95) * grad * grad
+
+    def codes(x, mantissa, u, least=0):
+        scale = x.amax(1, keepdim=True) * torch.tensor(1.0 / oa.TOP[mantissa], device=DEV)
+        y = x / scale
+        shift = 23 - mantissa
+        high = ((y.view(torch.int32) + (u << (shift - 16))) >> shift) - ((126 + mantissa) << mantissa)
+        low = torch.floor(y + u / 65536.0).int()
+        code = torch.maximum(torch.where(y >= 2 ** mantissa, high, low).clamp_max(2 ** (mantissa + 4) - 1), least * (x > 0).int())
+        e, f = code >> mantissa, (code & (2 ** mantissa - 1)).float()
+        return code, scale, torch.where(e > 0, (f + 2 ** mantissa) * torch.exp2((e - 1).float()), f) * scale
+
+    for t in range(1, 4):
+        grad = torch.randn((100, 256), generator=g, device=DEV) * size
+        for opt in (wide, eight):
+            elas.elas_adamw_step(opt, [grad.view(-1)], 1e-3, **HYPER)
+        m, v = moments(m, v, grad)
+        assert torch.equal(wide.m.view(100, 256), m) and torch.equal(wide.v.view(100, 256), v)
+        m8, v8 = moments(m8, v8, grad)
+        u = torch.from_numpy(oa.random_bits(t, 0, np.arange(n)).astype(np.int64)).to(DEV).view(100, 256)
+        code, scale, held = codes(m8.abs(), 3, (u & 0xFFFF).int())
+        sign = m8 < 0
+        assert torch.equal(eight.m.view(100, 256).int(), code | sign.int() << 7) and torch.equal(eight.m_scale, scale[:, 0])
+        m8 = torch.where(sign, -held, held)
+        code, scale, v8 = codes(v8, 4, (u >> 16).int(), least=1)      # (a v above 0 is never rounded to 0)
+        assert torch.equal(eight.v.view(100, 256).int(), code) and torch.equal(eight.v_scale, scale[:, 0])
+
+
 def test_state_can_be_saved_and_repeated():
     """A state put back gives the same step, bit for bit (random bits come from the step's number)."""
     params, _ = _views([5000, 33], [F32, BF], 1, 1.0)

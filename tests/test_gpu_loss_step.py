@@ -216,6 +216,44 @@ def test_two_streams_at_once():
             assert all(torch.equal(r[n], want[k][n]) for n in r)
 
 
+@pytest.mark.parametrize("T", [12, 700])
+def test_two_graphs_with_one_workspace(T):
+    """Replayed in turn, with other calls on the same workspace between (12 rows are split over workgroups)."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T)
+    V = 20000
+    x = torch.randn((T, V), generator=g, device=DEV).to(BF)
+    ids = torch.randint(-1, V, (T,), generator=g, device=DEV)
+    adv = torch.randn(T, generator=g, device=DEV)
+    ws = torch.empty(elas.elas_token_loss_workspace_bytes(T, V), dtype=torch.uint8, device=DEV)
+    outs = [{"stats": torch.empty(k, device=DEV), "logp": torch.empty(T, device=DEV), "dlogits": torch.empty_like(x)} for k in (2, 3)]
+    calls = [lambda: elas.elas_token_loss(x, ids, z_coef=0.1, out=outs[0], workspace=ws), lambda: elas.elas_policy_loss(x, ids, adv, out=outs[1], workspace=ws)]
+    want, graphs = [], []
+    for call, out in zip(calls, outs):
+        call()
+        want.append({k: t.clone() for k, t in out.items()})
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call()
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        graphs.append(graph)
+    for rep in range(3):
+        for out in outs:
+            for t in out.values():
+                t.fill_(9.0)
+        for graph in graphs:
+            graph.replay()
+        elas.elas_token_loss(x, ids, out={"stats": torch.empty(2, device=DEV)}, workspace=ws)
+        torch.cuda.synchronize()
+        for out, w in zip(outs, want):
+            assert all(torch.equal(out[k], w[k]) for k in w), rep
+
+
 def test_timing_tags():
     h = _Head(8)
     try:
