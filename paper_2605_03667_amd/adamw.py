@@ -45,7 +45,7 @@ class ElasAdamW:
         self.params = _tensors(params)
         n = len(self.params)
         self.params.arrays(written=True)
-        copies = [None] * n if copies is None else list(copies)
+        copies = [None] * n if copies is None else list(copies.tensors if isinstance(copies, ElasTensors) else copies)
         decay = [float(d) for d in decay] if hasattr(decay, "__len__") else [float(decay)] * n
         if len(copies) != n or len(decay) != n:
             raise ValueError(f"{n} parameters, {len(copies)} copies, {len(decay)} decays")

@@ -67,37 +67,41 @@ def _matrix(t: torch.Tensor, shape, dtype: torch.dtype, device: int, name: str):
 
 def _logits(logits, ids):
     """(T, V, device, flags, logits' address and pitch, ids' address)."""
-    if logits.dim() != 2:
-        raise ValueError(f"logits must be 2-D, got shape {tuple(logits.shape)}")
-    if logits.dtype != _BF16 and logits.dtype != _F32:
-        raise ValueError(f"logits must be torch.bfloat16 or torch.float32, got {logits.dtype}")
-    T, V = logits.shape
+    shape = logits.shape
+    if len(shape) != 2:
+        raise ValueError(f"logits must be 2-D, got shape {tuple(shape)}")
+    dtype = logits.dtype
+    if dtype == _F32:
+        flags = ELAS_LOGITS_F32
+    elif dtype == _BF16:
+        flags = 0
+    else:
+        raise ValueError(f"logits must be torch.bfloat16 or torch.float32, got {dtype}")
     dev = logits.get_device()
-    x, ld = _matrix(logits, (T, V), logits.dtype, dev, "logits")
-    if ids.shape != (T,):
+    x, ld = _matrix(logits, shape, dtype, dev, "logits")
+    T, V = shape
+    if ids.shape != shape[:1]:
         raise ValueError(f"ids has shape {tuple(ids.shape)}, expected {(T,)}")
-    ids_p, flags = _ids(ids, dev)
-    return T, V, dev, flags | (ELAS_LOGITS_F32 if logits.dtype == _F32 else 0), x, ld, ids_p
+    ids_p, ids_flag = _ids(ids, dev)
+    return T, V, dev, flags | ids_flag, x, ld, ids_p
 
 
-def _apart(d, logits):
-    """Raises where dlogits' memory overlaps the logits' and is not the very same rows."""
-    size = logits.element_size()
-    spans = [(t.data_ptr(), t.data_ptr() + ((t.shape[0] - 1) * t.stride(0) + t.shape[1]) * size) for t in (d, logits)]
-    if d.shape[0] and spans[0] != spans[1] and spans[0][0] < spans[1][1] and spans[1][0] < spans[0][1]:
-        # (columns beside one another in rows of one pitch are apart)
-        pitch = logits.stride(0)
-        offset = abs(spans[0][0] - spans[1][0]) // size % pitch if pitch else 0
-        if d.stride(0) != pitch or not logits.shape[1] <= offset <= pitch - logits.shape[1]:
-            raise ValueError("dlogits must be logits itself or overlap nothing of it")
+def _apart(T, V, size, x, ld, d, ld_out):
+    """Raises where the memory of the gradient (at ``d``) overlaps the logits' (at ``x``) and is not the very same rows."""
+    if d == x and ld_out == ld or not T:
+        return
+    end, end_out = x + ((T - 1) * ld + V) * size, d + ((T - 1) * ld_out + V) * size
+    # (columns beside one another in rows of one pitch are apart)
+    if x < end_out and d < end and (ld_out != ld or not V <= abs(x - d) // size % ld <= ld - V):
+        raise ValueError("dlogits must be logits itself or overlap nothing of it")
 
 
-def _gradient(dlogits, logits, dev):
+def _gradient(dlogits, logits, dev, x, ld):
     """Address and pitch of the gradient's tensor; (None, 0) where it is not wanted."""
     if dlogits is None:
         return None, 0
     p, pitch = _matrix(dlogits, logits.shape, logits.dtype, dev, "dlogits")
-    _apart(dlogits, logits)
+    _apart(*logits.shape, logits.element_size(), x, ld, p, pitch)
     return p, pitch
 
 
@@ -145,7 +149,7 @@ def elas_token_logp_bwd(dlogp, logits, ids, lse, scale: float = 1.0, dlse: torch
     T, V, dev, flags, x, ld, ids_p = _logits(logits, ids)
     if dlogits is None:
         dlogits = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
-    d_p, ld_out = _gradient(dlogits, logits, dev)
+    d_p, ld_out = _gradient(dlogits, logits, dev, x, ld)
     _on(dev, lib().elas_token_logp_bwd, _arg(dlogp, (T,), _F32, dev, "dlogp"), _opt(dlse, (T,), _F32, dev, "dlse"), x, ld, ids_p,
         _arg(lse, (T,), _F32, dev, "lse"), T, V, scale, flags, d_p, ld_out)
     return dlogits
@@ -166,7 +170,7 @@ def elas_token_loss(logits, ids, weight: torch.Tensor | None = None, scale: floa
         out = {"stats": _rows(2, logits.device), "logp": _rows(T, logits.device), "lse": _rows(T, logits.device),
                "dlogits": torch.empty((T, V), dtype=logits.dtype, device=logits.device)}
     stats_p = _arg(_required(out.get("stats"), "out['stats']"), (2,), _F32, dev, "out['stats']")
-    d_p, ld_out = _gradient(out.get("dlogits"), logits, dev)
+    d_p, ld_out = _gradient(out.get("dlogits"), logits, dev, x, ld)
     workspace, ws_p, ws_n = _space(workspace, elas_token_loss_workspace_bytes(T, V, flags & ELAS_LOGITS_F32), logits.device)
     _on(dev, lib().elas_token_loss, x, ld, ids_p, _opt(weight, (T,), _F32, dev, "weight"), T, V, scale, reduce, z_coef, flags,
         _opt(out.get("logp"), (T,), _F32, dev, "out['logp']"), _opt(out.get("lse"), (T,), _F32, dev, "out['lse']"), d_p, ld_out, stats_p,
@@ -193,7 +197,7 @@ def elas_policy_loss(logits, ids, advantage, old_logp: torch.Tensor | None = Non
         out = {"stats": _rows(3, logits.device), "logp": _rows(T, logits.device),
                "dlogits": torch.empty((T, V), dtype=logits.dtype, device=logits.device)}
     stats_p = _arg(_required(out.get("stats"), "out['stats']"), (3,), _F32, dev, "out['stats']")
-    d_p, ld_out = _gradient(out.get("dlogits"), logits, dev)
+    d_p, ld_out = _gradient(out.get("dlogits"), logits, dev, x, ld)
     row = (T,)
     workspace, ws_p, ws_n = _space(workspace, elas_token_loss_workspace_bytes(T, V, flags & ELAS_LOGITS_F32), logits.device)
     _on(dev, lib().elas_policy_loss, x, ld, ids_p, _arg(advantage, row, _F32, dev, "advantage"), _opt(old_logp, row, _F32, dev, "old_logp"),

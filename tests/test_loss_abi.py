@@ -228,12 +228,16 @@ def test_gradients_beside_their_logits():
     buf = torch.zeros(400, dtype=BF)
     rows = lambda at, pitch, n=4, v=8: buf[at:].as_strided((n, v), (pitch, 1))  # noqa: E731
     x = rows(40, 24)
+    def apart(d, x):
+        (n, v), at = x.shape, lambda t: (t.data_ptr(), t.stride(0))  # noqa: E731
+        binding._apart(n, v, 2, *at(x), *at(d))
+
     for good in (rows(40, 24), rows(48, 24), rows(32, 24), rows(56, 24), rows(40 + 3 * 24 + 8, 10), rows(0, 8), torch.zeros(4, 8, dtype=BF)):
-        binding._apart(good, x)
+        apart(good, x)
     for bad in (rows(41, 24), rows(47, 24), rows(33, 24), rows(57, 24), rows(40, 16), rows(16, 8), rows(40 + 24, 24)):
         with pytest.raises(ValueError, match="overlap"):
-            binding._apart(bad, x)
-    binding._apart(x[:0], x[:0])
+            apart(bad, x)
+    apart(x[:0], x[:0])
 
 
 def test_calls_go_to_the_operands_gpu(monkeypatch):
