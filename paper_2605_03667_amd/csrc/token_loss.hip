@@ -153,10 +153,11 @@ __device__ __forceinline__ const E* at_value(const E* uniform, int i) {
   return (const E*)((const char*)uniform + (uint32_t)i * (uint32_t)sizeof(E));
 }
 
-// Maximum and sum of a thread's pieces i, i + stride .. of a row and of an edge, 4 pieces at a time.
+// Maximum and sum of a thread's pieces i, i + stride .. of a row, 2 pieces at a time (200000 x 1000 bf16
+// without a gradient 80 us, with 4 at a time 98, the others alike).
 template <class E, bool STREAM>
 __device__ __forceinline__ void add_pieces(MaxSum& r, float c, const E* pieces, int i, int full, int stride) {
-  constexpr int N = Span<E>::N, AT_ONCE = 4;
+  constexpr int N = Span<E>::N, AT_ONCE = 2;
   for (; i < full; i += AT_ONCE * stride) {
     Span<E> p[AT_ONCE];
 #pragma unroll
@@ -524,7 +525,7 @@ __global__ __launch_bounds__(1024) void loss_sum_kernel(const double* part, int 
 }
 
 // Gradient from those of logp and lse: every value by itself, kChunk pieces of a row to a thread at a time (8192 x 32000
-// bf16: 168 us with 2, 174 with 4, 176 with 8 or 16).  Bound by HBM: 6.2 TB/s.  (A lse beyond kLargeLse leaves
+// bf16, by 4 waves: 168 us with 2, 174 with 4, 176 with 8 or 16).  Bound by HBM: 6.3 TB/s.  (A lse beyond kLargeLse leaves
 // exp(z - lse) an error of 2^-24 of that, and among logits of a type's lowest value it holds nothing of the sum at all.)
 constexpr float kLargeLse = 4096.f;
 constexpr int kChunk = 2;
@@ -757,9 +758,10 @@ hipError_t run_token_logp_bwd(const LogitsArgs& a, hipStream_t stream) {
   BwdRows r{};
   r.logits = a.logits; r.ids = a.ids; r.dlogits = a.dlogits; r.dlogp = a.dlogp; r.dlse = a.dlse; r.lse = a.lse_in; r.T = a.T; r.ld = a.ld;
   r.ld_out = a.ld_out; r.V = (int32_t)a.V; r.scale = a.scale; r.ids_i64 = a.ids_i64;
-  // (a wave where it takes a row at once, so that no lanes idle: 60000 x 1000 bf16 43 us, 71 by workgroups of 4)
+  // (a wave where it takes a row at once, else two, so that few lanes idle: 60000 x 1000 bf16 43 us, 71 by workgroups of 4;
+  // 100000 x 5000 359, 431 by 4; 65536 x 32000 1407 and 1428)
   const int64_t pieces = (a.V + (a.f32 ? 3 : 7)) / (a.f32 ? 4 : 8);
-  const int threads = pieces <= kChunk * 64 ? 64 : 256;
+  const int threads = pieces <= kChunk * 64 ? 64 : 128;
   r.chunks = (int32_t)((pieces + kChunk * threads - 1) / (kChunk * threads));
   TimedLaunch tl("token_logp_bwd", stream);
   const auto launch = [&](auto kernel) {
@@ -768,7 +770,7 @@ hipError_t run_token_logp_bwd(const LogitsArgs& a, hipStream_t stream) {
   if (threads == 64)
     a.f32 ? launch(logp_bwd_kernel<float, 64>) : launch(logp_bwd_kernel<uint16_t, 64>);
   else
-    a.f32 ? launch(logp_bwd_kernel<float, 256>) : launch(logp_bwd_kernel<uint16_t, 256>);
+    a.f32 ? launch(logp_bwd_kernel<float, 128>) : launch(logp_bwd_kernel<uint16_t, 128>);
   return hipGetLastError();
 }
 
