@@ -6,8 +6,8 @@
 // exp2((x - max) scale log2(e)), then the token's own terms, and writes the gradient.  The maximum is of the
 // logits themselves, so that a row of nothing but a type's lowest value is a uniform distribution at
 // any scale.  Statistics are 64-bit sums per workgroup over its rows, added up by a second launch.  65536 x 32000
-// bf16 with gradient: 1514 us, 5.5 TB/s (read twice: 2153); 16381 x 32000 bf16, an eighth padding and
-// a sixth of weight 0: 331; 2000 x 32000 float32: 86; 4093 x 32003 float32 without one: 70.
+// bf16 with gradient: 1514 to 1538 us, 5.5 TB/s (read twice: 2153); 16381 x 32000 bf16, an eighth padding
+// and a sixth of weight 0: 329; 2000 x 32000 float32: 86; 4093 x 32003 float32 without one: 72.
 #include <math.h>
 
 #include <algorithm>
