@@ -1,7 +1,7 @@
 // Log-probabilities of tokens from logits and the losses on them, with their gradients
 // (the formulas are in include/elas_loss.h).
 //
-// Bound by HBM: 2 to 6 instructions a value and an exponential or two against one read and one write of it.  So a row
+// Bound by HBM: about 8 instructions and an exponential or two a value against one read and one write of it.  So a row
 // is read once: a team of 1 to 16 waves holds it in registers, finds its maximum and the sum of
 // exp2((x - max) scale log2(e)), then the token's own terms, and writes the gradient.  The maximum is of the
 // logits themselves, so that a row of nothing but a type's lowest value is a uniform distribution at
