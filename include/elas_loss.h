@@ -107,7 +107,7 @@ int elas_policy_loss(const void* logits, int64_t ld, const void* ids, const floa
  *
  *     z_i = beta (c_i - d_i),  l_i = -(1 - smoothing) log sigmoid(z_i) - smoothing log sigmoid(-z_i)
  *     stats = mean_i l_i, share of z_i > 0, mean_i z_i;   margin_i = z_i
- *     dlogp = +-beta (smoothing - sigmoid(-z_i)) / pairs over the chosen / rejected answer
+ *     dlogp = +-beta (smoothing sigmoid(z_i) - (1 - smoothing) sigmoid(-z_i)) / pairs over the chosen / rejected answer
  *
  * logp, ref_logp [N] float32 (ref_logp NULL: 0); offsets [2 pairs + 1] int32
  * (ELAS_IDS_I64: int64), in rising order; the kernel holds each to 0 .. N.

@@ -156,7 +156,7 @@ def preference_loss(logp, ref, offsets, beta, smoothing):
         z = margin[i] = beta * (diff[a:b].sum() - diff[b:c].sum())
         soft = np.log1p(np.exp(-abs(z)))
         loss += (1 - smoothing) * (soft + max(-z, 0.0)) + smoothing * (soft + max(z, 0.0))
-        g = (smoothing - np.exp(-max(z, 0.0) - soft)) * beta / pairs
+        g = (smoothing * np.exp(-max(-z, 0.0) - soft) - (1 - smoothing) * np.exp(-max(z, 0.0) - soft)) * beta / pairs
         dlogp[a:b] = g
         dlogp[b:c] = -g
     n = max(pairs, 1)

@@ -94,12 +94,12 @@ struct Pair {
   __device__ __forceinline__ Pair(const PreferenceArgs& a, double chosen, double rejected) {
     z = (double)a.beta * (chosen - rejected);
     const double q = (double)a.smoothing;
-    // ln(1 + exp(-|z|)), and sigmoid(-z), without overflow
+    // ln(1 + exp(-|z|)), and sigmoid(z) and sigmoid(-z), without overflow, the smaller one not as 1 less the larger
     const double e = exp_of_minus(fabs(z)), soft = log_of_one_and(e);
-    const double away = (z > 0.0 ? e : 1.0) / (1.0 + e);
+    const double large = 1.0 / (1.0 + e), small = e * large, towards = z > 0.0 ? large : small, away = z > 0.0 ? small : large;
     // a weight of 0 takes no part, infinite as the other side may be
     loss = (q < 1.0 ? (1.0 - q) * (soft + fmax(-z, 0.0)) : 0.0) + (q > 0.0 ? q * (soft + fmax(z, 0.0)) : 0.0);
-    g = (float)((q - away) * (double)a.beta / (double)a.pairs);
+    g = (float)((q * towards - (1.0 - q) * away) * (double)a.beta / (double)a.pairs);
     if (z != z) loss = z, g = (float)z;
   }
 };

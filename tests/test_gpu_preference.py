@@ -31,9 +31,10 @@ def _verify(logp, ref, offsets, beta, smoothing):
     for k, w in want.items():
         g = got[k].double().cpu().numpy()
         # (a number below float32's normal range: a step of 2^-149)
-        # dlogp's relative change with z is at most 1 a unit of z
+        # dlogp's relative change with z is at most 1 a unit of z, and its two sigmoids, each to 2e-10 of itself, may cancel
         rel = 2.0 ** -24 * 1.01 + (noise if k == "dlogp" else 0.0)
-        assert np.all(np.abs(g - w) <= rel * np.abs(w) + 2.0 ** -149 + (0.0 if k == "dlogp" else noise)), (k, np.abs(g - w).max())
+        both = 2e-10 * abs(beta) / max(len(offsets) // 2, 1) * min(smoothing, 1 - smoothing) if k == "dlogp" else 0.0
+        assert np.all(np.abs(g - w) <= rel * np.abs(w) + both + 2.0 ** -149 + (0.0 if k == "dlogp" else noise)), (k, np.abs(g - w).max())
     alone = elas.elas_preference_loss(logp, offsets, ref, beta, smoothing, out={"stats": torch.empty(3, device=DEV)})
     assert torch.equal(alone["stats"], got["stats"])
     inplace = logp.clone()
@@ -74,6 +75,14 @@ def test_large_margins():
         g = r["dlogp"].cpu().numpy()
         assert np.isnan(g[:2]).all() if value != value else g[0] == (0.0 if value > 0 else -np.float32(0.1) / 2)
         assert np.isfinite(g[2:]).all()
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 0.25, 1.0])
+def test_gradients_of_far_margins(smoothing):
+    """A sigmoid near 0 is not 1 less one near 1: the gradient keeps its relative precision at both ends."""
+    for z in (-60.0, -33.0, -20.0, 20.0, 33.0, 60.0):
+        logp = torch.tensor([z, 0.0], device=DEV)
+        _verify(logp, None, torch.tensor([0, 1, 2], device=DEV), 1.0, smoothing)
 
 
 def test_no_pairs():
