@@ -105,6 +105,17 @@ def _gradient(dlogits, logits, dev, x, ld):
     return p, pitch
 
 
+def _rows_apart(T, written, read):
+    """Raises where a result [T] (of the addresses ``written``) overlaps another one or an operand [T] (``read``): the
+    thread that writes it is not the only one that reads the operand."""
+    size = 4 * T
+    for k, p in enumerate(written):
+        if p:
+            for q in written[:k] + read:
+                if q and -size < p - q < size:
+                    raise ValueError("logp and lse of out must not overlap each other nor another operand")
+
+
 def _space(workspace, need: int, device: torch.device):
     """The caller's workspace or a new one, its address and size."""
     if workspace is None:
@@ -137,6 +148,7 @@ def elas_token_logp_fwd(logits, ids, scale: float = 1.0, out: dict | None = None
         out = {"logp": _rows(T, logits.device), "lse": _rows(T, logits.device)}
     logp_p = _arg(_required(out.get("logp"), "out['logp']"), (T,), _F32, dev, "out['logp']")
     lse_p = _opt(out.get("lse"), (T,), _F32, dev, "out['lse']")
+    _rows_apart(T, (logp_p, lse_p), ())
     _on(dev, lib().elas_token_logp_fwd, x, ld, ids_p, T, V, scale, flags, logp_p, lse_p)
     return out
 
@@ -171,10 +183,12 @@ def elas_token_loss(logits, ids, weight: torch.Tensor | None = None, scale: floa
                "dlogits": torch.empty((T, V), dtype=logits.dtype, device=logits.device)}
     stats_p = _arg(_required(out.get("stats"), "out['stats']"), (2,), _F32, dev, "out['stats']")
     d_p, ld_out = _gradient(out.get("dlogits"), logits, dev, x, ld)
+    row = (T,)
+    weight_p = _opt(weight, row, _F32, dev, "weight")
+    rows = (_opt(out.get("logp"), row, _F32, dev, "out['logp']"), _opt(out.get("lse"), row, _F32, dev, "out['lse']"))
+    _rows_apart(T, rows, (weight_p,))
     workspace, ws_p, ws_n = _space(workspace, elas_token_loss_workspace_bytes(T, V, flags & ELAS_LOGITS_F32), logits.device)
-    _on(dev, lib().elas_token_loss, x, ld, ids_p, _opt(weight, (T,), _F32, dev, "weight"), T, V, scale, reduce, z_coef, flags,
-        _opt(out.get("logp"), (T,), _F32, dev, "out['logp']"), _opt(out.get("lse"), (T,), _F32, dev, "out['lse']"), d_p, ld_out, stats_p,
-        ws_p, ws_n)
+    _on(dev, lib().elas_token_loss, x, ld, ids_p, weight_p, T, V, scale, reduce, z_coef, flags, *rows, d_p, ld_out, stats_p, ws_p, ws_n)
     return out
 
 
@@ -199,10 +213,13 @@ def elas_policy_loss(logits, ids, advantage, old_logp: torch.Tensor | None = Non
     stats_p = _arg(_required(out.get("stats"), "out['stats']"), (3,), _F32, dev, "out['stats']")
     d_p, ld_out = _gradient(out.get("dlogits"), logits, dev, x, ld)
     row = (T,)
+    rows = (_arg(advantage, row, _F32, dev, "advantage"), _opt(old_logp, row, _F32, dev, "old_logp"),
+            _opt(ref_logp, row, _F32, dev, "ref_logp"), _opt(weight, row, _F32, dev, "weight"))
+    logp_p = _opt(out.get("logp"), row, _F32, dev, "out['logp']")
+    _rows_apart(T, (logp_p,), rows)
     workspace, ws_p, ws_n = _space(workspace, elas_token_loss_workspace_bytes(T, V, flags & ELAS_LOGITS_F32), logits.device)
-    _on(dev, lib().elas_policy_loss, x, ld, ids_p, _arg(advantage, row, _F32, dev, "advantage"), _opt(old_logp, row, _F32, dev, "old_logp"),
-        _opt(ref_logp, row, _F32, dev, "ref_logp"), _opt(weight, row, _F32, dev, "weight"), T, V, scale, reduce, clip_low, clip_high, kl_coef,
-        flags, _opt(out.get("logp"), row, _F32, dev, "out['logp']"), d_p, ld_out, stats_p, ws_p, ws_n)
+    _on(dev, lib().elas_policy_loss, x, ld, ids_p, *rows, T, V, scale, reduce, clip_low, clip_high, kl_coef, flags, logp_p, d_p, ld_out, stats_p,
+        ws_p, ws_n)
     return out
 
 

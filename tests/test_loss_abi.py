@@ -240,6 +240,26 @@ def test_gradients_beside_their_logits():
     apart(x[:0], x[:0])
 
 
+def test_results_apart_from_operands():
+    """A policy loss whose logp goes over old_logp (which other waves may still read), and the like, is refused
+    before the call."""
+    gpu = lambda t: t.as_subclass(_OnGpu)  # noqa: E731
+    x, ids, rows = gpu(torch.zeros(4, 10)), gpu(torch.zeros(4, dtype=torch.int64)), gpu(torch.zeros(60))
+    row = lambda k, shift=0: rows[8 * k + shift:8 * k + shift + 4]  # noqa: E731
+    stats = {"stats": rows[50:52]}
+    for fn, a, k in ((elas.elas_token_logp_fwd, (), {"out": {"logp": row(0), "lse": row(0)}}),
+                     (elas.elas_token_logp_fwd, (), {"out": {"logp": row(0), "lse": row(0, 3)}}),
+                     (elas.elas_token_loss, (), {"out": {**stats, "logp": row(0), "lse": row(0, 1)}}),
+                     (elas.elas_token_loss, (row(1),), {"out": {**stats, "logp": row(1)}}),
+                     (elas.elas_token_loss, (row(1),), {"out": {**stats, "lse": row(1, -3)}}),
+                     *((elas.elas_policy_loss, (row(1), row(2), row(3), row(4)), {"out": {"stats": rows[50:53], "logp": row(j)}}) for j in range(1, 5))):
+        with pytest.raises(ValueError, match="overlap"):
+            fn(x, ids, *a, **k)
+    binding._rows_apart(4, (100, 116), (84, 132, None))
+    binding._rows_apart(4, (100, None), (None, 200))
+    binding._rows_apart(0, (100, 100), (100,))
+
+
 def test_calls_go_to_the_operands_gpu(monkeypatch):
     """A default stream's handle does not say which GPU it is of: a call for another GPU than
     the current one is made with that one current."""
