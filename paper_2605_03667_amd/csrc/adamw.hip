@@ -25,7 +25,7 @@ constexpr int kBlock = ELAS_ADAMW_BLOCK;
 // Values of a piece: AT_ONCE blocks to each of a workgroup's 4 waves.  One, but two where moments in 8 bits and
 // weights in bf16 leave a block little to load (1B: 581 us with one, 523 with two; float32 weights 744 and 798).
 constexpr int piece_of(int at_once) { return 4 * at_once * kBlock; }
-constexpr uint32_t kGroups = 1u << 24;   // most workgroups per launch
+constexpr uint32_t kGroups = 1u << 23;   // most workgroups of a launch, of 256 threads: a grid has fewer than 2^32 threads
 // Values from which on nothing is kept in the caches (350M, 46 M values: 231 us, 245 kept; 130M in 8 bits, 17 M: 62 and 59).
 constexpr int64_t kStreamed = int64_t(1) << 25;
 constexpr float kTopM = 245760.f, kTopV = 507904.f;     // largest codes: 15 2^14, 31 2^14
@@ -453,7 +453,8 @@ hipError_t run_adamw(const AdamwArgs& a, hipStream_t stream) {
 hipError_t run_adam8_values(const uint8_t* codes, const float* scale, int64_t blocks, bool second, bool f32, void* out, hipStream_t stream) {
   TimedLaunch tl("adam8_values", stream);
   const auto launch = [&](auto kernel, auto* to) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((blocks * (kBlock / 8) + 255) / 256, 1 << 24)), dim3(256), 0, stream, codes, scale, blocks, to);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((blocks * (kBlock / 8) + 255) / 256, kGroups)), dim3(256), 0, stream, codes,
+                       scale, blocks, to);
   };
   if (second)
     f32 ? launch(adam8_values_kernel<true, float>, (float*)out) : launch(adam8_values_kernel<true, uint16_t>, (uint16_t*)out);

@@ -98,3 +98,34 @@ def test_adamw(bits):
             # a neighbour: an eighth of the value away at most, and half a step of bf16
             assert np.all(np.abs(m - want[k][1]) <= (1 / 8 + 2.0 ** -8) * np.abs(want[k][1]) + np.abs(want[k][1]).max() / oa.TOP[3])
     assert not p[0][: 1 << 20].any() and not p[0][n - (1 << 20):n - tail].any()
+
+
+def test_adamw_of_more_pieces_than_a_grid_has_threads_for():
+    """2^34 values in pieces of 1024, a workgroup of 256 threads to each, would be 2^32 threads."""
+    n, tail = (1 << 34) + 300, 600
+    p, g = torch.zeros(n, device=DEV), torch.zeros(n, dtype=BF, device=DEV)
+    ends = (slice(0, tail), slice(n - tail, n))
+    for at in ends:
+        p[at], g[at] = 0.5, torch.randn(tail, device=DEV).to(BF)
+    want = []
+    for at in ends:
+        x = p[at].double().cpu().numpy()
+        want.append(oa.step(x, g[at].double().cpu().numpy(), 0 * x, 0 * x, 1, 0.01, 0.9, 0.999, 1e-8, 0.0))
+    opt = elas.ElasAdamW([p], bits=8)
+    elas.elas_adamw_step(opt, [g], 0.01)
+    assert int(opt.step) == 1
+    for at, w in zip(ends, want):
+        assert np.all(np.abs(p[at].double().cpu().numpy() - w[0]) <= w[3] * 1.01 + 2.0 ** -24 * np.abs(w[0]))
+    assert not p[tail: 1 << 20].any() and not p[n - (1 << 20):n - tail].any()
+
+
+def test_values_of_more_codes_than_a_grid_has_threads_for():
+    """2^35 codes, 8 to a thread."""
+    blocks = (1 << 27) + 3
+    codes, scale = torch.zeros(256 * blocks, dtype=torch.uint8, device=DEV), torch.ones(blocks, device=DEV)
+    some = torch.randint(0, 256, (700,), dtype=torch.uint8, device=DEV)
+    codes[:700], codes[-700:] = some, some
+    want = elas.elas_adam8_values(torch.cat([some, some.new_zeros(68)]), scale[:3].clone())[:700]
+    got = elas.elas_adam8_values(codes, scale)
+    assert torch.equal(got[:700], want) and torch.equal(got[-700:], want)
+    assert not got[700: 1 << 20].any() and not got[256 * blocks - (1 << 20):-700].any()
