@@ -53,7 +53,7 @@ int elas_token_logp_fwd(const void* logits, int64_t ld, const void* ids, int64_t
  *
  *     dlogits_tj = scale (dlogp_t (1[j = id_t] - p_tj) + dlse_t p_tj)
  *
- * lse is the forward's on these logits (p = exp(z - lse) has a relative error of 2^-24 (|z| + 3 |z - lse| + 6);
+ * lse is that of elas_token_logp_fwd on these logits (of a loss too, where no weight is 0) (p = exp(z - lse) has a relative error of 2^-24 (|z| + 3 |z - lse| + 6);
  * where |lse| is above 4096 or not finite the row's sum is taken anew); dlse NULL: zero.
  */
 int elas_token_logp_bwd(const float* dlogp, const float* dlse, const void* logits, int64_t ld, const void* ids,
@@ -89,6 +89,7 @@ int elas_token_loss(const void* logits, int64_t ld, const void* ids, const float
  *     dlogp_t = reduce w_t (-r A [the clamp does not hold] - kl_coef (exp(q) - 1))
  *     dlogits_tj = scale dlogp_t (1[j = id_t] - p_tj)
  *
+ * A coefficient or an advantage of 0 takes no part, as large as what it multiplies may be.
  * old_logp NULL: the policy that sampled the tokens is this one (r = 1, with its
  * gradient).  ref_logp NULL: no KL term (kl_coef is then 0).  weight NULL: 1; a
  * token of weight 0 takes no part.  logp and dlogits may be NULL: not wanted.

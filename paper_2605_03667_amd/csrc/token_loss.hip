@@ -66,7 +66,7 @@ __device__ __forceinline__ float exp_minus_line(float q) {
     s = fmaf(s, q, 1.f) * (1.f / 2.f);
     return s * q * q;
   }
-  return expm1f(q) - q;
+  return q == INFINITY ? q : expm1f(q) - q;
 }
 
 // ln of a sum of exponentials; its two parts are added in 64 bits.
@@ -107,12 +107,16 @@ __device__ __forceinline__ Terms row_terms(const Rows& a, int64_t t, float w, fl
     const float ratio = a.old_logp ? expf((float)(logp - (double)a.old_logp[t])) : 1.f;
     const bool held = adv > 0.f ? ratio > a.high : adv < 0.f && ratio < a.low;
     const float bounded = fminf(fmaxf(ratio, a.low), a.high);
-    float loss = -(held ? bounded * adv : ratio * adv), g = held ? 0.f : -ratio * adv, k = 0.f;
+    // (an advantage or a coefficient of 0 takes no part where the exponential beside it passes float32's range)
+    const float gain = adv == 0.f && ratio == INFINITY ? 0.f : ratio * adv;
+    float loss = -(held ? bounded * adv : gain), g = held ? 0.f : -gain, k = 0.f;
     if (a.ref_logp) {
       const float q = (float)((double)a.ref_logp[t] - logp);
       k = exp_minus_line(q);
-      loss = fmaf(a.kl_coef, k, loss);
-      g = fmaf(-a.kl_coef, expm1f(q), g);
+      if (a.kl_coef != 0.f) {
+        loss = fmaf(a.kl_coef, k, loss);
+        g = fmaf(-a.kl_coef, expm1f(q), g);
+      }
     }
     r.sum[0] = (double)c * (double)loss;
     r.sum[1] = (double)c * (double)k;

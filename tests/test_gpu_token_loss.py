@@ -258,6 +258,36 @@ def _all_near(got, want, dtype):
         _near(got[k], *want[k], dtype if k == "dlogits" else F32, k)
 
 
+@pytest.mark.parametrize("gradient", [True, False])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [100, 5001, 32000])
+def test_zeros_beside_exponentials_that_overflow(V, dtype, gradient):
+    """kl_coef 0 where the reference is e^200 times as sure of a token (or the policy rules it out), and advantage 0
+    where the ratio is e^100: neither takes part."""
+    T = 6
+    x, ids, g = _inputs(T, V, dtype, V + 5)
+    x[0].scatter_(0, ids[:1], -200.0)
+    x[1].scatter_(0, ids[1:2], -INF)
+    logp = elas.elas_token_logp_fwd(x, ids)["logp"]
+    adv, ref = torch.randn(T, generator=g, device=DEV), torch.full((T,), -1.0, device=DEV)
+    old = logp.clone()
+    old[1] = -2.0          # (its ratio is 0)
+    old[2] -= 100.0
+    adv[2] = 0.0
+    n = _f64(x)
+    want, near = ol.policy_loss(np.where(np.isinf(n), -600.0, n), ids.cpu().numpy(), _f64(adv), _f64(old), _f64(ref), None, 1.0, 0.5, 0.2, 0.2, 0.0)
+    assert not near.any()
+    out = {"stats": torch.empty(3, device=DEV)}
+    if gradient:
+        out["dlogits"] = torch.empty_like(x)
+    elas.elas_policy_loss(x, ids, adv, old_logp=old, ref_logp=ref, reduce=0.5, out=out)
+    for k in (0, 2):
+        _near(out["stats"][k], want["stats"][0][k], want["stats"][1][k], name=k)
+    assert out["stats"][1] == INF
+    if gradient:
+        _near(out["dlogits"], *want["dlogits"], dtype, "dlogits")
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("V", [100, 1000, 5001, 32000, 66000, 140003])
 def test_in_place(V, dtype):
