@@ -53,8 +53,8 @@ extern "C" {
  *                infinite or NaN the step is skipped: nothing changes, step neither.
  * rate_factor    device float32 [1] or NULL: a schedule that a captured graph can follow.
  * m, v and the scales are 16-byte aligned.
- * Requires 0 <= n < 2^20, fewer than 2^40 values in all, 0 <= beta < 1, finite rate and eps > 0
- * (all in float32), max_norm >= 0, step >= 0.  workspace >= elas_adamw_workspace_bytes() bytes.
+ * Requires 0 <= n < 2^20, fewer than 2^40 values in all, 0 <= beta < 1, finite rate and
+ * eps >= 2^-126 (all in float32), max_norm >= 0, step >= 0.  workspace >= elas_adamw_workspace_bytes() bytes.
  */
 size_t elas_adamw_workspace_bytes(void);
 int elas_adamw_step(void* const* params, const void* const* grads, uint16_t* const* copies, const int64_t* numel,

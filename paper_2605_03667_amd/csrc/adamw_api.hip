@@ -43,7 +43,8 @@ int elas_adamw_step(void* const* params, const void* const* grads, uint16_t* con
   ELAS_CHECK(check_scale((float)rate, "rate (as float32)"));
   ELAS_CHECK(check_beta(beta1, "beta1"));
   ELAS_CHECK(check_beta(beta2, "beta2"));
-  if (!((float)eps > 0.f) || !isfinite((float)eps)) return fail(ELAS_ERR_SHAPE, "eps must be positive and finite in float32");
+  // (a moment of 0 over an eps whose reciprocal float32 cannot hold would be NaN)
+  if (!((float)eps >= 0x1p-126f) || !isfinite((float)eps)) return fail(ELAS_ERR_SHAPE, "eps must be at least 2^-126 and finite in float32");
   if (!(max_norm >= 0.0)) return fail(ELAS_ERR_SHAPE, "max_norm must not be negative or NaN");
   if (n > 0 && (!params || !grads || !numel || !param_dtype || !grad_dtype || !decay))
     return fail(ELAS_ERR_NULL, "params, grads, numel, param_dtype, grad_dtype or decay is NULL");

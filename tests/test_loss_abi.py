@@ -158,6 +158,17 @@ def test_adamw_refusals():
     assert call(ws=None) == NULL and call(ws=A + 8) == ALIGN and call(wsb=elas.elas_adamw_workspace_bytes() - 1) == WORKSPACE
 
 
+def test_adamw_refuses_an_eps_without_a_reciprocal():
+    """0 / (0 + eps) is 0 only where 1 / eps is a float32."""
+    def call(eps):
+        p, n, t, w = (ctypes.c_void_p * 1)(A), (ctypes.c_int64 * 1)(5), (ctypes.c_int32 * 1)(0), (ctypes.c_float * 1)(0.0)
+        # (no workspace: an eps that is taken is refused for that)
+        return _status("elas_adamw_step", dict(p=p, g=p, c=None, n=n, pt=t, gt=t, w=w, count=1, bits=32, m=A, ms=None, v=A, vs=None, step=A, rate=1e-3,
+                                               factor=None, b1=0.9, b2=0.99, eps=eps, norm=None, max=1.0, **dict(WS, ws=None)))
+
+    assert call(1e-40) == SHAPE and call(2.0 ** -127) == SHAPE and call(2.0 ** -126) == NULL
+
+
 def test_adam8_values_refusals():
     def call(**kw):
         return _status("elas_adam8_values", dict(codes=A, scale=A, blocks=4, flags=0, out=A), **kw)
