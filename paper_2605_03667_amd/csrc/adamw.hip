@@ -7,7 +7,7 @@
 // at a time, 4 to a lane: a block of moments in 8 bits is one wave's, its largest magnitude
 // a maximum over the wave.  Bound by HBM where weights are float32 (1B, 246 M values with copies: 1317 us in 32 bits,
 // 5.6 TB/s; 748 in 8 bits, 5.9 TB/s), by about 60 instructions a value in 8 bits with bf16 weights and gradients (524 us, 4.7
-// TB/s).  60M, 3.9 M values: 20.6 us of kernel and 29 a call, which is what reading three lists of 49 tensors costs the host.
+// TB/s).  60M, 3.9 M values: 20.6 us of kernel, 22.3 a call.
 #include <math.h>
 
 #include <algorithm>

@@ -237,6 +237,15 @@ def elas_embed_bwd(ids, dx, V: int, scale: float = 1.0, dtable: torch.Tensor | N
 # ---- norm and clipping of the gradients ------------------------------------------------
 
 
+# Compares types, devices, shapes and strides of many tensors with those that it was made of in one call, where this torch
+# has it (three lists of 49 tensors, an AdamW step of 60M: 14.4 us of Python, 21.9 by asking each tensor).  It also says no
+# where only torch's modes differ or a tensor comes twice; each is asked then.
+try:
+    from torch._C._dynamo.guards import TensorGuards
+except ImportError:
+    TensorGuards = None
+
+
 class ElasTensors:
     """A list of GPU tensors (float32 or bf16, contiguous, any shapes) as the C ABI
     takes it.  A program that uses the same tensors every step makes it once; the
@@ -251,6 +260,7 @@ class ElasTensors:
         self._dtype = (ctypes.c_int32 * n)()
         self.layout = self._addresses = None
         self._apart = False
+        self._guard = None
         self.device = self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
 
     def __len__(self):
@@ -260,8 +270,16 @@ class ElasTensors:
         """The host arrays of addresses, lengths and types; of tensors that the call
         writes, no two may overlap."""
         ts = self.tensors
-        addresses, layout = list(map(torch.Tensor.data_ptr, ts)), (list(map(torch.Tensor.numel, ts)), [t.dtype for t in ts])
-        if addresses != self._addresses or layout != self.layout or not all(map(torch.Tensor.is_contiguous, ts)):
+        addresses = list(map(torch.Tensor.data_ptr, ts))
+        same = self._guard is not None and self._guard.check(*ts)
+        layout = self.layout if same else (list(map(torch.Tensor.numel, ts)), [t.dtype for t in ts])
+        changed = not same and (layout != self.layout or not all(map(torch.Tensor.is_contiguous, ts)))
+        if changed:
+            self._guard = None
+        if not changed and addresses == self._addresses:
+            if self._guard is None and TensorGuards is not None:
+                self._guard = TensorGuards(*ts, dynamic_dims_sizes=[list(t.shape) for t in ts], dynamic_dims_strides=[list(t.stride()) for t in ts])
+        else:
             dev = self.device.index
             for k, t in enumerate(ts):
                 if t.dtype != _F32 and t.dtype != _BF16:

@@ -1,6 +1,7 @@
 """The loss and the update as a training step uses them together: logits to losses, their
 gradient to the weights' and to AdamW with the gradients' norm, against the same steps in
 64-bit torch; the calls captured in a graph, and made on another stream."""
+import numpy as np
 import pytest
 import torch
 
@@ -328,3 +329,36 @@ def test_example_step(bits):
         moved = (v - before[k]).abs()
         assert moved.max() > 0 and (moved <= 1e-2 * (1.001 + 0.1 * before[k].abs()) + 2.0 ** -23 * before[k].abs()).all(), k
         assert torch.equal(model.w[k], v.to(BF)), k
+
+
+@pytest.mark.parametrize("change, match", [(lambda t: t.t(), "contiguous"), (lambda t: t.view(torch.int32), "float32 or torch.bfloat16"),
+                                           (lambda t: t.to(BF), None), (lambda t: t[:2], None), (lambda t: t.reshape(4, 8), None)])
+def test_a_handle_in_use_sees_what_its_tensors_became(change, match):
+    """After several steps with the same tensors, one is given another type, length or order, in the same memory or not."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(3)
+    ts = [torch.randn((8, 4), generator=gen, device=DEV) for _ in range(3)]
+    h = elas.ElasTensors(ts)
+    want = elas.elas_grad_norm(h).clone()
+    for mode in (torch.enable_grad, torch.no_grad, torch.inference_mode, torch.enable_grad):
+        with mode():
+            assert torch.equal(elas.elas_grad_norm(h), want)
+    before = ts[1].data
+    ts[1].data = change(before)
+    if match:
+        for _ in range(2):
+            with pytest.raises(ValueError, match=match):
+                elas.elas_grad_norm(h)
+    else:
+        for _ in range(3):
+            assert torch.equal(elas.elas_grad_norm(h), elas.elas_grad_norm([t.clone() for t in ts]))
+    ts[1].data = before
+    for _ in range(3):
+        assert torch.equal(elas.elas_grad_norm(h), want)
+
+
+def test_a_handle_may_hold_a_tensor_twice():
+    g = torch.full((100,), 2.0, device=DEV)
+    h = elas.ElasTensors([g, g])
+    for _ in range(4):
+        assert float(elas.elas_grad_norm(h)) == np.float32(800.0 ** 0.5)
