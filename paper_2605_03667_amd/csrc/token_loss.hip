@@ -626,17 +626,19 @@ __global__ __launch_bounds__(TH) void logp_bwd_kernel(const BwdRows a) {
 
 int groups_of(int64_t T) { return (int)std::min<int64_t>(T, kGroups); }
 
-// Whether rows are split, and how: few rows of 16 KB and more, up to 8 MB (64 x 32000 bf16, 4 MB: 7.9 us, not split 9.5;
-// 256 x 32000, 16 MB: 13.9 and 10.6), into at most 16 parts, which one thread joins for the statistics (16 x 131072
-// float32: 9.2 us with 16, 11.5 with 8, 10.3 with 32).
-constexpr int64_t kSplitRows = 256, kSplitRow = 16384, kSplitBytes = 8 << 20;
+// Whether rows are split, and how: rows of 16 KB and more, of which there are too few for a workgroup each to fill the card.
+// In us, split and not: 48 x 32000 bf16 6.8 and 9.4, 128 of them 8.6 and 9.8, 160 x 64000 14.4 and 13.6, 256 x 16000 8.3
+// and 7.7; float32, whose second read is twice as long, 48 x 32000 8.0 and 9.0, 96 x 90791 19.0 and 22.1, 96 x 32000 10.2 and
+// 9.4, 128 x 64000 19.1 and 16.4.  At most 16 parts, which one thread joins for the statistics (16 x 131072 float32: 9.2
+// us with 16, 11.5 with 8, 10.3 with 32).
+constexpr int64_t kSplitRowsBf16 = 128, kSplitRowsF32 = 96, kSplitRow = 16384;
 constexpr int kParts = 16;
 struct SplitPlan {
   bool split;
   int parts, per;
   SplitPlan(int64_t T, int64_t V, bool f32) {
     const int64_t n = f32 ? 4 : 8, pieces = (V + n - 1) / n, bytes = pieces * 16;
-    split = T > 0 && T <= kSplitRows && bytes >= kSplitRow && T * bytes <= kSplitBytes;
+    split = T > 0 && T <= (f32 ? kSplitRowsF32 : kSplitRowsBf16) && bytes >= kSplitRow;
     const int64_t at_least = (pieces + kParts * 256 - 1) / (kParts * 256);
     per = (int)(256 * std::max<int64_t>(at_least, 2));
     parts = (int)((pieces + per - 1) / per);
