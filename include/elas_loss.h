@@ -71,7 +71,7 @@ int elas_token_logp_bwd(const float* dlogp, const float* dlse, const void* logit
  * weight NULL: 1; a token of weight 0 takes no part.  logp, lse, dlogits may be
  * NULL: not wanted.  stats: device float32 [2].
  * workspace (of this call and the next): 16-byte aligned, at least
- * elas_token_loss_workspace_bytes(T, V, flags) bytes, which is 0 for sizes that no call takes.
+ * elas_token_loss_workspace_bytes(T, V, flags) bytes, which is 0 for sizes that no call takes and never less for more tokens.
  */
 size_t elas_token_loss_workspace_bytes(int64_t T, int64_t V, uint32_t flags);
 int elas_token_loss(const void* logits, int64_t ld, const void* ids, const float* weight, int64_t T, int64_t V,

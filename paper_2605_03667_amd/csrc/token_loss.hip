@@ -633,12 +633,13 @@ int groups_of(int64_t T) { return (int)std::min<int64_t>(T, kGroups); }
 // us with 16, 11.5 with 8, 10.3 with 32).
 constexpr int64_t kSplitRowsBf16 = 128, kSplitRowsF32 = 96, kSplitRow = 16384;
 constexpr int kParts = 16;
+constexpr int64_t split_rows(bool f32) { return f32 ? kSplitRowsF32 : kSplitRowsBf16; }
 struct SplitPlan {
   bool split;
   int parts, per;
   SplitPlan(int64_t T, int64_t V, bool f32) {
     const int64_t n = f32 ? 4 : 8, pieces = (V + n - 1) / n, bytes = pieces * 16;
-    split = T > 0 && T <= (f32 ? kSplitRowsF32 : kSplitRowsBf16) && bytes >= kSplitRow;
+    split = T > 0 && T <= split_rows(f32) && bytes >= kSplitRow;
     const int64_t at_least = (pieces + kParts * 256 - 1) / (kParts * 256);
     per = (int)(256 * std::max<int64_t>(at_least, 2));
     parts = (int)((pieces + per - 1) / per);
@@ -730,9 +731,11 @@ hipError_t launch_rows(const Rows& r, bool f32, const char* tag, unsigned* group
 
 }  // namespace
 
+// (never less for fewer tokens, so that what the largest batch needs will do for all)
 size_t token_loss_workspace_bytes(int64_t T, int64_t V, bool f32) {
-  const SplitPlan plan(T, V, f32);
-  return plan.split ? plan.bytes(T) : (size_t)groups_of(T) * kSums * sizeof(double);
+  const int64_t few = std::min(T, split_rows(f32));
+  const SplitPlan plan(few, V, f32);
+  return std::max(plan.split ? plan.bytes(few) : 0, (size_t)groups_of(T) * kSums * sizeof(double));
 }
 
 hipError_t run_token_loss(const LogitsArgs& a, hipStream_t stream) {

@@ -191,6 +191,13 @@ def test_workspace_of_sizes_out_of_range():
     assert 0 < elas.elas_preference_loss_workspace_bytes((1 << 40) - 1, (1 << 30) - 1) < 1 << 24
 
 
+@pytest.mark.parametrize("flags", [0, elas.ELAS_LOGITS_F32])
+@pytest.mark.parametrize("V", [1000, 8192, 32000, 131072])
+def test_the_workspace_of_a_batch_is_enough_for_smaller_ones(V, flags):
+    sizes = [elas.lib().elas_token_loss_workspace_bytes(T, V, flags) for T in range(1200)]
+    assert sizes[0] == 0 and sizes == sorted(sizes)
+
+
 def test_binding_refusals():
     """The binding's checks raise before any address is used; the tensors are on the CPU."""
     def raises(match, fn, *a, **k):
