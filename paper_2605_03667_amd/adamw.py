@@ -90,14 +90,14 @@ class ElasAdamW:
             self._copy_addresses = self.copies._addresses
         return self._copy_pointers
 
-
     def _check_apart(self, grads: ElasTensors) -> None:
         """Raises where a parameter or a copy overlaps another tensor of the step (what one
         thread writes another would read)."""
-        lists = [(self.params, True), (grads, False)] + ([(self.copies, True)] if self.copies else [])
-        seen = [t._addresses for t, _ in lists]
-        if self._disjoint is not None and all(a is b for a, b in zip(seen, self._disjoint)):
+        seen = (self.params._addresses, grads._addresses, self.copies and self.copies._addresses)
+        before = self._disjoint
+        if before is not None and seen[0] is before[0] and seen[1] is before[1] and seen[2] is before[2]:
             return
+        lists = [(self.params, True), (grads, False)] + ([(self.copies, True)] if self.copies else [])
         spans = sorted((a, a + n * t.itemsize, written) for tensors, written in lists for a, n, t in zip(tensors._addresses, *tensors.layout) if n)
         end = end_written = 0
         for start, stop, written in spans:
