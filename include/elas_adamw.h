@@ -42,7 +42,8 @@ extern "C" {
  * bits 8:  m, v uint8 [256 blocks], m_scale, v_scale float32 [blocks].  A code stands for a
  *          multiple of its block's scale: with f its lowest 3 bits (m; 4 for v) and e the 4 bits
  *          above, f where e = 0, else (f + 8) 2^(e-1) (v: f + 16); m's highest bit is its
- *          sign.  The scale is the block's largest magnitude / 245760 (v: 507904).  A magnitude
+ *          sign.  The scale is the block's largest magnitude / 245760 (v: 507904), rounded up
+ *          where that is below 2^-126.  A magnitude
  *          is rounded to one of its two neighbours by chance, so that its expectation is
  *          its value and averages that move by less than a step move all the same; the
  *          random bits are a hash of t, k and the value's index (32 bits of it), so a step can be repeated.

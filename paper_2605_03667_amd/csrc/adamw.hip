@@ -157,12 +157,16 @@ __device__ __forceinline__ void wave_max2(uint32_t& a, uint32_t& b) {
   b = (uint32_t)__builtin_amdgcn_readlane((int)v, 32);
 }
 
-// A block's magnitudes in units of its scale s: products with the reciprocal, corrected by their remainders, which came out
+// A block's scale, its largest magnitude (`top`, as bits) over the largest code, and its magnitudes in units of it: products with
+// the reciprocal, corrected by their remainders, which came out
 // as the division's rounding in all of 1.7e8 quotients of random mantissas (scales whose remainders may leave the range of
-// float32 are divided).
-__device__ __forceinline__ void in_units(float scale, const float (&x)[4], float (&y)[4]) {
-  // (a block of zeros, or of magnitudes whose scale float32 cannot hold: unit 1)
-  const float s = scale > 0.f ? scale : 1.f;
+// float32 are divided).  Below float32's normal range a scale has few bits and is rounded up: rounded down it would leave the
+// largest magnitude beyond the largest code, or be 0 with nothing left of the block.
+template <int MANTISSA>
+__device__ __forceinline__ float in_units(uint32_t top, const float (&x)[4], float (&y)[4]) {
+  constexpr float TOP = MANTISSA == 3 ? kTopM : kTopV;
+  float scale = as_float(top) * (1.f / TOP);
+  const float s = top ? scale : 1.f;       // (a block of zeros: unit 1)
   if (s >= 0x1p-90f && s <= 0x1p90f) {
     const float r0 = __builtin_amdgcn_rcpf(s), r = fmaf(fmaf(-s, r0, 1.f), r0, r0);
 #pragma unroll
@@ -171,9 +175,11 @@ __device__ __forceinline__ void in_units(float scale, const float (&x)[4], float
       y[k] = fmaf(fmaf(-q, s, v), r, q);
     }
   } else {
+    if (scale < 0x1p-126f && scale * TOP < as_float(top)) scale += 0x1p-149f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = fabsf(x[k]) / s;
+    for (int k = 0; k < 4; ++k) y[k] = fabsf(x[k]) / scale;
   }
+  return scale;
 }
 
 struct Update {
@@ -293,10 +299,8 @@ struct Block {
         top_v = b > top_v ? b : top_v;
       }
       wave_max2(top_m, top_v);
-      const float new_m = as_float(top_m) * (1.f / kTopM), new_v = as_float(top_v) * (1.f / kTopV);
       float ym[4], yv[4];
-      in_units(new_m, mv, ym);
-      in_units(new_v, vv, yv);
+      const float new_m = in_units<3>(top_m, mv, ym), new_v = in_units<4>(top_v, vv, yv);
       uint32_t to_m = 0, to_v = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
