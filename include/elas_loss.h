@@ -54,7 +54,7 @@ int elas_token_logp_fwd(const void* logits, int64_t ld, const void* ids, int64_t
  *     dlogits_tj = scale (dlogp_t (1[j = id_t] - p_tj) + dlse_t p_tj)
  *
  * lse is that of elas_token_logp_fwd on these logits (of a loss too, where no weight is 0) (p = exp(z - lse) has a relative error of 2^-24 (|z| + 3 |z - lse| + 6);
- * where |lse| is above 4096 or not finite the row's sum is taken anew); dlse NULL: zero.
+ * where |lse| is above 64 (bf16 logits: 4096) or not finite the row's sum is taken anew); dlse NULL: zero.
  */
 int elas_token_logp_bwd(const float* dlogp, const float* dlse, const void* logits, int64_t ld, const void* ids,
                         const float* lse, int64_t T, int64_t V, float scale, uint32_t flags, void* dlogits,

@@ -546,9 +546,13 @@ __global__ __launch_bounds__(1024) void loss_sum_kernel(const double* part, int 
 }
 
 // Gradient from those of logp and lse: every value by itself, kChunk pieces of a row to a thread at a time (8192 x 32000
-// bf16, by 4 waves: 168 us with 2, 174 with 4, 176 with 8 or 16).  Bound by HBM: 6.3 TB/s.  (A lse beyond kLargeLse leaves
-// exp(z - lse) an error of 2^-24 of that, and among logits of a type's lowest value it holds nothing of the sum at all.)
-constexpr float kLargeLse = 4096.f;
+// bf16, by 4 waves: 168 us with 2, 174 with 4, 176 with 8 or 16).  Bound by HBM: 6.3 TB/s.  A lse is rounded to 2^-24 of itself, and
+// exp(z - lse) is off by as much as lse is: up to 64 no more than by the exponent's own roundings at e^-20 (3 of 2^-24 of it each).
+// Beyond, the row's sum is taken anew, from one more read of it (8192 x 32000 float32: 618 us, 335 at a lse of 12; always by the row's
+// first workgroup, and so on one die in 8: 6025).  A bf16 gradient's own rounding, 2^-9, hides 2^-12, which is 4096.  (Among
+// logits of a type's lowest value a lse holds nothing of the sum at all.)
+template <class E>
+constexpr float kLargeLse = sizeof(E) == 2 ? 4096.f : 64.f;
 constexpr int kChunk = 2;
 
 struct BwdRows {
@@ -590,9 +594,11 @@ __global__ __launch_bounds__(TH) void logp_bwd_kernel(const BwdRows a) {
     const float g = a.dlogp[t], e = a.dlse ? a.dlse[t] : 0.f, lse = a.lse[t];
     const float at_label = a.scale * g, all = a.scale * (e - g);
     const int at = (int)id - cut.lead;
-    if (!(fabsf(lse) <= kLargeLse)) {
-      // the whole row by its first workgroup, which finds its maximum and sum anew
-      if (chunk > 0) continue;
+    if (!(fabsf(lse) <= kLargeLse<E>)) {
+      // the whole row by one of its workgroups, which finds its maximum and sum anew: another one from row to row, as workgroups
+      // are dealt out to the dies in turn
+      if (chunk != (int)((uint32_t)t % (uint32_t)a.chunks)) continue;
+      const bool edge = tid < cut.edges;
       const float c = a.scale * kLog2E;
       MaxSum r;
       add_long_pieces(r, c, xp, tid, cut.full, TH);
