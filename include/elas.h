@@ -79,6 +79,7 @@ extern "C" {
 #define ELAS_ERR_WORKSPACE   4  /* workspace missing or smaller than required      */
 #define ELAS_ERR_FLAGS       5  /* unknown or unsupported flag bits                */
 #define ELAS_ERR_DEVICE      6  /* a HIP call or kernel launch failed              */
+#define ELAS_ERR_OVERLAP     7  /* a result overlaps another buffer of the call    */
 
 /* ---- flags ---------------------------------------------------------------- */
 /* elas_sparsify_24: what the top-2 selection ranks (Algorithm 1). */

@@ -35,7 +35,9 @@ extern "C" {
  *                as bf16, rounded to nearest.
  * numel, decay   HOST arrays of n lengths (>= 0) and weight decays (finite).
  * The arrays are read before the call returns.  Tensors need their element's alignment
- * only.  What is written (params, copies, moments, step) overlaps nothing else of the call.
+ * only.  What is written (params, copies, moments, step) overlaps nothing else of the call: ELAS_ERR_OVERLAP
+ * between the moments, step, norm, rate_factor, workspace and anything; tensors of the lists are
+ * not compared with one another.
  * Tensor k's moments begin at value 256 sum_{j<k} ceil(numel[j] / 256) of m and v; what fills
  * up its last block is written as 0.  There are `blocks` = sum_k ceil(numel[k] / 256).
  * bits 32: m, v float32 [256 blocks]; m_scale, v_scale NULL.

@@ -19,7 +19,9 @@
  * dlogits  T rows of V values of the logits' type, row t at dlogits + t ld_out, ld_out >= V;
  *          what lies behind the V values of a row is not touched.  It may be
  *          logits itself with the same pitch (every row is read before it is
- *          written); otherwise outputs overlap nothing.
+ *          written).
+ * What a call writes, its workspace included, overlaps nothing else of it but where that is said
+ * (ELAS_ERR_OVERLAP); what lies between a row's V values and the next row is not the matrix's.
  * Per-token operands and results are float32 [T] and need 4-byte alignment.
  * Sums over the vocabulary are float32, in groups of at most 32 values, of which a thread adds up at most
  * 16 + V / 8192; per-token terms and sums over tokens are 64-bit.  Their order is fixed by the sizes, the types and the

@@ -45,7 +45,7 @@ ELAS_FWD_FUSED = 16
 ELAS_FWD_UNFUSED = 32
 
 _STATUS = {0: "ELAS_OK", 1: "ELAS_ERR_NULL", 2: "ELAS_ERR_SHAPE", 3: "ELAS_ERR_ALIGN",
-           4: "ELAS_ERR_WORKSPACE", 5: "ELAS_ERR_FLAGS", 6: "ELAS_ERR_DEVICE"}
+           4: "ELAS_ERR_WORKSPACE", 5: "ELAS_ERR_FLAGS", 6: "ELAS_ERR_DEVICE", 7: "ELAS_ERR_OVERLAP"}
 
 
 _STATUS_CODE = {v: k for k, v in _STATUS.items()}

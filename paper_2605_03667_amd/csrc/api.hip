@@ -175,6 +175,7 @@ const char* elas_status_string(int status) {
     case ELAS_ERR_WORKSPACE: return "ELAS_ERR_WORKSPACE";
     case ELAS_ERR_FLAGS: return "ELAS_ERR_FLAGS";
     case ELAS_ERR_DEVICE: return "ELAS_ERR_DEVICE";
+    case ELAS_ERR_OVERLAP: return "ELAS_ERR_OVERLAP";
     default: return "ELAS_ERR_UNKNOWN";
   }
 }

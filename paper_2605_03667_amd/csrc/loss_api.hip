@@ -4,6 +4,7 @@
 #include "checks.h"
 
 using elas::begin_call;
+using elas::check_apart;
 using elas::check_elem_ptr;
 using elas::check_optional_ptr;
 using elas::check_scale;
@@ -11,6 +12,7 @@ using elas::check_workspace;
 using elas::device_status;
 using elas::fail;
 using elas::LogitsArgs;
+using elas::Memory;
 
 namespace {
 
@@ -42,6 +44,18 @@ int check_logits(LogitsArgs& a, const void* logits, int64_t ld, const void* ids,
   return ELAS_OK;
 }
 
+// What a call on logits reads and writes.  (A gradient in its logits' place: the rows once, as a result.)
+Memory gradient(const LogitsArgs& a) {
+  const int64_t size = a.f32 ? 4 : 2;
+  return Memory(a.dlogits, a.T, a.V * size, a.ld_out * size, "dlogits");
+}
+Memory logits(const LogitsArgs& a) {
+  const int64_t size = a.f32 ? 4 : 2;
+  return Memory(a.logits == a.dlogits ? nullptr : a.logits, a.T, a.V * size, a.ld * size, "logits");
+}
+Memory ids(const LogitsArgs& a) { return Memory(a.ids, a.T * (a.ids_i64 ? 8 : 4), "ids"); }
+Memory tokens(const LogitsArgs& a, const float* p, const char* name) { return Memory(p, a.T * 4, name); }
+
 size_t workspace_of(const LogitsArgs& a) { return elas::token_loss_workspace_bytes(a.T, a.V, a.f32); }
 
 }  // namespace
@@ -62,6 +76,7 @@ int elas_token_logp_fwd(const void* logits, int64_t ld, const void* ids, int64_t
   if (T == 0) return ELAS_OK;
   ELAS_CHECK(check_elem_ptr(logp, 4, "logp"));
   ELAS_CHECK(check_optional_ptr(lse, 4, "lse"));
+  ELAS_CHECK(check_apart({tokens(a, logp, "logp"), tokens(a, lse, "lse"), ::logits(a), ::ids(a)}, 2));
   a.logp = logp; a.lse = lse;
   return device_status(elas::run_token_loss(a, (hipStream_t)stream), "log-probability launch");
 }
@@ -76,6 +91,7 @@ int elas_token_logp_bwd(const float* dlogp, const float* dlse, const void* logit
   ELAS_CHECK(check_elem_ptr(dlogp, 4, "dlogp"));
   ELAS_CHECK(check_optional_ptr(dlse, 4, "dlse"));
   ELAS_CHECK(check_elem_ptr(lse, 4, "lse"));
+  ELAS_CHECK(check_apart({gradient(a), ::logits(a), ::ids(a), tokens(a, dlogp, "dlogp"), tokens(a, dlse, "dlse"), tokens(a, lse, "lse")}, 1));
   a.dlogp = dlogp; a.dlse = dlse; a.lse_in = lse;
   return device_status(elas::run_token_logp_bwd(a, (hipStream_t)stream), "log-probability backward launch");
 }
@@ -96,6 +112,8 @@ int elas_token_loss(const void* logits, int64_t ld, const void* ids, const float
   }
   ELAS_CHECK(check_elem_ptr(stats, 4, "stats"));
   ELAS_CHECK(check_workspace(workspace, workspace_bytes, workspace_of(a)));
+  ELAS_CHECK(check_apart({tokens(a, logp, "logp"), tokens(a, lse, "lse"), gradient(a), Memory(stats, 8, "stats"),
+                          Memory(workspace, (int64_t)workspace_of(a), "workspace"), ::logits(a), ::ids(a), tokens(a, weight, "weight")}, 5));
   a.weight = weight; a.reduce = reduce; a.z_coef = z_coef; a.logp = logp; a.lse = lse; a.stats = stats; a.ws = workspace;
   return device_status(elas::run_token_loss(a, (hipStream_t)stream), "token loss launch");
 }
@@ -122,6 +140,9 @@ int elas_policy_loss(const void* logits, int64_t ld, const void* ids, const floa
   }
   ELAS_CHECK(check_elem_ptr(stats, 4, "stats"));
   ELAS_CHECK(check_workspace(workspace, workspace_bytes, workspace_of(a)));
+  ELAS_CHECK(check_apart({tokens(a, logp, "logp"), gradient(a), Memory(stats, 12, "stats"),
+                          Memory(workspace, (int64_t)workspace_of(a), "workspace"), ::logits(a), ::ids(a), tokens(a, advantage, "advantage"),
+                          tokens(a, old_logp, "old_logp"), tokens(a, ref_logp, "ref_logp"), tokens(a, weight, "weight")}, 4));
   a.advantage = advantage; a.old_logp = old_logp; a.ref_logp = ref_logp; a.weight = weight; a.reduce = reduce;
   a.low = 1.f - clip_low; a.high = 1.f + clip_high; a.kl_coef = kl_coef; a.logp = logp; a.stats = stats; a.ws = workspace;
   return device_status(elas::run_token_loss(a, (hipStream_t)stream), "policy loss launch");
@@ -151,7 +172,12 @@ int elas_preference_loss(const float* logp, const float* ref_logp, const void* o
   }
   if (N > 0) ELAS_CHECK(check_optional_ptr(dlogp, 4, "dlogp"));
   ELAS_CHECK(check_elem_ptr(stats, 4, "stats"));
-  ELAS_CHECK(check_workspace(workspace, workspace_bytes, elas::preference_workspace_bytes(N, pairs)));
+  const size_t need = elas::preference_workspace_bytes(N, pairs);
+  ELAS_CHECK(check_workspace(workspace, workspace_bytes, need));
+  // (a gradient in logp's place: once, as a result)
+  ELAS_CHECK(check_apart({Memory(margin, 4 * pairs, "margin"), Memory(dlogp, 4 * N, "dlogp"), Memory(stats, 12, "stats"),
+                          Memory(workspace, (int64_t)need, "workspace"), Memory(logp == dlogp ? nullptr : logp, 4 * N, "logp"),
+                          Memory(ref_logp, 4 * N, "ref_logp"), Memory(pairs ? offsets : nullptr, (2 * pairs + 1) * (a.i64 ? 8 : 4), "offsets")}, 4));
   a.N = N; a.pairs = pairs; a.logp = logp; a.ref = ref_logp; a.offsets = offsets; a.beta = beta; a.smoothing = smoothing;
   a.margin = margin; a.dlogp = N > 0 ? dlogp : nullptr; a.stats = stats; a.ws = workspace;
   return device_status(elas::run_preference(a, (hipStream_t)stream), "preference loss launch");
