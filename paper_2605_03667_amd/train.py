@@ -238,12 +238,23 @@ def elas_embed_bwd(ids, dx, V: int, scale: float = 1.0, dtable: torch.Tensor | N
 
 
 # Compares types, devices, shapes and strides of many tensors with those that it was made of in one call, where this torch
-# has it (three lists of 49 tensors, an AdamW step of 60M: 14.4 us of Python, 21.9 by asking each tensor).  It also says no
-# where only torch's modes differ or a tensor comes twice; each is asked then.
+# has it (three lists of 49 tensors, an AdamW step of 60M: 14.4 us of Python, 21.9 by asking each tensor).  The class is not part of
+# torch's documented interface, so whatever goes wrong with it is as if it were not there.  It also says no where only torch's
+# modes differ or a tensor comes twice; each tensor is asked then, and after _GUARDS such answers without a change always.
 try:
     from torch._C._dynamo.guards import TensorGuards
 except ImportError:
     TensorGuards = None
+_GUARDS = 3
+
+
+def _guard(ts):
+    """A comparison of the tensors ``ts`` with what they are now, or None where there is none that agrees."""
+    try:
+        guard = TensorGuards(*ts, dynamic_dims_sizes=[list(t.shape) for t in ts], dynamic_dims_strides=[list(t.stride()) for t in ts])
+        return guard if guard.check(*ts) else None
+    except Exception:
+        return None
 
 
 class ElasTensors:
@@ -260,7 +271,7 @@ class ElasTensors:
         self._dtype = (ctypes.c_int32 * n)()
         self.layout = self._addresses = None
         self._apart = False
-        self._guard = None
+        self._guard, self._guards = None, _GUARDS
         self.device = self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
 
     def __len__(self):
@@ -271,14 +282,22 @@ class ElasTensors:
         writes, no two may overlap."""
         ts = self.tensors
         addresses = list(map(torch.Tensor.data_ptr, ts))
-        same = self._guard is not None and self._guard.check(*ts)
+        same = False
+        if self._guard is not None:
+            try:
+                same = self._guard.check(*ts)
+            except Exception:
+                pass
+            if not same:
+                self._guard = None
         layout = self.layout if same else (list(map(torch.Tensor.numel, ts)), [t.dtype for t in ts])
         changed = not same and (layout != self.layout or not all(map(torch.Tensor.is_contiguous, ts)))
         if changed:
-            self._guard = None
+            self._guards = _GUARDS
         if not changed and addresses == self._addresses:
-            if self._guard is None and TensorGuards is not None:
-                self._guard = TensorGuards(*ts, dynamic_dims_sizes=[list(t.shape) for t in ts], dynamic_dims_strides=[list(t.stride()) for t in ts])
+            if self._guard is None and self._guards:
+                self._guards -= 1
+                self._guard = _guard(ts)
         else:
             dev = self.device.index
             for k, t in enumerate(ts):
