@@ -31,7 +31,8 @@ _SIGNATURES.update({
 class ElasAdamW:
     """The state of AdamW over a list of tensors: the parameters (float32 or bf16,
     contiguous, any shapes), their bf16 copies where there are any (one for each
-    parameter, None for those without one), a weight decay for each, and the moments.
+    parameter, None for those without one), a weight decay for each (``decay``: set as a
+    whole, also between steps), and the moments.
 
     ``bits`` is 32 or 8.  The moments ``m`` and ``v`` are flat tensors (float32, or
     uint8 codes with a float32 scale for each block of 256 in ``m_scale`` and
@@ -46,14 +47,10 @@ class ElasAdamW:
         n = len(self.params)
         self.params.arrays(written=True)
         copies = [None] * n if copies is None else list(copies.tensors if isinstance(copies, ElasTensors) else copies)
-        decay = [float(d) for d in decay] if hasattr(decay, "__len__") else [float(decay)] * n
-        if len(copies) != n or len(decay) != n:
-            raise ValueError(f"{n} parameters, {len(copies)} copies, {len(decay)} decays")
-        if not all(map(math.isfinite, decay)):
-            raise ValueError("decay must be finite")
+        if len(copies) != n:
+            raise ValueError(f"{n} parameters, {len(copies)} copies")
         self.bits = bits
         self.decay = decay
-        self._decay = (_f32 * n)(*decay)
         self._with_copy = [k for k, c in enumerate(copies) if c is not None]
         self.copies = ElasTensors([copies[k] for k in self._with_copy]) if self._with_copy else None
         self._copy_pointers = (_p * n)()
@@ -72,6 +69,20 @@ class ElasAdamW:
 
     def __len__(self):
         return len(self.params)
+
+    @property
+    def decay(self) -> tuple:
+        return self._decays
+
+    @decay.setter
+    def decay(self, decay) -> None:
+        n = len(self.params)
+        decay = tuple(float(d) for d in decay) if hasattr(decay, "__len__") else (float(decay),) * n
+        if len(decay) != n:
+            raise ValueError(f"{n} parameters, {len(decay)} decays")
+        if not all(map(math.isfinite, decay)):
+            raise ValueError("decay must be finite")
+        self._decays, self._decay = decay, (_f32 * n)(*decay)
 
     def _check_copies(self):
         """The host array of the copies' addresses (None: there are none)."""
