@@ -127,17 +127,4 @@ __device__ __forceinline__ double block_sums(const double (&s)[K], double (*lds)
   return v;
 }
 
-// Of bit patterns: for magnitudes in the order of their values, NaN above them all.
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-  const auto step = [&](uint32_t o) { v = v > o ? v : o; };
-  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));
-  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));
-  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));
-  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true));
-  const auto s16 = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = s16[0] > s16[1] ? s16[0] : s16[1];
-  const auto s32 = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return s32[0] > s32[1] ? s32[0] : s32[1];
-}
-
 }  // namespace elas

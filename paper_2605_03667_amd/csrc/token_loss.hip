@@ -308,9 +308,9 @@ __global__ __launch_bounds__(Team<WAVES>::THREADS * Team<WAVES>::ROWS) void rows
 }
 
 // A loss with its gradient, the row in the registers of its team: PARTS pieces to a thread, what lies
-// behind the row -inf.  BEYOND: a longer row, whose pieces behind those are read twice (4000 x 160000 bf16: 599 us, with 12
-// held, which spill, 865; 4000 x 131072 float32:
-// 853 us, 1300 with all of it read twice).  Loads and stores are non-temporal (65536 x 32000 bf16: 1488 us, with plain
+// behind the row -inf.  BEYOND: a longer row, whose pieces behind those are read twice (4000 x 160000 bf16: 565 to 599 us, with 12
+// held, which spill, 865; 4000 x 131072 float32: 853 us, 1300 with all of it read twice; of these teams' 128 registers up to
+// 8 still go to scratch memory).  Loads and stores are non-temporal (65536 x 32000 bf16: 1488 us, with plain
 // loads 1548; before them, plain stores too, 1597 for 1537).
 template <int KIND, class E, int WAVES, int PARTS, bool BEYOND>
 __global__ __launch_bounds__(Team<WAVES>::THREADS * Team<WAVES>::ROWS) void held_kernel(const Rows a) {
@@ -651,8 +651,8 @@ int groups_of(int64_t T) { return (int)std::min<int64_t>(T, kGroups); }
 
 // Whether rows are split, and how: rows of 16 KB and more, of which there are too few for a workgroup each to fill the card.
 // In us, split and not: 48 x 32000 bf16 6.8 and 9.4, 128 of them 8.6 and 9.8, 160 x 64000 14.4 and 13.6, 256 x 16000 8.3
-// and 7.7; float32, whose second read is twice as long, 48 x 32000 8.0 and 9.0, 96 x 90791 19.0 and 22.1, 96 x 32000 10.2 and
-// 9.4, 128 x 64000 19.1 and 16.4.  At most 16 parts, which one thread joins for the statistics (16 x 131072 float32: 9.2
+// and 7.7; float32, whose second read is twice as long, 48 x 32000 8.0 and 9.0, 96 x 90791 19.0 and 22.1, 128 x 64000 19.1
+// and 16.4.  Rows alone do not say it all: 96 x 32000 float32 loses 0.8 us by it (10.2 and 9.4), where 96 x 90791 gains 3.1.  At most 16 parts, which one thread joins for the statistics (16 x 131072 float32: 9.2
 // us with 16, 11.5 with 8, 10.3 with 32).
 constexpr int64_t kSplitRowsBf16 = 128, kSplitRowsF32 = 96, kSplitRow = 16384;
 constexpr int kParts = 16;
