@@ -95,7 +95,7 @@ int elas_token_loss(const void* logits, int64_t ld, const void* ids, const float
  * old_logp NULL: the policy that sampled the tokens is this one (r = 1, with its
  * gradient).  ref_logp NULL: no KL term (kl_coef is then 0).  weight NULL: 1; a
  * token of weight 0 takes no part.  logp and dlogits may be NULL: not wanted.
- * stats: device float32 [3].  Requires 0 <= clip_low <= 1, clip_high >= 0, finite coefficients.
+ * stats: device float32 [3].  Requires 0 <= clip_low <= 1, clip_high >= 0 (infinite: no upper bound), finite reduce and kl_coef.
  */
 int elas_policy_loss(const void* logits, int64_t ld, const void* ids, const float* advantage, const float* old_logp,
                      const float* ref_logp, const float* weight, int64_t T, int64_t V, float scale, float reduce,

@@ -652,8 +652,8 @@ int groups_of(int64_t T) { return (int)std::min<int64_t>(T, kGroups); }
 // Whether rows are split, and how: rows of 16 KB and more, of which there are too few for a workgroup each to fill the card.
 // In us, split and not: 48 x 32000 bf16 6.8 and 9.4, 128 of them 8.6 and 9.8, 160 x 64000 14.4 and 13.6, 256 x 16000 8.3
 // and 7.7; float32, whose second read is twice as long, 48 x 32000 8.0 and 9.0, 96 x 90791 19.0 and 22.1, 128 x 64000 19.1
-// and 16.4.  Rows alone do not say it all: 96 x 32000 float32 loses 0.8 us by it (10.2 and 9.4), where 96 x 90791 gains 3.1.  At most 16 parts, which one thread joins for the statistics (16 x 131072 float32: 9.2
-// us with 16, 11.5 with 8, 10.3 with 32).
+// and 16.4.  Rows alone do not say it all: 96 x 32000 float32 loses 0.8 us by it (10.2 and 9.4), where 96 x 90791 gains 3.1.  At
+// most 16 parts, which one thread joins for the statistics (16 x 131072 float32: 9.2 us with 16, 11.5 with 8, 10.3 with 32).
 constexpr int64_t kSplitRowsBf16 = 128, kSplitRowsF32 = 96, kSplitRow = 16384;
 constexpr int kParts = 16;
 constexpr int64_t split_rows(bool f32) { return f32 ? kSplitRowsF32 : kSplitRowsBf16; }
